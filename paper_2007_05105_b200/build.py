@@ -6,13 +6,14 @@ import subprocess
 import sys
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(_HERE, "csrc", "adascale.cu")]
-HEADERS = [os.path.join(os.path.dirname(_HERE), "include", "adascale.h"),
-           os.path.join(_HERE, "csrc", "adascale_kernels.cuh")]
+_SOURCE_NAMES = ("adascale.cu", "ops_embed.cu", "ops_distill.cu", "ops_norm.cu")
+SOURCES = [os.path.join(_HERE, "csrc", name) for name in _SOURCE_NAMES]
+HEADERS = [os.path.join(os.path.dirname(_HERE), "include", name) for name in ("adascale.h", "adascale_ops.h")] + \
+          [os.path.join(_HERE, "csrc", name) for name in ("adascale_kernels.cuh", "ops_common.cuh")]
 LIB = os.path.join(_HERE, "libadascale_b200.so")
 
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
 
 
 def _nvcc():

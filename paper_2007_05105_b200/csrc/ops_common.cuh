@@ -1,0 +1,188 @@
+#pragma once
+// Shared by the language-model operators (ops_embed.cu, ops_distill.cu, ops_norm.cu): element types,
+// 16-byte accesses, launches and argument checks.  The operators' C ABI is include/adascale_ops.h.
+#include "../../include/adascale_ops.h"
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+namespace {
+
+typedef __nv_bfloat16 bf16;
+
+constexpr long long kMaxRows = ADASCALE_OPS_MAX_ROWS;
+
+// ---- element types -------------------------------------------------------------------------
+
+template <int DT> struct ElemOf;
+template <> struct ElemOf<ADASCALE_F32> { typedef float type; };
+template <> struct ElemOf<ADASCALE_BF16> { typedef bf16 type; };
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(bf16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void put(float *p, float x) { *p = x; }
+__device__ __forceinline__ void put(bf16 *p, float x) { *p = __float2bfloat16_rn(x); }
+
+// The two bf16 values of a 32-bit word, widened (exact).
+__device__ __forceinline__ float bf_lo(unsigned w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ unsigned bf_pack(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const unsigned *>(&v);
+}
+
+// V adjacent elements as 32-bit floats; V > 1 wants the address aligned to the smaller of V
+// elements and 16 bytes.
+template <int V> __device__ __forceinline__ void load_vec(const float *p, float (&x)[V])
+{
+    if constexpr (V == 1) {
+        x[0] = *p;
+    } else {
+        static_assert(V % 4 == 0, "whole 16-byte accesses");
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i) {
+            const float4 q = reinterpret_cast<const float4 *>(p)[i];
+            x[4 * i] = q.x;
+            x[4 * i + 1] = q.y;
+            x[4 * i + 2] = q.z;
+            x[4 * i + 3] = q.w;
+        }
+    }
+}
+template <int V> __device__ __forceinline__ void load_vec(const bf16 *p, float (&x)[V])
+{
+    if constexpr (V == 1) {
+        x[0] = to_f32(*p);
+    } else if constexpr (V == 4) {
+        const uint2 q = *reinterpret_cast<const uint2 *>(p);
+        x[0] = bf_lo(q.x);
+        x[1] = bf_hi(q.x);
+        x[2] = bf_lo(q.y);
+        x[3] = bf_hi(q.y);
+    } else {
+        static_assert(V % 8 == 0, "whole 16-byte accesses");
+#pragma unroll
+        for (int i = 0; i < V / 8; ++i) {
+            const uint4 q = reinterpret_cast<const uint4 *>(p)[i];
+            x[8 * i] = bf_lo(q.x);
+            x[8 * i + 1] = bf_hi(q.x);
+            x[8 * i + 2] = bf_lo(q.y);
+            x[8 * i + 3] = bf_hi(q.y);
+            x[8 * i + 4] = bf_lo(q.z);
+            x[8 * i + 5] = bf_hi(q.z);
+            x[8 * i + 6] = bf_lo(q.w);
+            x[8 * i + 7] = bf_hi(q.w);
+        }
+    }
+}
+template <int V> __device__ __forceinline__ void store_vec(float *p, const float (&x)[V])
+{
+    if constexpr (V == 1) {
+        *p = x[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i)
+            reinterpret_cast<float4 *>(p)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
+}
+template <int V> __device__ __forceinline__ void store_vec(bf16 *p, const float (&x)[V])
+{
+    if constexpr (V == 1) {
+        put(p, x[0]);
+    } else if constexpr (V == 4) {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(bf_pack(x[0], x[1]), bf_pack(x[2], x[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < V / 8; ++i)
+            reinterpret_cast<uint4 *>(p)[i] = make_uint4(bf_pack(x[8 * i], x[8 * i + 1]), bf_pack(x[8 * i + 2], x[8 * i + 3]),
+                                                         bf_pack(x[8 * i + 4], x[8 * i + 5]), bf_pack(x[8 * i + 6], x[8 * i + 7]));
+    }
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// A token id or label of either width.
+__device__ __forceinline__ long long load_id(const void *p, int wide, long long i)
+{
+    return wide ? static_cast<const long long *>(p)[i] : (long long)static_cast<const int *>(p)[i];
+}
+
+// ---- programmatic dependent launch ---------------------------------------------------------
+// The rule of adascale_kernels.cuh: a kernel lets its successor start early only after its own
+// wait has returned, and touches nothing in global memory before that wait.
+__device__ __forceinline__ void griddep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// ---- host side -----------------------------------------------------------------------------
+
+// cluster > 1: blocks per cluster (n_blocks is a multiple of it).
+template <typename Args>
+cudaError_t launch(void (*kernel)(Args), long long n_blocks, int threads, size_t smem, cudaStream_t s, const Args &a,
+                   int cluster = 1)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)n_blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+#define OPS_CU(...)                                    \
+    do {                                               \
+        if ((__VA_ARGS__) != cudaSuccess) {            \
+            (void)cudaGetLastError(); /* not sticky */ \
+            return ADASCALE_ERR_CUDA;                  \
+        }                                              \
+    } while (0)
+
+// Streaming multiprocessors of the current device (asked once per device).
+inline int sm_count()
+{
+    static int known[64] = {0};  // benign race: every thread writes the same number
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev >= 0 && dev < 64 && known[dev]) return known[dev];
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (dev >= 0 && dev < 64) known[dev] = n;
+    return n;
+}
+
+inline bool is_dtype(int d) { return d == ADASCALE_F32 || d == ADASCALE_BF16; }
+inline bool is_itype(int d) { return d == ADASCALE_I32 || d == ADASCALE_I64; }
+inline int elem_bytes(int dtype) { return dtype == ADASCALE_F32 ? 4 : 2; }
+inline int id_bytes(int itype) { return itype == ADASCALE_I32 ? 4 : 8; }
+inline bool on(const void *p, int bytes) { return (uintptr_t)p % (uintptr_t)bytes == 0; }
+// Every row of the matrix starts on a boundary of `bytes`; an absent matrix does not object.
+inline bool rows_on(const void *p, long long ld, long long n_rows, int elem, int bytes)
+{
+    return !p || (on(p, bytes) && (n_rows <= 1 || ld * elem % bytes == 0));
+}
+__host__ __device__ inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+}  // namespace
