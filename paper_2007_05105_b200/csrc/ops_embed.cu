@@ -74,13 +74,20 @@ struct Pair {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortCluster = 8;      // portable cluster size
+constexpr int kSortCluster = 8;      // blocks that sort together (portable cluster size); 1 for short lists
+constexpr int kSortAlone = 2048;     // tokens up to which one block sorts on its own
 constexpr int kSortBits = 8;         // digit of one pass
 constexpr int kSortBins = 1 << kSortBits;
-constexpr int kZeroRun = 16;         // adjacent vocabulary rows that belong to one block of the zero-fill
+constexpr int kZeroBlocks = 112;     // blocks that write zeros beside the sort: 15 clusters of 8 are resident at once (with 17, 32 us for 22)
+constexpr int kZeroRun = 16;         // adjacent vocabulary rows that belong to one of them
 constexpr int kZeroBits = 32 * 1024; // rows that a block keeps presence bits of at a time
-constexpr int kWindow = 64;          // sorted entries of one window
+constexpr int kBatch = 8;            // tokens that a thread requests together
 constexpr int kSumThreads = 128;
+constexpr int kDepth = 16;             // rows on their way per thread of the window sums
+constexpr int kSumBlocks = 5;       // their blocks per SM
+constexpr int kMostPairs = 1024;     // sorted entries that a block of them holds
+constexpr int kLeastWindow = 8;
+constexpr int kSpill = 8;            // entries that a window takes from the next one to finish its last run
 
 struct SortArgs {
     const void *tokens;
@@ -89,7 +96,6 @@ struct SortArgs {
     long long n, vocab, ld_grad, padding;
     long long row_bytes;  // of the gradient; its rows are zeroed where no token points
     int wide, passes;
-    int zero_blocks;    // blocks after the sorting cluster; 0 when accumulating
     int grad_bytes;     // bytes of a gradient element
     int vec;            // gradient rows can be written in 16-byte pieces
 };
@@ -100,34 +106,43 @@ __device__ __forceinline__ int key_of(const SortArgs &a, long long i)
     return id >= 0 && id < a.vocab && id != a.padding ? (int)id : (int)a.vocab;
 }
 
-// Zeros for the rows that no token names.  Block z of Z has the vocabulary rows whose run number
-// (row / kZeroRun) is z modulo Z, so that a batch that uses only frequent, adjacent ids still
-// spreads evenly.  It marks the present ones in a bit field while it reads the whole list of
-// tokens (from L2: the list is small beside what is written), then writes the others.
-__device__ void zero_absent(const SortArgs &a, unsigned *bits, int z)
+// Zeros for the rows that no token names, while the first cluster sorts.  Block z has the
+// vocabulary rows whose run number (row / kZeroRun) is z modulo kZeroBlocks, so that a batch that uses
+// only frequent, adjacent ids still spreads evenly.  The blocks of a cluster share the reading
+// of the token list: each reads its part and sets presence bits in the shared memory of
+// the block that has the row; then every block writes its absent rows.
+__device__ void zero_absent(const SortArgs &a, unsigned *bits, const cg::cluster_group &cluster, int z)
 {
-    const int Z = a.zero_blocks;
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const long long runs = ceil_div(a.vocab, kZeroRun);
-    const long long mine = z < runs ? (runs - 1 - z) / Z + 1 : 0;  // runs of this block
+    const long long most = ceil_div(runs, kZeroBlocks);  // runs of a block
     constexpr int kRuns = kZeroBits / kZeroRun;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (long long r0 = 0; r0 < mine; r0 += kRuns) {
-        const int here = (int)(mine - r0 < kRuns ? mine - r0 : kRuns);
-        __syncthreads();
-        for (int i = threadIdx.x; i < (here * kZeroRun + 31) / 32; i += kSortThreads) bits[i] = 0u;
-        __syncthreads();
-        for (long long i = threadIdx.x; i < a.n; i += kSortThreads) {
-            const unsigned key = (unsigned)key_of(a, i), run = key / kZeroRun;
-            if (run % (unsigned)Z != (unsigned)z) continue;
-            const long long local = (long long)(run / (unsigned)Z) - r0;
-            if (local < 0 || local >= here) continue;
-            const int b = (int)local * kZeroRun + (int)(key % kZeroRun);
-            atomicOr(&bits[b >> 5], 1u << (b & 31));
+    const long long part = ceil_div(a.n, blocks), from = part * rank, to = from + part < a.n ? from + part : a.n;
+    for (long long r0 = 0; r0 < most; r0 += kRuns) {
+        const int here = (int)(most - r0 < kRuns ? most - r0 : kRuns);
+        for (int i = threadIdx.x; i < here * kZeroRun / 32 + 1; i += kSortThreads) bits[i] = 0u;
+        cluster.sync();
+        for (long long i0 = from + threadIdx.x; i0 < to; i0 += kBatch * kSortThreads) {
+            unsigned key[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const long long i = i0 + u * kSortThreads;
+                key[u] = i < to ? (unsigned)key_of(a, i) : (unsigned)a.vocab;
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const unsigned run = key[u] / kZeroRun, owner = run % kZeroBlocks;
+                const long long local = (long long)(run / kZeroBlocks) - r0;
+                if (owner / blocks != (unsigned)(z / blocks) || local < 0 || local >= here || key[u] == (unsigned)a.vocab) continue;
+                const int b = (int)local * kZeroRun + (int)(key[u] % kZeroRun);
+                atomicOr(cluster.map_shared_rank(&bits[b >> 5], owner % blocks), 1u << (b & 31));
+            }
         }
-        __syncthreads();
+        cluster.sync();
         for (int b = warp; b < here * kZeroRun; b += kSortWarps) {
             if (bits[b >> 5] >> (b & 31) & 1u) continue;
-            const long long row = ((r0 + b / kZeroRun) * Z + z) * kZeroRun + b % kZeroRun;
+            const long long row = ((r0 + b / kZeroRun) * kZeroBlocks + z) * kZeroRun + b % kZeroRun;
             if (row >= a.vocab) continue;
             char *p = static_cast<char *>(a.grad) + row * a.ld_grad * a.grad_bytes;
             if (a.vec) {
@@ -138,12 +153,27 @@ __device__ void zero_absent(const SortArgs &a, unsigned *bits, int z)
                 for (long long j = lane; j < a.row_bytes / 2; j += 32) reinterpret_cast<unsigned short *>(p)[j] = 0;
             }
         }
+        __syncthreads();  // the bits are read before the next range clears them
     }
 }
 
-// Stable radix sort of (token, position) by token, least significant digit first, by the eight
-// blocks of one cluster.  Every warp owns a contiguous stretch of the current order.  Per pass: it
-// counts its stretch's digits in shared memory (match_any groups equal digits of 32 entries, one
+// Lanes of the warp with this lane's digit, among those in `has`.  Eight votes: __match_any_sync
+// took about 800 cycles a call here with 32 warps at it.
+__device__ __forceinline__ unsigned same_digit(unsigned digit, unsigned has)
+{
+    unsigned same = has;
+#pragma unroll
+    for (int b = 0; b < kSortBits; ++b) {
+        const bool set = digit >> b & 1u;
+        const unsigned vote = __ballot_sync(0xffffffffu, set);
+        same &= set ? vote : ~vote;
+    }
+    return same;
+}
+
+// Stable radix sort of (token, position) by token, least significant digit first, by the blocks
+// of one cluster.  Every warp owns a contiguous stretch of the current order.  Per pass: it
+// counts its stretch's digits in shared memory (votes group equal digits of 32 entries, one
 // lane adds the group's size: no atomics, and the order within a group is the lane order), the
 // counts are turned into first destinations (over digits, blocks and warps in that order; block
 // totals travel through distributed shared memory), and a second walk over the stretch writes
@@ -153,18 +183,19 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_tokens(const __grid_co
 {
     __shared__ unsigned count[kSortWarps][kSortBins];  // also the bit field of the zero-fill
     __shared__ unsigned total[kSortBins];              // of this block, read by the whole cluster
-    __shared__ unsigned scan[kSortBins / 32];
+    __shared__ unsigned scan[kSortBins / 32], start[kSortBins];
     static_assert(sizeof(count) * 8 >= kZeroBits, "the zero-fill's bits fit");
     griddep_wait();
     griddep_launch();
-    if (blockIdx.x >= kSortCluster) {
-        zero_absent(a, &count[0][0], blockIdx.x - kSortCluster);
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks();
+    if ((int)blockIdx.x >= blocks) {
+        zero_absent(a, &count[0][0], cluster, (int)blockIdx.x - blocks);
         return;
     }
-    cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = (int)blockIdx.x;
     const unsigned below = (1u << lane) - 1u;
-    const long long stretch = ceil_div(ceil_div(a.n, kSortCluster * kSortWarps), 32) * 32;
+    const long long stretch = ceil_div(ceil_div(a.n, blocks * kSortWarps), 32) * 32;
     const long long first = ((long long)rank * kSortWarps + warp) * stretch;
     const long long last = first + stretch < a.n ? first + stretch : a.n;
 
@@ -172,20 +203,41 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_tokens(const __grid_co
         const Pair *src = a.buf[pass & 1];
         Pair *dst = a.buf[(pass + 1) & 1];
         const int shift = pass * kSortBits;
+        Pair p[kBatch];  // of the batch read last: a stretch of one batch is read once per pass
+        auto read = [&](long long i0) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const long long i = i0 + 32 * u + lane;
+                p[u].key = p[u].pos = 0;
+                if (i >= last) continue;
+                if (pass) {
+                    const int2 q = __ldcg(reinterpret_cast<const int2 *>(src) + i);
+                    p[u].key = q.x;
+                    p[u].pos = q.y;
+                } else {
+                    p[u].key = key_of(a, i);
+                    p[u].pos = (int)i;
+                }
+            }
+        };
         for (int i = lane; i < kSortBins; i += 32) count[warp][i] = 0u;
         __syncwarp();
-        for (long long i0 = first; i0 < last; i0 += 32) {
-            const long long i = i0 + lane;
-            const bool has = i < last;
-            const int key = !has ? 0 : pass ? __ldcg(&src[i].key) : key_of(a, i);
-            const unsigned digit = has ? (unsigned)key >> shift & (kSortBins - 1) : kSortBins;
-            const unsigned same = __match_any_sync(0xffffffffu, digit);
-            if (has && !(same & below)) count[warp][digit] += __popc(same);
-            __syncwarp();
+        for (long long i0 = first; i0 < last; i0 += 32 * kBatch) {
+            read(i0);
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                if (i0 + 32 * u >= last) break;
+                const bool has = i0 + 32 * u + lane < last;
+                const unsigned digit = (unsigned)p[u].key >> shift & (kSortBins - 1);
+                const unsigned same = same_digit(digit, __ballot_sync(0xffffffffu, has));
+                if (has && !(same & below)) count[warp][digit] += __popc(same);
+                __syncwarp();
+            }
         }
         __syncthreads();
         unsigned sum = 0;
         if (tid < kSortBins) {  // exclusive prefix over the block's warps; the block's total
+#pragma unroll 8
             for (int w = 0; w < kSortWarps; ++w) {
                 const unsigned c = count[w][tid];
                 count[w][tid] = sum;
@@ -196,8 +248,8 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_tokens(const __grid_co
         cluster.sync();
         unsigned before = 0, all = 0;  // entries with this digit in earlier blocks, in the cluster
         if (tid < kSortBins) {
-#pragma unroll
-            for (int r = 0; r < kSortCluster; ++r) {
+#pragma unroll 8
+            for (int r = 0; r < blocks; ++r) {
                 const unsigned c = *cluster.map_shared_rank(&total[tid], r);
                 before += r < rank ? c : 0u;
                 all += c;
@@ -214,31 +266,25 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_tokens(const __grid_co
         __syncthreads();
         if (tid < kSortBins) {
             for (int w = 0; w < warp; ++w) before += scan[w];
-            for (int w = 0; w < kSortWarps; ++w) count[w][tid] += before;
+            start[tid] = before;
         }
         __syncthreads();
-        for (long long i0 = first; i0 < last; i0 += 32) {
-            const long long i = i0 + lane;
-            const bool has = i < last;
-            Pair p;
-            if (has && pass) {
-                const int2 q = __ldcg(reinterpret_cast<const int2 *>(src) + i);
-                p.key = q.x;
-                p.pos = q.y;
-            } else {
-                p.key = has ? key_of(a, i) : 0;
-                p.pos = (int)i;
+        for (long long i0 = first; i0 < last; i0 += 32 * kBatch) {
+            if (stretch > 32 * kBatch) read(i0);
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                if (i0 + 32 * u >= last) break;
+                const bool has = i0 + 32 * u + lane < last;
+                const unsigned digit = (unsigned)p[u].key >> shift & (kSortBins - 1);
+                const unsigned same = same_digit(digit, __ballot_sync(0xffffffffu, has));
+                const unsigned at = has ? start[digit] + count[warp][digit] + __popc(same & below) : 0u;
+                __syncwarp();
+                if (has && !(same & below)) count[warp][digit] += __popc(same);
+                if (has) reinterpret_cast<int2 *>(dst)[at] = make_int2(p[u].key, p[u].pos);
+                __syncwarp();
             }
-            const unsigned digit = has ? (unsigned)p.key >> shift & (kSortBins - 1) : kSortBins;
-            const unsigned same = __match_any_sync(0xffffffffu, digit);
-            const unsigned at = has ? count[warp][digit] + __popc(same & below) : 0u;
-            __syncwarp();
-            if (has && !(same & below)) count[warp][digit] += __popc(same);
-            if (has) reinterpret_cast<int2 *>(dst)[at] = make_int2(p.key, p.pos);
-            __syncwarp();
         }
-        // the next pass reads what all blocks wrote (and their totals are free again)
-        __threadfence();
+        // the next pass reads what all blocks wrote (the barrier orders it), and their totals are free again
         cluster.sync();
     }
 }
@@ -247,19 +293,35 @@ struct SumArgs {
     const Pair *sorted;
     const void *dout;
     void *grad;
-    float *pieces;      // [windows][2][ld_piece]: a window's part of a long run: 0 one that began earlier, 1 one that begins here
+    float *pieces;      // [windows][2][ld_piece]: a window's part of a run that 0 began earlier, 1 begins here and goes on
     long long n, vocab, ld_dout, ld_grad, ld_piece;
+    int window;         // sorted entries of one window
     int nv;             // vectors of a row
     int accumulate;
     float scale;
 };
 
+// A row's sums (V columns at c) to the gradient.  Accumulating into 32 bits is left to the L2
+// cache, which adds without making the walk wait for the old value (one thread has the element, so
+// the order is fixed); bf16 needs the one rounding of old + new and is read, added and written here.
 template <typename GT, int V>
 __device__ __forceinline__ void write_row(const SumArgs &a, int key, int c, float (&acc)[V])
 {
     GT *p = static_cast<GT *>(a.grad) + (long long)key * a.ld_grad + (long long)c * V;
     float out[V];
     if (a.accumulate) {
+        if constexpr (sizeof(GT) == 4) {
+            if constexpr (V == 1) {
+                asm volatile("red.global.add.f32 [%0], %1;" ::"l"(p), "f"(a.scale * acc[0]) : "memory");
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i += 4)
+                    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p + i), "f"(a.scale * acc[i]),
+                                 "f"(a.scale * acc[i + 1]), "f"(a.scale * acc[i + 2]), "f"(a.scale * acc[i + 3])
+                                 : "memory");
+            }
+            return;
+        }
         load_vec<V>(p, out);
 #pragma unroll
         for (int i = 0; i < V; ++i) out[i] = fmaf(a.scale, acc[i], out[i]);
@@ -270,153 +332,172 @@ __device__ __forceinline__ void write_row(const SumArgs &a, int key, int c, floa
     store_vec<V>(p, out);
 }
 
-// A run of equal tokens that crosses at most one window boundary is short: the window in which it
-// begins sums it to its end and writes its row.  One that crosses two or more is long: every window
-// that it touches leaves the sum of its part, and k_join adds those up in order.  So no window
-// sums more than two windows' entries, however the tokens are distributed, and both sides of a
-// boundary decide from a few keys, without knowing where the run begins or ends:
-//   at the front of window [a, b):  long  <=>  it fills the window too (key[b] is the same), or key[a-kWindow-1] is the same
-//   at its back:                    long  <=>  key[a-1] is the same, or key[b+kWindow] is the same
+// Adds V elements of dout as they lie in 16 bytes.
+template <typename DT, int V> __device__ __forceinline__ void add_to(float (&acc)[V], const uint4 &w)
+{
+    const unsigned q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (V == 8) {
+            acc[2 * i] += bf_lo(q[i]);
+            acc[2 * i + 1] += bf_hi(q[i]);
+        } else {
+            acc[i] += __uint_as_float(q[i]);
+        }
+    }
+}
+
+__device__ __forceinline__ void copy_async(void *dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 __device__ __forceinline__ bool same_key(const Pair *s, long long n, long long i, int key)
 {
     return i >= 0 && i < n && s[i].key == key;
 }
 
-// One thread per window and vector of 16 bytes of dout.
+// The sorted list is cut into windows of equal length; one thread walks over a window for one
+// vector (16 bytes of dout; one element where rows are not aligned) and adds rows until the token
+// changes.  A run that crosses into the next window by at most kSpill entries is finished by the window
+// it comes from; where it goes further, each window leaves the sum of its part as a piece, and
+// k_join adds the pieces in order.  So no window has more than kSpill entries more than another, however
+// the tokens are distributed, and both sides of a boundary decide from one key: that of entry
+// kSpill after it.  The pairs come through shared memory, the rows through a
+// ring of kDepth asynchronous 16-byte copies per thread that only this thread reads: no barrier,
+// no registers held, and a row's trip to memory is covered by the ones before it.  (With rows
+// requested four at a time into registers the walk took about 10 us per window of 16, latency after latency:
+// 22 us for 32768 x 1024 bf16, against 11 us for the bytes.)
 template <typename DT, typename GT, int V>
-__global__ void __launch_bounds__(kSumThreads) k_sum_windows(const __grid_constant__ SumArgs a)
+__global__ void __launch_bounds__(kSumThreads, kSumBlocks) k_sum_windows(const __grid_constant__ SumArgs a)
 {
+    __shared__ uint4 ring[V == 1 ? 1 : kDepth][V == 1 ? 1 : kSumThreads];
+    __shared__ int2 pairs[kMostPairs + kSpill + 2];
     griddep_wait();
-    const long long t = (long long)blockIdx.x * kSumThreads + threadIdx.x;
-    const long long w = t / a.nv;
-    const int c = (int)(t % a.nv);
-    const long long lo = w * kWindow, hi = lo + kWindow < a.n ? lo + kWindow : a.n;
-    if (lo >= a.n) return;
-    const Pair *s = a.sorted;
-    long long i = lo;
-    int key = s[lo].key;
-    bool head = same_key(s, a.n, lo - 1, key);  // the run at the front began earlier
-    const bool head_long = head && (same_key(s, a.n, hi, key) || same_key(s, a.n, lo - kWindow - 1, key));
-    if (key >= a.vocab) return;
-    if (head && !head_long) {  // another window's: on to the run after it
-        long long past = hi;
-        while (i < past) {
-            const long long mid = (i + past) / 2;
-            if (s[mid].key == key)
-                i = mid + 1;
-            else
-                past = mid;
-        }
-        if (i == hi) return;
-        key = s[i].key;
-        if (key >= a.vocab) return;
+    griddep_launch();
+    const long long t0 = (long long)blockIdx.x * kSumThreads, t1 = t0 + kSumThreads - 1;
+    const long long base = t0 / a.nv * a.window - 1;  // entry of pairs[0]
+    const int here = (int)(t1 / a.nv - t0 / a.nv + 1) * a.window + kSpill + 2;
+    for (int i = threadIdx.x; i < here; i += kSumThreads) {
+        const long long at = base + i;
+        pairs[i] = at >= 0 && at < a.n ? __ldcg(reinterpret_cast<const int2 *>(a.sorted) + at) : make_int2(-1, 0);
+    }
+    __syncthreads();
+    const long long t = t0 + threadIdx.x, w = t / a.nv;
+    const int c = (int)(t - w * a.nv);
+    if (w * a.window >= a.n) return;
+    int lo = (int)(w * a.window - base);  // places in pairs; entries beyond the list have key -1
+    int hi = lo + (int)(a.n - w * a.window < a.window ? a.n - w * a.window : a.window);
+    const int absent = (int)a.vocab;
+    bool head = pairs[lo - 1].x == pairs[lo].x;  // the run at the front began earlier
+    if (head && pairs[lo + kSpill].x != pairs[lo].x) {  // and is finished there
+        const int old = pairs[lo].x;
+        while (lo < hi && pairs[lo].x == old) ++lo;
         head = false;
     }
-    const int back = s[hi - 1].key;
-    const bool crosses = same_key(s, a.n, hi, back);
-    const bool back_long = crosses && (same_key(s, a.n, lo - 1, back) || same_key(s, a.n, hi + kWindow, back));
-    const long long end = crosses && !back_long ? (hi + kWindow < a.n ? hi + kWindow : a.n) : hi;
+    if (lo == hi) return;
+    int key = pairs[lo].x;
+    if (key == absent) return;  // entries without a part come last in the list
+    const int back = pairs[hi - 1].x;
+    const bool tail = back != absent && pairs[hi].x == back && pairs[hi + kSpill].x == back;
+    if (!tail)
+        while (pairs[hi].x == back) ++hi;
+    while (pairs[hi - 1].x == absent) --hi;
 
     float acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
     const DT *dout = static_cast<const DT *>(a.dout) + (long long)c * V;
-    bool done = false;
-    constexpr int U = 4;  // rows requested together
-    for (; i < end && !done; i += U) {
-        int2 p[U];
-        float x[U][V];
+    auto row = [&](int i) { return dout + (long long)pairs[i].y * a.ld_dout; };
+    auto next_run = [&](int i) {  // before entry i is added
+        const int k = pairs[i].x;
+        if (k == key) return;
+        if (head)
+            store_vec<V>(a.pieces + 2 * w * a.ld_piece + (long long)c * V, acc);
+        else
+            write_row<GT, V>(a, key, c, acc);
+        head = false;
+        key = k;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            p[u] = i + u < end ? reinterpret_cast<const int2 *>(s)[i + u] : make_int2(-1, 0);
-            if (i + u >= hi && p[u].x != back) p[u].x = -1;  // past the window only its last run may go on
-        }
+        for (int e = 0; e < V; ++e) acc[e] = 0.f;
+    };
+    if constexpr (V == 1) {
+        constexpr int U = 4;
+        for (int i = lo; i < hi; i += U) {
+            float x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (p[u].x >= 0 && p[u].x < a.vocab) load_vec<V>(dout + (long long)p[u].y * a.ld_dout, x[u]);
-        }
+            for (int u = 0; u < U; ++u) x[u] = to_f32(*row(i + u < hi ? i + u : hi - 1));
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (done || i + u >= end) continue;
-            if (p[u].x != key) {  // the run ends here
-                if (key < a.vocab) {
-                    if (head)
-                        store_vec<V>(a.pieces + 2 * w * a.ld_piece + (long long)c * V, acc);
-                    else
-                        write_row<GT, V>(a, key, c, acc);
-                }
-                head = false;
-                key = p[u].x;
-                done = key < 0 || key >= a.vocab;
-#pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] = 0.f;
+            for (int u = 0; u < U; ++u) {
+                if (i + u >= hi) break;
+                next_run(i + u);
+                acc[0] += x[u];
             }
-            if (!done) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += x[u][e];
-            }
+        }
+    } else {
+        uint4 *mine = &ring[0][threadIdx.x];
+        for (int u = 0; u < kDepth; ++u) {
+            if (lo + u < hi) copy_async(mine + u * kSumThreads, row(lo + u));
+            copy_commit();
+        }
+        for (int i = lo, slot = 0; i < hi; ++i, slot = slot + 1 == kDepth ? 0 : slot + 1) {
+            copy_wait<kDepth - 1>();
+            const uint4 x = mine[slot * kSumThreads];
+            next_run(i);
+            add_to<DT, V>(acc, x);
+            if (i + kDepth < hi) copy_async(mine + slot * kSumThreads, row(i + kDepth));
+            copy_commit();
         }
     }
-    if (done) return;
-    if (head || back_long)
+    if (head || tail)
         store_vec<V>(a.pieces + (2 * w + (head ? 0 : 1)) * a.ld_piece + (long long)c * V, acc);
     else
         write_row<GT, V>(a, key, c, acc);
 }
 
-// The rows of long runs: block (w, slab) has the run that begins in window w, if one does.
+// The rows of runs that windows left in pieces: warp (w, slab) has the run that begins in window w,
+// if it was.  Nearly all warps find none and leave after one round trip.
 template <typename GT, int V>
 __global__ void __launch_bounds__(kSumThreads) k_join(const __grid_constant__ SumArgs a)
 {
     griddep_wait();
-    const long long slabs = (a.nv + 31) / 32;
-    const long long w = blockIdx.x / slabs;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    constexpr int kWarps = kSumThreads / 32;
-    const int c = (int)(blockIdx.x % slabs) * 32 + lane;
-    const long long lo = w * kWindow, hi = lo + kWindow;
+    const int slabs = (a.nv + 31) / 32;
+    const long long item = (long long)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5), w = item / slabs;
+    const int lane = threadIdx.x & 31, c = (int)(item % slabs) * 32 + lane;
+    const long long lo = w * a.window, hi = lo + a.window;
     const Pair *s = a.sorted;
     if (hi >= a.n) return;
-    const int key = s[hi - 1].key;
-    if (key >= a.vocab || same_key(s, a.n, lo - 1, key) || !same_key(s, a.n, hi, key) || !same_key(s, a.n, hi + kWindow, key)) return;
-    // windows that the run touches: w .. last
-    long long last = w + 2;
+    // windows w + 1 + lane that have a piece of the run, if it begins in w; every key is asked for at once
+    const int key = s[hi - 1].key, front = s[lo].key, before = lo ? s[lo - 1].key : -1;
+    const long long ask = hi + (long long)lane * a.window + kSpill;
+    const int there = ask < a.n ? s[ask].key : -1;
+    unsigned reached = __ballot_sync(0xffffffffu, there == key);
+    if (key >= a.vocab || !(reached & 1u) || (front == key && before == key)) return;
+    long long last = w;
     for (;;) {  // 32 windows at a time
-        const long long v = last + 1 + lane;
-        const unsigned goes_on = __ballot_sync(0xffffffffu, same_key(s, a.n, v * kWindow, key));
-        const int more = goes_on == 0xffffffffu ? 32 : __ffs(~goes_on) - 1;
+        const int more = reached == 0xffffffffu ? 32 : __ffs(~reached) - 1;
         last += more;
         if (more < 32) break;
+        reached = __ballot_sync(0xffffffffu, same_key(s, a.n, (last + 1 + lane) * a.window + kSpill, key));
     }
-    __shared__ float part[kWarps][32][V];
+    if (c >= a.nv) return;
     float acc[V];
+    const float *piece = a.pieces + (long long)c * V;
+    load_vec<V>(piece + (2 * w + 1) * a.ld_piece, acc);
+    constexpr int U = 16;
+    for (long long v = w + 1; v <= last; v += U) {
+        float x[U][V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    if (c < a.nv) {
-        // warp q adds windows w + q, w + q + 4, ... ; then the four sums are added in order
-        for (long long v = w + warp; v <= last; v += 4 * kWarps) {
-            float x[4][V];
+        for (int u = 0; u < U; ++u)
+            if (v + u <= last) load_vec<V>(piece + 2 * (v + u) * a.ld_piece, x[u]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const long long at = v + u * kWarps;
-                if (at <= last) load_vec<V>(a.pieces + (2 * at + (at == w ? 1 : 0)) * a.ld_piece + (long long)c * V, x[u]);
-            }
+        for (int u = 0; u < U; ++u) {
+            if (v + u > last) break;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (v + u * kWarps > last) break;
-#pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += x[u][e];
-            }
+            for (int e = 0; e < V; ++e) acc[e] += x[u][e];
         }
-    }
-#pragma unroll
-    for (int e = 0; e < V; ++e) part[warp][lane][e] = acc[e];
-    __syncthreads();
-    if (warp || c >= a.nv) return;
-#pragma unroll
-    for (int q = 1; q < kWarps; ++q) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] += part[q][lane][e];
     }
     write_row<GT, V>(a, key, c, acc);
 }
@@ -433,22 +514,34 @@ cudaError_t launch_lookup(const adascale_embed_args &g, LookupArgs a, bool vec, 
                : launch(k_lookup<TT, OT, 1>, blocks, kLookupThreads, 0, s, a);
 }
 
+// Entries of a window: one wave of blocks, but no more than a block's pairs have room for.
+int window_of(long long n, int nv, int sms)
+{
+    const long long threads = (long long)sms * kSumBlocks * kSumThreads;
+    long long w = ceil_div(n * nv, threads);
+    const long long most = kMostPairs / (kSumThreads / nv + 2);  // windows of a block, at most
+    if (w > most) w = most;
+    return (int)(w < kLeastWindow ? kLeastWindow : w);
+}
+
 template <typename DT, typename GT, int V>
-cudaError_t launch_sums(SumArgs a, long long dim, cudaStream_t s)
+cudaError_t launch_sums(SumArgs a, long long dim, int sms, cudaStream_t s)
 {
     a.nv = (int)(dim / V);
-    const long long windows = ceil_div(a.n, kWindow);
+    a.window = window_of(a.n, a.nv, sms);
+    const long long windows = ceil_div(a.n, a.window);
     cudaError_t e = launch(k_sum_windows<DT, GT, V>, ceil_div(windows * a.nv, kSumThreads), kSumThreads, 0, s, a);
-    // a long run touches three windows at least
-    if (e == cudaSuccess && windows > 2) e = launch(k_join<GT, V>, (windows - 2) * ceil_div(a.nv, 32), kSumThreads, 0, s, a);
-    return e;
+    if (e != cudaSuccess || windows == 1) return e;
+    constexpr int JV = V == 1 ? 1 : 4;
+    a.nv = (int)(dim / JV);
+    return launch(k_join<GT, JV>, ceil_div((windows - 1) * ceil_div(a.nv, 32), kSumThreads / 32), kSumThreads, 0, s, a);
 }
 
 template <typename DT, typename GT>
-cudaError_t launch_sums(const SumArgs &a, long long dim, bool vec, cudaStream_t s)
+cudaError_t launch_sums(const SumArgs &a, long long dim, bool vec, int sms, cudaStream_t s)
 {
     constexpr int V = 16 / sizeof(DT);
-    return vec ? launch_sums<DT, GT, V>(a, dim, s) : launch_sums<DT, GT, 1>(a, dim, s);
+    return vec ? launch_sums<DT, GT, V>(a, dim, sms, s) : launch_sums<DT, GT, 1>(a, dim, sms, s);
 }
 
 long long piece_stride(long long dim) { return ceil_div(dim, 8) * 8; }
@@ -484,7 +577,7 @@ int64_t adascale_embed_grad_workspace(int64_t n_tokens, int64_t dim)
 {
     if (n_tokens < 0 || n_tokens > kMaxRows || dim < 1 || dim > kMaxRows) return 0;
     const long long pairs = ceil_div(n_tokens, 2) * 2;
-    return 2 * pairs * (long long)sizeof(Pair) + ceil_div(n_tokens, kWindow) * 2 * piece_stride(dim) * (long long)sizeof(float);
+    return 2 * pairs * (long long)sizeof(Pair) + ceil_div(n_tokens, kLeastWindow) * 2 * piece_stride(dim) * (long long)sizeof(float);
 }
 
 adascale_status adascale_embed_grad(const adascale_embed_grad_args *g, void *cuda_stream)
@@ -521,13 +614,8 @@ adascale_status adascale_embed_grad(const adascale_embed_grad_args *g, void *cud
     while ((g->vocab >> (kSortBits * a.passes)) > 0) ++a.passes;  // the largest key is vocab itself
     a.grad_bytes = eg;
     a.vec = rows_on(g->grad, g->ld_grad, g->vocab, eg, 16) && a.row_bytes % 16 == 0;
-    if (!g->accumulate) {  // one block per SM, in whole clusters; fewer for a small vocabulary
-        long long blocks = sms / kSortCluster * kSortCluster - kSortCluster;
-        const long long runs = ceil_div(g->vocab, kZeroRun);
-        if (blocks > runs) blocks = ceil_div(runs, kSortCluster) * kSortCluster;
-        a.zero_blocks = (int)(blocks < kSortCluster ? kSortCluster : blocks);
-    }
-    OPS_CU(launch(k_sort_tokens, kSortCluster + a.zero_blocks, kSortThreads, 0, s, a, kSortCluster));
+    const int cluster = g->n_tokens <= kSortAlone ? 1 : kSortCluster;
+    OPS_CU(launch(k_sort_tokens, cluster + (g->accumulate ? 0 : kZeroBlocks), kSortThreads, 0, s, a, cluster));
     if (g->n_tokens == 0) return ADASCALE_OK;
 
     SumArgs b = {};
@@ -545,9 +633,9 @@ adascale_status adascale_embed_grad(const adascale_embed_grad_args *g, void *cud
     const bool vec = g->dim % 8 == 0 && rows_on(g->dout, g->ld_dout, g->n_tokens, ed, 16) &&
                      rows_on(g->grad, g->ld_grad, g->vocab, eg, 16);
     if (g->dout_dtype == ADASCALE_F32)
-        OPS_CU(g->grad_dtype == ADASCALE_F32 ? launch_sums<float, float>(b, g->dim, vec, s) : launch_sums<float, bf16>(b, g->dim, vec, s));
+        OPS_CU(g->grad_dtype == ADASCALE_F32 ? launch_sums<float, float>(b, g->dim, vec, sms, s) : launch_sums<float, bf16>(b, g->dim, vec, sms, s));
     else
-        OPS_CU(g->grad_dtype == ADASCALE_F32 ? launch_sums<bf16, float>(b, g->dim, vec, s) : launch_sums<bf16, bf16>(b, g->dim, vec, s));
+        OPS_CU(g->grad_dtype == ADASCALE_F32 ? launch_sums<bf16, float>(b, g->dim, vec, sms, s) : launch_sums<bf16, bf16>(b, g->dim, vec, sms, s));
     return ADASCALE_OK;
 }
 
