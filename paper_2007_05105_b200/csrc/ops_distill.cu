@@ -49,36 +49,8 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// Two 32-bit floats in a register pair: sm_100 adds, multiplies and multiply-adds both with one
-// instruction.  The walks over a row are bound by instruction issue before anything else (26.8
-// instructions per entry without this and 62 % of the issue slots taken, at half the memory's rate).
-typedef unsigned long long f2;
-
-__device__ __forceinline__ f2 pack2(float lo, float hi)
-{
-    f2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack2(f2 v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ f2 add2(f2 a, f2 b)
-{
-    f2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f2 mul2(f2 a, f2 b)
-{
-    f2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
-{
-    f2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
+// The walks over a row work on packed pairs: they are bound by instruction issue before anything else
+// (26.8 instructions per entry without pairs, 62 % of the issue slots taken at half the memory's rate).
 __device__ __forceinline__ f2 ex2_2(f2 v)
 {
     float a, b;

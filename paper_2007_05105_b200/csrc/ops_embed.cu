@@ -347,13 +347,6 @@ template <typename DT, int V> __device__ __forceinline__ void add_to(float (&acc
     }
 }
 
-__device__ __forceinline__ void copy_async(void *dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ bool same_key(const Pair *s, long long n, long long i, int key)
 {
     return i >= 0 && i < n && s[i].key == key;

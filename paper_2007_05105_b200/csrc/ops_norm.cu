@@ -4,373 +4,583 @@
 // With n = (v - mean) r, r = 1 / sqrt(var + eps) (RMS: mean = 0) and dn = dout * w, the gradient of a norm is
 //   dv = r [ dn - n mean(dn n) - mean(dn) ]          (RMS: without the last term)
 // so both directions of a row need its elements and a handful of sums over them.
+//
+// Both kernels are bound by memory: every array is read or written once, and a row's elements
+// stay in registers between the sums.  A row belongs to a group of threads with up to 32 (gradient: 16)
+// elements each; persistent groups walk over the rows, and the next row of every array
+// arrives in shared memory by one bulk copy each while the group works on the current one.  What had
+// to be brought down is the number of instructions: with 8 elements a thread, plain loads and the
+// kinds of matrix and row told apart at run time, a row of 1024 cost 2400 warp instructions forward and 3500 backward
+// (the SM issues at most 2100 and 3100 in the time that the row's bytes take).  Hence work on packed pairs, many
+// elements a thread, kernels compiled for the types and for rows that fill the group.
 #include "ops_common.cuh"
 
 namespace {
 
-constexpr int kMinThreads = 128;   // of a block
-constexpr int kMaxThreads = 1024;
-constexpr int kElems = 8;          // of a row per thread and vector set
-constexpr int kSets = 5;           // column sums of the gradient: dw_pre, db_pre, dw_post, db_post, dgate
+constexpr int kForwardElems = 32;   // of a row per thread
+constexpr int kGradElems = 16;      // fewer: up to five column sums of each stay in registers
+constexpr int kSums = 5;            // dw_pre, db_pre, dw_post, db_post, dgate
 enum { kDwPre, kDbPre, kDwPost, kDbPost, kDgate };
+constexpr int kStages = 2;
+constexpr int kStageMost = 4096;    // widest row that is staged
 
-// A row belongs to a group of `group` threads (a power of two, 32 .. 1024); thread t has NV sets of eight
-// elements: with V = 8 vector i is (i * group + t), with V = 1 the elements i * group + t.
-template <int NV, int V> __device__ __forceinline__ int column(int j, int group, int t)
+struct Rows {
+    char *p;
+    long long pitch;  // bytes between rows
+    int is_bf16;
+    __device__ __forceinline__ char *row(long long r) const { return p + r * pitch; }
+};
+
+// Types of the stream and of the block's side that a kernel is compiled for; kAny: told apart at run time.
+enum { kF32 = 0, kBf16 = 1, kAny = 2 };
+template <int T> __device__ __forceinline__ bool is_bf16(const Rows &m)
 {
-    return (j * group + t) * V;
+    if constexpr (T == kAny) return m.is_bf16;
+    return T == kBf16;
 }
 
-// Sums of K values over each group of threads, for all groups of the block at once; one
-// barrier: consecutive calls use alternate halves of the scratch.
-template <int K> struct GroupSum {
-    float (*scratch)[kMaxThreads / 32][K];  // [2][warps][K]
-    int group, turn;
+// A thread's elements are E / V sets of V adjacent ones: set j starts at column (j * group + t) * V.  V = 4 where
+// rows start on 16-byte boundaries (16 or 8 bytes an access, adjacent over the lanes), 1 otherwise.  FULL: the
+// group has exactly the row's columns.  Elements are kept as pairs.
+template <int E, int V, bool FULL> struct Place {
+    int group, t, dim;
+    __device__ __forceinline__ int column(int j) const { return (j * group + t) * V; }
+    __device__ __forceinline__ bool has(int j) const { return FULL || column(j) < dim; }
+};
 
-    __device__ __forceinline__ void operator()(float (&v)[K])
+// The thread's elements of the row at p; those that it does not have become `none`.
+template <int E, int V, bool FULL> __device__ __forceinline__ void read(const Place<E, V, FULL> &at, const char *p, bool bf, f2 (&x)[E / 2], float none = 0.f)
+{
+    if constexpr (V == 4) {
+#pragma unroll
+        for (int j = 0; j < E / 4; ++j) {
+            if (!at.has(j)) {
+                x[2 * j] = x[2 * j + 1] = pack2(none, none);
+            } else if (bf) {
+                const uint2 q = *reinterpret_cast<const uint2 *>(p + (unsigned)at.column(j) * 2);
+                x[2 * j] = pack2(bf_lo(q.x), bf_hi(q.x));
+                x[2 * j + 1] = pack2(bf_lo(q.y), bf_hi(q.y));
+            } else {
+                const float4 q = *reinterpret_cast<const float4 *>(p + (unsigned)at.column(j) * 4);
+                x[2 * j] = pack2(q.x, q.y);
+                x[2 * j + 1] = pack2(q.z, q.w);
+            }
+        }
+    } else {
+        float v[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            v[j] = none;
+            if (at.has(j)) v[j] = bf ? to_f32(reinterpret_cast<const bf16 *>(p)[at.column(j)]) : reinterpret_cast<const float *>(p)[at.column(j)];
+        }
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) x[i] = pack2(v[2 * i], v[2 * i + 1]);
+    }
+}
+// The thread's columns of a float32 vector.
+template <int E, int V, bool FULL> __device__ __forceinline__ void read(const Place<E, V, FULL> &at, const float *p, f2 (&x)[E / 2])
+{
+    read<E, V, FULL>(at, reinterpret_cast<const char *>(p), false, x);
+}
+
+template <int E, int V, bool FULL> __device__ __forceinline__ void write(const Place<E, V, FULL> &at, char *p, bool bf, const f2 (&x)[E / 2])
+{
+    float v[E];
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) unpack2(x[i], v[2 * i], v[2 * i + 1]);
+#pragma unroll
+    for (int j = 0; j < E / V; ++j) {
+        if (!at.has(j)) continue;
+        if constexpr (V == 4) {
+            const float *s = v + 4 * j;
+            if (bf) *reinterpret_cast<uint2 *>(p + (size_t)at.column(j) * 2) = make_uint2(bf_pack(s[0], s[1]), bf_pack(s[2], s[3]));
+            else *reinterpret_cast<float4 *>(p + (size_t)at.column(j) * 4) = make_float4(s[0], s[1], s[2], s[3]);
+        } else {
+            if (bf) put(reinterpret_cast<bf16 *>(p) + at.column(j), v[j]);
+            else put(reinterpret_cast<float *>(p) + at.column(j), v[j]);
+        }
+    }
+}
+
+template <int E> __device__ __forceinline__ void fill(f2 (&x)[E / 2], float v)
+{
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) x[i] = pack2(v, v);
+}
+
+// Sums of two values over the lanes of a warp: the first exchange halves the work by sending each half of
+// the warp one of the two.  Lanes 0-15 end up with the first sum, lanes 16-31 with the second.
+__device__ __forceinline__ float warp_sum_pair(float a, float b, int lane)
+{
+    const bool upper = lane & 16;
+    float mine = upper ? b : a;
+    mine += __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    return mine;
+}
+
+// Sums over a row's group: a warp (any number of them in a block, each for itself), or the whole
+// block, with one barrier (consecutive calls use alternate halves of the scratch).
+template <int GROUP> struct GroupSum {
+    float (*scratch)[GROUP / 32][2];  // [2][warps][2]
+    int turn;
+
+    __device__ __forceinline__ void operator()(float &a, float &b)
     {
+        const int lane = threadIdx.x & 31;
+        const float mine = warp_sum_pair(a, b, lane);
+        if constexpr (GROUP == 32) {
+            a = __shfl_sync(0xffffffffu, mine, 0);
+            b = __shfl_sync(0xffffffffu, mine, 16);
+        } else {
+            if ((lane & 15) == 0) scratch[turn][threadIdx.x >> 5][lane >> 4] = mine;
+            __syncthreads();
+            constexpr int kPer = GROUP / 32;
+            const float2 v = *reinterpret_cast<const float2 *>(scratch[turn][lane & (kPer - 1)]);
+            a = v.x;
+            b = v.y;
 #pragma unroll
-        for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
-        if (group == 32) return;
-        const int warp = threadIdx.x >> 5, per = group >> 5, first = warp & ~(per - 1);
-        if ((threadIdx.x & 31) == 0) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) scratch[turn][warp][k] = v[k];
+            for (int o = kPer / 2; o > 0; o >>= 1) {
+                a += __shfl_xor_sync(0xffffffffu, a, o);
+                b += __shfl_xor_sync(0xffffffffu, b, o);
+            }
+            turn ^= 1;
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            float s = 0.f;
-            for (int w = 0; w < per; ++w) s += scratch[turn][first + w][k];
-            v[k] = s;
+    }
+    __device__ __forceinline__ void operator()(float &a)
+    {
+        if constexpr (GROUP == 32) {
+            a = warp_sum(a);
+        } else {
+            float none = 0.f;
+            (*this)(a, none);
         }
-        turn ^= 1;
     }
 };
 
+template <int E> __device__ __forceinline__ float total(const f2 (&v)[E / 2])
+{
+    f2 s = v[0];
+#pragma unroll
+    for (int i = 1; i < E / 2; ++i) s = add2(s, v[i]);
+    float a, b;
+    unpack2(s, a, b);
+    return a + b;
+}
+template <int E> __device__ __forceinline__ float products(const f2 (&v)[E / 2], const f2 (&w)[E / 2])
+{
+    f2 s = mul2(v[0], w[0]);
+#pragma unroll
+    for (int i = 1; i < E / 2; ++i) s = fma2(v[i], w[i], s);
+    float a, b;
+    unpack2(s, a, b);
+    return a + b;
+}
+// v - mean; elements that the thread does not have stay 0.
+template <int E, int V, bool FULL> __device__ __forceinline__ void centre(const Place<E, V, FULL> &at, f2 (&v)[E / 2], float mean)
+{
+    const f2 m = pack2(-mean, -mean);
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) v[i] = add2(v[i], m);
+    if constexpr (!FULL) {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            float a, b;
+            unpack2(v[i], a, b);
+            v[i] = pack2(at.has(2 * i / V) ? a : 0.f, at.has((2 * i + 1) / V) ? b : 0.f);
+        }
+    }
+}
+template <int E> __device__ __forceinline__ void scale(f2 (&v)[E / 2], float s)
+{
+    const f2 q = pack2(s, s);
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) v[i] = mul2(v[i], q);
+}
+template <int E> __device__ __forceinline__ void times(f2 (&v)[E / 2], const f2 (&w)[E / 2])
+{
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) v[i] = mul2(v[i], w[i]);
+}
+template <int E> __device__ __forceinline__ void plus(f2 (&v)[E / 2], const f2 (&w)[E / 2])
+{
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) v[i] = add2(v[i], w[i]);
+}
+template <int E> __device__ __forceinline__ void sigmoids(f2 (&v)[E / 2])
+{
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+        float a, b;
+        unpack2(v[i], a, b);
+        v[i] = pack2(1.f / (1.f + __expf(-a)), 1.f / (1.f + __expf(-b)));
+    }
+}
+
+// The rows of a group in shared memory, kStages at a time: the arrays of a row one after another.  One thread
+// of the group asks for them; a stage is asked for again after a barrier of the group behind its last read.
+// A copy that does not arrive within the wait's bound is given up: the group stops and poisons its results.
+struct Stages {
+    char *base;       // the group's
+    u64 *full;        // [kStages]
+    unsigned bytes;   // of a row, all arrays
+    template <int N> __device__ __forceinline__ void request(const Rows *const (&arrays)[N], long long row, int dim, int stage) const
+    {
+        mbar_expect_tx(full + stage, bytes);
+        char *to = base + stage * bytes;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            if (!arrays[k]->p) continue;
+            const unsigned part = (unsigned)dim * (arrays[k]->is_bf16 ? 2 : 4);
+            bulk_load(to, arrays[k]->row(row), part, full + stage);
+            to += part;
+        }
+    }
+};
+
+template <int GROUP> __device__ __forceinline__ void group_barrier()
+{
+    if constexpr (GROUP == 32) __syncwarp();
+    else __syncthreads();
+}
+
 struct NormArgs {
-    const void *x, *y, *gate;
-    void *x_new, *h;
-    const float *w_post, *b_post, *w_pre, *b_pre;
-    long long n, ld_x, ld_y, ld_x_new, ld_h, ld_gate;
-    int dim, group;
+    Rows x, y, x_new, h, gate;  // y.p null: the norm alone
+    const float *gate_channel, *w_post, *b_post, *w_pre, *b_pre;
+    long long n;
+    int dim;
     int post, pre, gate_kind;
+    unsigned stage_bytes;
     float inv_dim, res_scale, eps;
 };
 
-__device__ __forceinline__ float sigmoid(float a) { return 1.f / (1.f + __expf(-a)); }
+// Threads of a block: of its one group, or four warps that are groups of their own.
+__host__ __device__ constexpr int threads_of(int group) { return group == 32 ? 128 : group; }
+// Blocks that an SM holds: as many as leave a thread the registers that it needs.  Gradient, 16384 x 1024 (f32
+// stream, bf16 block, layer norms, channel gate): 384 threads an SM (168 registers) 61 us, 256 (180) 68, 512 (128) 81.
+constexpr int forward_blocks(int group) { return group <= 128 ? 512 / threads_of(group) : group <= 256 ? 2 : 1; }
+constexpr int gradient_blocks(int group) { return group <= 128 ? 384 / threads_of(group) : 1; }
 
-// R rows per group of threads at once: their loads are in flight together, a weight is read
-// once for R rows, and a barrier serves R sums.
-template <typename XT, typename YT, int V, int NV, int R>
-__global__ void __launch_bounds__(kMaxThreads) k_boundary(const __grid_constant__ NormArgs a)
+template <int XT, int YT, int V, bool FULL, int GROUP>
+__global__ void __launch_bounds__(threads_of(GROUP), forward_blocks(GROUP)) k_boundary(const __grid_constant__ NormArgs a)
 {
-    constexpr int J = NV * kElems / V;  // accesses per thread and row
-    __shared__ float scratch[2][kMaxThreads / 32][R];
+    constexpr int E = kForwardElems, kGroups = threads_of(GROUP) / GROUP;
+    constexpr bool kStaged = V == 4 && GROUP * E <= kStageMost;
+    extern __shared__ __align__(128) char room[];
+    __shared__ __align__(8) float scratch[2][GROUP / 32][2];
+    __shared__ u64 full[kGroups][kStages];
+    const int mine = threadIdx.x / GROUP;
+    const Place<E, V, FULL> at = {GROUP, (int)threadIdx.x % GROUP, a.dim};
+    const long long all = (long long)gridDim.x * kGroups;
+    const Stages stages = {room + mine * kStages * a.stage_bytes, full[mine], a.stage_bytes};
+    GroupSum<GROUP> sum = {scratch, 0};
+    long long row = (long long)blockIdx.x * kGroups + mine;
+    if (kStaged && at.t == 0) {
+        for (int s = 0; s < kStages; ++s) mbar_init(full[mine] + s, 1);
+        mbar_publish();
+    }
+    group_barrier<GROUP>();
     griddep_wait();
-    const int t = threadIdx.x & (a.group - 1), groups = blockDim.x / a.group;
-    const long long row0 = ((long long)blockIdx.x * groups + threadIdx.x / a.group) * R;
-    GroupSum<R> sum = {scratch, a.group, 0};
-    float x[R][J][V], y[R][J][V];
-
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = column<NV, V>(j, a.group, t);
-            const bool in = c < a.dim && row0 + r < a.n;
-#pragma unroll
-            for (int e = 0; e < V; ++e) x[r][j][e] = y[r][j][e] = 0.f;
-            if (in) load_vec<V>(static_cast<const XT *>(a.x) + (row0 + r) * a.ld_x + c, x[r][j]);
-            if (in && a.y) load_vec<V>(static_cast<const YT *>(a.y) + (row0 + r) * a.ld_y + c, y[r][j]);
-        }
-    }
-    float s[R];
-    // mean and 1 / deviation of every row of v; v is centred
-    auto stats = [&](float (&v)[R][J][V], int kind) {
-        if (kind == ADASCALE_NORM_LAYER) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                s[r] = 0.f;
-#pragma unroll
-                for (int j = 0; j < J; ++j)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) s[r] += v[r][j][e];
+    griddep_launch();
+    const Rows *const arrays[3] = {&a.x, &a.y, &a.gate};
+    if (kStaged && at.t == 0)
+        for (int s = 0; s < kStages; ++s)
+            if (row + s * all < a.n) stages.request(arrays, row + s * all, a.dim, s);
+    int stage = 0;
+    unsigned parity = 0;
+    for (; row < a.n; row += all) {
+        const char *px = a.x.row(row), *py = a.y.row(row), *pg = a.gate.row(row);
+        if constexpr (kStaged) {
+            if (!mbar_wait(full[mine] + stage, parity)) {
+                f2 lost[E / 2];
+                fill<E>(lost, __int_as_float(0x7fffffff));
+                write<E, V, FULL>(at, a.h.row(row), is_bf16<YT>(a.h), lost);
+                mbar_wait(full[mine] + (stage ^ 1), parity ^ (stage == 1));  // the other copy in flight
+                break;
             }
+            px = stages.base + stage * stages.bytes;
+            py = px + a.dim * (is_bf16<XT>(a.x) ? 2 : 4);
+            pg = py + a.dim * (is_bf16<YT>(a.y) ? 2 : 4);
+        }
+        f2 x[E / 2], y[E / 2], w[E / 2];
+        float s;
+        read<E, V, FULL>(at, px, is_bf16<XT>(a.x), x);
+        if (a.y.p) {
+            read<E, V, FULL>(at, py, is_bf16<YT>(a.y), y);
+            if (a.post != ADASCALE_NORM_NONE) {
+                if (a.post == ADASCALE_NORM_LAYER) {
+                    s = total<E>(y);
+                    sum(s);
+                    centre<E, V, FULL>(at, y, s * a.inv_dim);
+                }
+                s = products<E>(y, y);
+                sum(s);
+                scale<E>(y, rsqrtf(fmaf(s, a.inv_dim, a.eps)));
+                read<E, V, FULL>(at, a.w_post, w);
+                times<E>(y, w);
+                if (a.b_post) {
+                    read<E, V, FULL>(at, a.b_post, w);
+                    plus<E>(y, w);
+                }
+            }
+            if (a.gate_kind != ADASCALE_GATE_NONE) {
+                if (a.gate_kind == ADASCALE_GATE_CHANNEL) {
+                    read<E, V, FULL>(at, a.gate_channel, w);
+                } else {
+                    read<E, V, FULL>(at, pg, is_bf16<YT>(a.gate), w);
+                    sigmoids<E>(w);
+                }
+                times<E>(y, w);
+            }
+            const f2 rs = pack2(a.res_scale, a.res_scale);
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) x[i] = fma2(rs, y[i], x[i]);
+            write<E, V, FULL>(at, a.x_new.row(row), is_bf16<XT>(a.x_new), x);
+        }
+        if constexpr (kStaged) {  // everything of the stage has been read
+            group_barrier<GROUP>();
+            if (at.t == 0 && row + kStages * all < a.n) stages.request(arrays, row + kStages * all, a.dim, stage);
+            stage ^= 1;
+            parity ^= stage == 0;
+        }
+        if (a.pre == ADASCALE_NORM_LAYER) {
+            s = total<E>(x);
             sum(s);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    const bool in = column<NV, V>(j, a.group, t) < a.dim;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) v[r][j][e] = in ? v[r][j][e] - s[r] * a.inv_dim : 0.f;
-                }
+            centre<E, V, FULL>(at, x, s * a.inv_dim);
         }
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            s[r] = 0.f;
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) s[r] = fmaf(v[r][j][e], v[r][j][e], s[r]);
-        }
+        s = products<E>(x, x);
         sum(s);
-#pragma unroll
-        for (int r = 0; r < R; ++r) s[r] = rsqrtf(fmaf(s[r], a.inv_dim, a.eps));
-    };
-
-    if (a.y) {
-        if (a.post != ADASCALE_NORM_NONE) stats(y, a.post);
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = column<NV, V>(j, a.group, t);
-            if (c >= a.dim) continue;
-            float w[V], b[V], g[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                w[e] = g[e] = 1.f;
-                b[e] = 0.f;
-            }
-            if (a.post != ADASCALE_NORM_NONE) load_vec<V>(a.w_post + c, w);
-            if (a.b_post) load_vec<V>(a.b_post + c, b);
-            if (a.gate_kind == ADASCALE_GATE_CHANNEL) load_vec<V>(static_cast<const float *>(a.gate) + c, g);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                if (row0 + r >= a.n) break;
-                if (a.gate_kind == ADASCALE_GATE_SIGMOID) {
-                    load_vec<V>(static_cast<const YT *>(a.gate) + (row0 + r) * a.ld_gate + c, g);
-#pragma unroll
-                    for (int e = 0; e < V; ++e) g[e] = sigmoid(g[e]);
-                }
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float u = a.post != ADASCALE_NORM_NONE ? fmaf(y[r][j][e] * s[r], w[e], b[e]) : y[r][j][e];
-                    x[r][j][e] = fmaf(a.res_scale * g[e], u, x[r][j][e]);
-                }
-                store_vec<V>(static_cast<XT *>(a.x_new) + (row0 + r) * a.ld_x_new + c, x[r][j]);
-            }
+        scale<E>(x, rsqrtf(fmaf(s, a.inv_dim, a.eps)));
+        read<E, V, FULL>(at, a.w_pre, w);
+        times<E>(x, w);
+        if (a.b_pre) {
+            read<E, V, FULL>(at, a.b_pre, w);
+            plus<E>(x, w);
         }
-    }
-    stats(x, a.pre);
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-        const int c = column<NV, V>(j, a.group, t);
-        if (c >= a.dim) continue;
-        float w[V], b[V];
-        load_vec<V>(a.w_pre + c, w);
-#pragma unroll
-        for (int e = 0; e < V; ++e) b[e] = 0.f;
-        if (a.b_pre) load_vec<V>(a.b_pre + c, b);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (row0 + r >= a.n) break;
-#pragma unroll
-            for (int e = 0; e < V; ++e) x[r][j][e] = fmaf(x[r][j][e] * s[r], w[e], b[e]);
-            store_vec<V>(static_cast<YT *>(a.h) + (row0 + r) * a.ld_h + c, x[r][j]);
-        }
+        write<E, V, FULL>(at, a.h.row(row), is_bf16<YT>(a.h), x);
     }
 }
 
 struct GradArgs {
-    const void *x, *y, *dx_new, *dh, *gate;
-    const float *w_post, *b_post, *w_pre;
-    void *dx, *dy, *dgate;
-    float *partial;  // [groups of the launch][kSets][ld_partial]
-    long long n, ld_x, ld_y, ld_dx_new, ld_dh, ld_gate, ld_dx, ld_dy, ld_dgate;
-    int dim, group, ld_partial;
+    Rows x, y, dx_new, dh, gate, dx, dy, dgate;  // absent ones have a null pointer
+    const float *gate_channel, *w_post, *b_post, *w_pre;
+    float *partial;  // [blocks][kSums][ld_partial]
+    long long n;
+    int dim, ld_partial;
     int post, pre, gate_kind;
+    unsigned stage_bytes;
     float inv_dim, res_scale, eps;
 };
 
-// A group of threads walks over rows group, group + groups, ...; every thread keeps the column sums
-// of its columns in registers and leaves them at the end, one row of partial sums per group.
-template <typename XT, typename YT, int V, int NV, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_boundary_grad(const __grid_constant__ GradArgs a)
+// Every thread keeps the column sums of its columns in registers over all its rows; at the end the
+// warps of a block are added in order, where they are groups, and the block leaves one row of partial
+// sums.  The sums over a row come in pairs (x and y, twice; the two of each norm's gradient): four
+// barriers a row, none where a row is one warp's.
+template <int XT, int YT, int V, bool FULL, int GROUP>
+__global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_boundary_grad(const __grid_constant__ GradArgs a)
 {
-    constexpr int J = NV * kElems / V;
-    __shared__ float scratch1[2][kMaxThreads / 32][1], scratch2[2][kMaxThreads / 32][2];
+    constexpr int E = kGradElems, kGroups = threads_of(GROUP) / GROUP;
+    constexpr bool kStaged = V == 4 && GROUP * E <= kStageMost;
+    extern __shared__ __align__(128) char room[];
+    __shared__ __align__(8) float scratch[2][GROUP / 32][2];
+    __shared__ u64 full[kGroups][kStages];
+    const int mine = threadIdx.x / GROUP;
+    const Place<E, V, FULL> at = {GROUP, (int)threadIdx.x % GROUP, a.dim};
+    const long long all = (long long)gridDim.x * kGroups;
+    const Stages stages = {room + mine * kStages * a.stage_bytes, full[mine], a.stage_bytes};
+    GroupSum<GROUP> sum = {scratch, 0};
+    long long row = (long long)blockIdx.x * kGroups + mine;
+    if (kStaged && at.t == 0) {
+        for (int s = 0; s < kStages; ++s) mbar_init(full[mine] + s, 1);
+        mbar_publish();
+    }
+    group_barrier<GROUP>();
     griddep_wait();
     griddep_launch();
-    const int t = threadIdx.x & (a.group - 1), groups = blockDim.x / a.group;
-    const long long me = (long long)blockIdx.x * groups + threadIdx.x / a.group, all = (long long)gridDim.x * groups;
-    GroupSum<1> sum1 = {scratch1, a.group, 0};
-    GroupSum<2> sum2 = {scratch2, a.group, 0};
-    float acc[kSets][J][V];
+    const Rows *const arrays[5] = {&a.x, &a.dh, &a.dx_new, &a.y, &a.gate};
+    if (kStaged && at.t == 0)
+        for (int s = 0; s < kStages; ++s)
+            if (row + s * all < a.n) stages.request(arrays, row + s * all, a.dim, s);
+    const bool has_y = a.y.p != nullptr, arrives = a.dx_new.p != nullptr, post = a.post != ADASCALE_NORM_NONE;
+    const bool centre_x = a.pre == ADASCALE_NORM_LAYER, centre_y = has_y && a.post == ADASCALE_NORM_LAYER;
+    f2 acc[kSums][E / 2];
 #pragma unroll
-    for (int k = 0; k < kSets; ++k)
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int e = 0; e < V; ++e) acc[k][j][e] = 0.f;
-
-    auto stats = [&](float (&v)[J][V], int kind) -> float {  // centres v, returns 1 / deviation
-        float s[1] = {0.f};
-        if (kind == ADASCALE_NORM_LAYER) {
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) s[0] += v[j][e];
-            sum1(s);
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const bool in = column<NV, V>(j, a.group, t) < a.dim;
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[j][e] = in ? v[j][e] - s[0] * a.inv_dim : 0.f;
+    for (int k = 0; k < kSums; ++k) fill<E>(acc[k], 0.f);
+    int stage = 0;
+    unsigned parity = 0;
+    for (; row < a.n; row += all) {
+        const char *px = a.x.row(row), *ph = a.dh.row(row), *pd = a.dx_new.row(row), *py = a.y.row(row), *pg = a.gate.row(row);
+        if constexpr (kStaged) {
+            if (!mbar_wait(full[mine] + stage, parity)) {
+                fill<E>(acc[kDwPre], __int_as_float(0x7fffffff));
+                mbar_wait(full[mine] + (stage ^ 1), parity ^ (stage == 1));  // the other copy in flight
+                break;
             }
+            px = stages.base + stage * stages.bytes;
+            ph = px + a.dim * (is_bf16<XT>(a.x) ? 2 : 4);
+            pd = ph + a.dim * (is_bf16<YT>(a.dh) ? 2 : 4);
+            py = arrives ? pd + a.dim * (is_bf16<XT>(a.dx_new) ? 2 : 4) : pd;
+            pg = py + a.dim * (is_bf16<YT>(a.y) ? 2 : 4);
         }
-        s[0] = 0.f;
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int e = 0; e < V; ++e) s[0] = fmaf(v[j][e], v[j][e], s[0]);
-        sum1(s);
-        return rsqrtf(fmaf(s[0], a.inv_dim, a.eps));
-    };
+        f2 x[E / 2], y[E / 2], dx[E / 2], dh[E / 2], w[E / 2];
+        float s0, s1;
+        read<E, V, FULL>(at, px, is_bf16<XT>(a.x), x);
+        read<E, V, FULL>(at, ph, is_bf16<YT>(a.dh), dh);
+        if (has_y) read<E, V, FULL>(at, py, is_bf16<YT>(a.y), y);
+        else fill<E>(y, 0.f);
+        if (centre_x || centre_y) {
+            s0 = total<E>(x);
+            s1 = total<E>(y);
+            sum(s0, s1);
+            if (centre_x) centre<E, V, FULL>(at, x, s0 * a.inv_dim);
+            if (centre_y) centre<E, V, FULL>(at, y, s1 * a.inv_dim);
+        }
+        s0 = products<E>(x, x);
+        s1 = products<E>(y, y);
+        sum(s0, s1);
+        const float rx = rsqrtf(fmaf(s0, a.inv_dim, a.eps)), ry = post ? rsqrtf(fmaf(s1, a.inv_dim, a.eps)) : 1.f;
 
-    for (long long base = 0; base < a.n; base += all) {  // the same number of rounds for every group of a block
-        const long long row = base + me;
-        const bool live = row < a.n;
-        float x[J][V], y[J][V], dx[J][V], dh[J][V];
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = column<NV, V>(j, a.group, t);
-            const bool in = live && c < a.dim;
-#pragma unroll
-            for (int e = 0; e < V; ++e) x[j][e] = y[j][e] = dx[j][e] = dh[j][e] = 0.f;
-            if (in) {
-                load_vec<V>(static_cast<const XT *>(a.x) + row * a.ld_x + c, x[j]);
-                load_vec<V>(static_cast<const YT *>(a.dh) + row * a.ld_dh + c, dh[j]);
-                if (a.dx_new) load_vec<V>(static_cast<const XT *>(a.dx_new) + row * a.ld_dx_new + c, dx[j]);
-                if (a.y) load_vec<V>(static_cast<const YT *>(a.y) + row * a.ld_y + c, y[j]);
-            }
-        }
         // dx = dx' + pre^T(dh)
-        float r = stats(x, a.pre);
-        float s[2] = {0.f, 0.f};
+        scale<E>(x, rx);
+        read<E, V, FULL>(at, a.w_pre, w);
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = column<NV, V>(j, a.group, t);
-            if (c >= a.dim) continue;
-            float w[V];
-            load_vec<V>(a.w_pre + c, w);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                x[j][e] *= r;
-                acc[kDwPre][j][e] = fmaf(dh[j][e], x[j][e], acc[kDwPre][j][e]);
-                acc[kDbPre][j][e] += dh[j][e];
-                dh[j][e] *= w[e];
-                s[0] = fmaf(dh[j][e], x[j][e], s[0]);
-                s[1] += dh[j][e];
-            }
+        for (int i = 0; i < E / 2; ++i) {
+            acc[kDwPre][i] = fma2(dh[i], x[i], acc[kDwPre][i]);
+            acc[kDbPre][i] = add2(acc[kDbPre][i], dh[i]);
+            dh[i] = mul2(dh[i], w[i]);
         }
-        sum2(s);
-        if (a.pre != ADASCALE_NORM_LAYER) s[1] = 0.f;
+        s0 = products<E>(dh, x);
+        s1 = total<E>(dh);
+        sum(s0, s1);
+        if (arrives) read<E, V, FULL>(at, pd, is_bf16<XT>(a.dx_new), dx);
+        else fill<E>(dx, 0.f);
+        {
+            const float mean = centre_x ? s1 * a.inv_dim : 0.f;
+            const f2 minus = pack2(-mean, -mean), share = pack2(-s0 * a.inv_dim, -s0 * a.inv_dim), r = pack2(rx, rx);
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = column<NV, V>(j, a.group, t);
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                dx[j][e] = fmaf(r, fmaf(-x[j][e], s[0] * a.inv_dim, dh[j][e] - s[1] * a.inv_dim), dx[j][e]);
-            if (live && c < a.dim) store_vec<V>(static_cast<XT *>(a.dx) + row * a.ld_dx + c, dx[j]);
+            for (int i = 0; i < E / 2; ++i) dx[i] = fma2(r, fma2(x[i], share, add2(dh[i], minus)), dx[i]);
         }
-        if (!a.y) continue;
-        // gate and post
-        r = a.post != ADASCALE_NORM_NONE ? stats(y, a.post) : 1.f;
-        s[0] = s[1] = 0.f;
+        write<E, V, FULL>(at, a.dx.row(row), is_bf16<XT>(a.dx), dx);
+
+        if (has_y) {  // gate and post; x, dh are free
+            if (post) scale<E>(y, ry);
+            scale<E>(dx, a.res_scale);
+            if (a.gate_kind != ADASCALE_GATE_NONE) {
+                f2 (&u)[E / 2] = x;
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = column<NV, V>(j, a.group, t);
-            if (c >= a.dim || !live) continue;
-            float w[V], b[V], g[V], da[V];
+                for (int i = 0; i < E / 2; ++i) u[i] = y[i];
+                if (post) {
+                    read<E, V, FULL>(at, a.w_post, w);
+                    times<E>(u, w);
+                    if (a.b_post) {
+                        read<E, V, FULL>(at, a.b_post, w);
+                        plus<E>(u, w);
+                    }
+                }
+                times<E>(u, dx);  // gradient of the gate
+                if (a.gate_kind == ADASCALE_GATE_SIGMOID) {
+                    read<E, V, FULL>(at, pg, is_bf16<YT>(a.gate), w);
+                    sigmoids<E>(w);
+                    if (a.dgate.p) {
+                        const f2 one = pack2(1.f, 1.f), minus_one = pack2(-1.f, -1.f);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                w[e] = g[e] = 1.f;
-                b[e] = 0.f;
+                        for (int i = 0; i < E / 2; ++i) u[i] = mul2(mul2(u[i], w[i]), fma2(w[i], minus_one, one));
+                        write<E, V, FULL>(at, a.dgate.row(row), is_bf16<YT>(a.dgate), u);
+                    }
+                } else {
+                    read<E, V, FULL>(at, a.gate_channel, w);
+                    plus<E>(acc[kDgate], u);
+                }
+                times<E>(dx, w);
             }
-            if (a.post != ADASCALE_NORM_NONE) load_vec<V>(a.w_post + c, w);
-            if (a.b_post) load_vec<V>(a.b_post + c, b);
-            if (a.gate_kind == ADASCALE_GATE_CHANNEL) load_vec<V>(static_cast<const float *>(a.gate) + c, g);
-            if (a.gate_kind == ADASCALE_GATE_SIGMOID) {
-                load_vec<V>(static_cast<const YT *>(a.gate) + row * a.ld_gate + c, g);
+            if (post) {
+                read<E, V, FULL>(at, a.w_post, w);
 #pragma unroll
-                for (int e = 0; e < V; ++e) g[e] = sigmoid(g[e]);
-            }
+                for (int i = 0; i < E / 2; ++i) {
+                    acc[kDwPost][i] = fma2(dx[i], y[i], acc[kDwPost][i]);
+                    acc[kDbPost][i] = add2(acc[kDbPost][i], dx[i]);
+                    dx[i] = mul2(dx[i], w[i]);
+                }
+                s0 = products<E>(dx, y);
+                s1 = total<E>(dx);
+                sum(s0, s1);
+                const float mean = centre_y ? s1 * a.inv_dim : 0.f;
+                const f2 minus = pack2(-mean, -mean), share = pack2(-s0 * a.inv_dim, -s0 * a.inv_dim), r = pack2(ry, ry);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                y[j][e] *= r;
-                const float ds = a.res_scale * dx[j][e], dg = ds * fmaf(y[j][e], w[e], b[e]);
-                da[e] = dg * g[e] * (1.f - g[e]);
-                acc[kDgate][j][e] += dg;
-                const float du = ds * g[e];
-                acc[kDwPost][j][e] = fmaf(du, y[j][e], acc[kDwPost][j][e]);
-                acc[kDbPost][j][e] += du;
-                dx[j][e] = du * w[e];
-                s[0] = fmaf(dx[j][e], y[j][e], s[0]);
-                s[1] += dx[j][e];
+                for (int i = 0; i < E / 2; ++i) dx[i] = mul2(r, fma2(y[i], share, add2(dx[i], minus)));
             }
-            if (a.gate_kind == ADASCALE_GATE_SIGMOID && a.dgate)
-                store_vec<V>(static_cast<YT *>(a.dgate) + row * a.ld_dgate + c, da);
+            if (a.dy.p) write<E, V, FULL>(at, a.dy.row(row), is_bf16<YT>(a.dy), dx);
         }
-        if (a.post != ADASCALE_NORM_NONE) {
-            sum2(s);
-            if (a.post != ADASCALE_NORM_LAYER) s[1] = 0.f;
-        } else {
-            s[0] = s[1] = 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = column<NV, V>(j, a.group, t);
-            if (!live || c >= a.dim || !a.dy) continue;
-#pragma unroll
-            for (int e = 0; e < V; ++e) dx[j][e] = r * fmaf(-y[j][e], s[0] * a.inv_dim, dx[j][e] - s[1] * a.inv_dim);
-            store_vec<V>(static_cast<YT *>(a.dy) + row * a.ld_dy + c, dx[j]);
+        if constexpr (kStaged) {
+            group_barrier<GROUP>();
+            if (at.t == 0 && row + kStages * all < a.n) stages.request(arrays, row + kStages * all, a.dim, stage);
+            stage ^= 1;
+            parity ^= stage == 0;
         }
     }
-    if (me >= a.n) return;  // no row, and no partial sums are read
+
+    // one set of sums at a time: the block's group, or its warps in order
+    char *to = reinterpret_cast<char *>(a.partial + (long long)blockIdx.x * kSums * a.ld_partial);
+    float *gather = reinterpret_cast<float *>(room);  // [kGroups][ld_partial]
 #pragma unroll
-    for (int k = 0; k < kSets; ++k)
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = column<NV, V>(j, a.group, t);
-            if (c < a.dim) store_vec<V>(a.partial + (me * kSets + k) * a.ld_partial + c, acc[k][j]);
+    for (int k = 0; k < kSums; ++k) {
+        if constexpr (kGroups == 1) {
+            write<E, V, FULL>(at, to + (size_t)k * a.ld_partial * 4, false, acc[k]);
+        } else {
+            __syncthreads();
+            write<E, V, FULL>(at, reinterpret_cast<char *>(gather + mine * a.ld_partial), false, acc[k]);
+            __syncthreads();
+            for (int c = threadIdx.x; c < a.dim; c += threads_of(GROUP)) {
+                float s = gather[c];
+                for (int q = 1; q < kGroups; ++q) s += gather[q * a.ld_partial + c];
+                reinterpret_cast<float *>(to)[k * a.ld_partial + c] = s;
+            }
         }
+    }
 }
 
 struct ColumnArgs {
     const float *partial;
-    void *out[kSets];
+    void *out[kSums];
     int dim, ld_partial, n_partials, bf16_out;
 };
 
-// Column sums of the partial sums, in a fixed order: 32 columns per block, warp q adds rows q, q + 16, ...
-constexpr int kColumnWarps = 16;
+// Column sums of the blocks' partial sums, in a fixed order: 32 columns per block, warp q adds rows q, q + 32, ...
+constexpr int kColumnWarps = 32;
 __global__ void __launch_bounds__(kColumnWarps * 32) k_columns(const __grid_constant__ ColumnArgs a)
 {
-    __shared__ float part[kColumnWarps][32];
+    __shared__ float part[kColumnWarps][33];
     griddep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int chunks = (a.dim + 31) / 32, set = blockIdx.x / chunks, c = (blockIdx.x % chunks) * 32 + lane;
-    if (!a.out[set]) return;
+    const int chunks = (a.dim + 31) / 32, which = blockIdx.x / chunks, c0 = (blockIdx.x % chunks) * 32, c = c0 + lane;
+    if (!a.out[which]) return;
     float s = 0.f;
     if (c < a.dim) {
-#pragma unroll 4
-        for (int p = warp; p < a.n_partials; p += kColumnWarps) s += a.partial[((long long)p * kSets + set) * a.ld_partial + c];
+        constexpr int U = 10;
+        const float *p = a.partial + (long long)which * a.ld_partial + c;
+        const long long pitch = (long long)kSums * a.ld_partial;
+        for (int q = warp; q < a.n_partials; q += U * kColumnWarps) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = q + u * kColumnWarps < a.n_partials ? __ldcg(p + (q + u * kColumnWarps) * pitch) : 0.f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) s += x[u];
+        }
     }
     part[warp][lane] = s;
     __syncthreads();
-    if (warp || c >= a.dim) return;
-#pragma unroll
-    for (int q = 1; q < kColumnWarps; ++q) s += part[q][lane];
+    s = warp_sum(part[lane][warp]);  // column c0 + warp
+    if (lane || c0 + warp >= a.dim) return;
     if (a.bf16_out)
-        put(static_cast<bf16 *>(a.out[set]) + c, s);
+        put(static_cast<bf16 *>(a.out[which]) + c0 + warp, s);
     else
-        put(static_cast<float *>(a.out[set]) + c, s);
+        put(static_cast<float *>(a.out[which]) + c0 + warp, s);
 }
 
 // ---- host side -----------------------------------------------------------------------------
 
-constexpr int kMaxPartials = 148 * 16;  // groups of a gradient launch, at most
+constexpr int kMaxPartials = 148 * 16;  // blocks of a gradient launch, at most
 
 // Threads per row for `per` elements each.
 int group_of(long long dim, int per)
@@ -382,50 +592,85 @@ int group_of(long long dim, int per)
 
 bool norm_kind(int k, bool none_too) { return k == ADASCALE_NORM_RMS || k == ADASCALE_NORM_LAYER || (none_too && k == ADASCALE_NORM_NONE); }
 
-template <typename XT, typename YT, int V>
-cudaError_t launch_boundary(NormArgs a, int sms, cudaStream_t s)
+Rows rows(const void *p, long long ld, int dtype)
 {
-    const bool wide = a.dim > kMaxThreads * kElems;
-    a.group = group_of(a.dim, wide ? 2 * kElems : kElems);
-    const int threads = a.group < kMinThreads ? kMinThreads : a.group, groups = threads / a.group;
-    if (wide) return launch(k_boundary<XT, YT, V, 2, 1>, ceil_div(a.n, groups), threads, 0, s, a);
-    if (a.n >= 4LL * sms * (2048 / a.group)) return launch(k_boundary<XT, YT, V, 1, 2>, ceil_div(a.n, 2 * groups), threads, 0, s, a);
-    return launch(k_boundary<XT, YT, V, 1, 1>, ceil_div(a.n, groups), threads, 0, s, a);
+    return {static_cast<char *>(const_cast<void *>(p)), ld * elem_bytes(dtype), dtype == ADASCALE_BF16};
+}
+unsigned row_bytes(const Rows &m, int dim) { return !m.p ? 0 : (unsigned)dim * (m.is_bf16 ? 2 : 4); }
+
+// Blocks of a persistent launch: `most` an SM, fewer where their stages do not fit.
+long long resident(int sms, int most, size_t smem)
+{
+    const long long fit = (long long)(224 * 1024 / (smem + 2 * 1024));
+    return (long long)sms * (fit < most ? (fit < 1 ? 1 : fit) : most);
 }
 
-template <typename XT, typename YT> cudaError_t launch_boundary(const NormArgs &a, bool vec, int sms, cudaStream_t s)
+// Shared memory beyond the 48 KB that need no permission, what the kernel declares itself included.
+template <typename Args> cudaError_t launch_staged(void (*kernel)(Args), long long blocks, int threads, size_t smem, cudaStream_t s, const Args &a)
 {
-    return vec ? launch_boundary<XT, YT, 8>(a, sms, s) : launch_boundary<XT, YT, 1>(a, sms, s);
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    return launch(kernel, blocks, threads, smem, s, a);
 }
 
-// Blocks of a gradient launch.
-long long grad_blocks(long long n, int group, int sms)
+template <int XT, int YT, int V, bool FULL, int GROUP> cudaError_t launch_boundary(const NormArgs &a, int sms, cudaStream_t s)
 {
-    const int threads = group < kMinThreads ? kMinThreads : group, groups = threads / group;
-    long long blocks = (long long)sms * (512 / threads < 1 ? 1 : 512 / threads);
-    if (blocks * groups > kMaxPartials) blocks = kMaxPartials / groups;
-    const long long need = ceil_div(n, groups);
-    return blocks < need ? blocks : need;
+    constexpr int kGroups = threads_of(GROUP) / GROUP;
+    constexpr bool kStaged = V == 4 && GROUP * kForwardElems <= kStageMost;
+    const size_t smem = kStaged ? (size_t)kGroups * kStages * a.stage_bytes : 0;
+    const long long need = ceil_div(a.n, kGroups), most = resident(sms, forward_blocks(GROUP), smem);
+    return launch_staged(k_boundary<XT, YT, V, FULL, GROUP>, need < most ? need : most, threads_of(GROUP), smem, s, a);
+}
+template <int XT, int YT, int V, bool FULL> cudaError_t launch_boundary(const NormArgs &a, int group, int sms, cudaStream_t s)
+{
+    switch (group) {
+    case 32: return launch_boundary<XT, YT, V, FULL, 32>(a, sms, s);
+    case 64: return launch_boundary<XT, YT, V, FULL, 64>(a, sms, s);
+    case 128: return launch_boundary<XT, YT, V, FULL, 128>(a, sms, s);
+    case 256: return launch_boundary<kAny, kAny, V, FULL, 256>(a, sms, s);
+    }
+    return launch_boundary<kAny, kAny, V, FULL, 512>(a, sms, s);
+}
+template <int XT, int YT> cudaError_t launch_boundary(const NormArgs &a, bool vec, int sms, cudaStream_t s)
+{
+    const int group = group_of(a.dim, kForwardElems);
+    if (!vec) return launch_boundary<kAny, kAny, 1, false>(a, group, sms, s);
+    return group * kForwardElems == a.dim ? launch_boundary<XT, YT, 4, true>(a, group, sms, s) : launch_boundary<XT, YT, 4, false>(a, group, sms, s);
 }
 
-template <typename XT, typename YT, int V>
-cudaError_t launch_grad(GradArgs a, int sms, cudaStream_t s, long long &partials)
+template <int XT, int YT, int V, bool FULL, int GROUP> cudaError_t launch_grad(const GradArgs &a, int sms, cudaStream_t s, int &partials)
 {
-    const bool wide = a.dim > 512 * kElems;
-    a.group = group_of(a.dim, wide ? 2 * kElems : kElems);
-    const int threads = a.group < kMinThreads ? kMinThreads : a.group, groups = threads / a.group;
-    const long long blocks = grad_blocks(a.n, a.group, sms);
-    partials = blocks * groups < a.n ? blocks * groups : a.n;
-    if (threads <= 256) return launch(k_boundary_grad<XT, YT, V, 1, 256>, blocks, threads, 0, s, a);
-    if (threads <= 512) return wide ? launch(k_boundary_grad<XT, YT, V, 2, 512>, blocks, threads, 0, s, a)
-                                    : launch(k_boundary_grad<XT, YT, V, 1, 512>, blocks, threads, 0, s, a);
-    return launch(k_boundary_grad<XT, YT, V, 2, 1024>, blocks, threads, 0, s, a);
+    constexpr int kGroups = threads_of(GROUP) / GROUP;
+    constexpr bool kStaged = V == 4 && GROUP * kGradElems <= kStageMost;
+    const long long need = ceil_div(a.n, kGroups);
+    size_t smem = kStaged ? (size_t)kGroups * kStages * a.stage_bytes : 0;
+    const size_t gather = (size_t)kGroups * a.ld_partial * sizeof(float);
+    if (kGroups > 1 && smem < gather) smem = gather;
+    long long blocks = resident(sms, gradient_blocks(GROUP), smem);
+    if (blocks > kMaxPartials) blocks = kMaxPartials;
+    if (blocks > need) blocks = need;
+    partials = (int)blocks;
+    return launch_staged(k_boundary_grad<XT, YT, V, FULL, GROUP>, blocks, threads_of(GROUP), smem, s, a);
 }
-
-template <typename XT, typename YT>
-cudaError_t launch_grad(const GradArgs &a, bool vec, int sms, cudaStream_t s, long long &partials)
+template <int XT, int YT, int V, bool FULL> cudaError_t launch_grad(const GradArgs &a, int group, int sms, cudaStream_t s, int &partials)
 {
-    return vec ? launch_grad<XT, YT, 8>(a, sms, s, partials) : launch_grad<XT, YT, 1>(a, sms, s, partials);
+    switch (group) {
+    case 32: return launch_grad<XT, YT, V, FULL, 32>(a, sms, s, partials);
+    case 64: return launch_grad<XT, YT, V, FULL, 64>(a, sms, s, partials);
+    case 128: return launch_grad<XT, YT, V, FULL, 128>(a, sms, s, partials);
+    case 256: return launch_grad<XT, YT, V, FULL, 256>(a, sms, s, partials);
+    case 512: return launch_grad<kAny, kAny, V, FULL, 512>(a, sms, s, partials);
+    }
+    return launch_grad<kAny, kAny, V, FULL, 1024>(a, sms, s, partials);
+}
+template <int XT, int YT> cudaError_t launch_grad(const GradArgs &a, bool vec, int sms, cudaStream_t s, int &partials)
+{
+    const int group = group_of(a.dim, kGradElems);
+    if (!vec) return launch_grad<kAny, kAny, 1, false>(a, group, sms, s, partials);
+    return group * kGradElems == a.dim ? launch_grad<XT, YT, 4, true>(a, group, sms, s, partials)
+                                       : launch_grad<XT, YT, 4, false>(a, group, sms, s, partials);
 }
 
 }  // namespace
@@ -453,21 +698,17 @@ adascale_status adascale_residual_norm(const adascale_residual_norm_args *g, voi
     const int sms = sm_count();
     if (!sms) return ADASCALE_ERR_CUDA;
     NormArgs a = {};
-    a.x = g->x;
-    a.y = g->y;
-    a.x_new = g->x_new;
-    a.h = g->h;
-    a.gate = g->gate;
-    a.w_post = g->w_post;
+    a.x = rows(g->x, g->ld_x, g->x_dtype);
+    a.y = rows(g->y, g->ld_y, g->y_dtype);
+    a.x_new = rows(g->x_new, g->ld_x_new, g->x_dtype);
+    a.h = rows(g->h, g->ld_h, g->y_dtype);
+    a.gate = rows(matrix ? g->gate : nullptr, g->ld_gate, g->y_dtype);
+    a.gate_channel = gated && !matrix ? static_cast<const float *>(g->gate) : nullptr;
+    a.w_post = post ? g->w_post : nullptr;
     a.b_post = g->post == ADASCALE_NORM_LAYER ? g->b_post : nullptr;
     a.w_pre = g->w_pre;
     a.b_pre = g->pre == ADASCALE_NORM_LAYER ? g->b_pre : nullptr;
     a.n = g->n_rows;
-    a.ld_x = g->ld_x;
-    a.ld_y = g->ld_y;
-    a.ld_x_new = g->ld_x_new;
-    a.ld_h = g->ld_h;
-    a.ld_gate = g->ld_gate;
     a.dim = (int)g->dim;
     a.post = g->post;
     a.pre = g->pre;
@@ -476,23 +717,24 @@ adascale_status adascale_residual_norm(const adascale_residual_norm_args *g, voi
     a.res_scale = g->res_scale;
     a.eps = g->eps;
     const long long n = g->n_rows;
-    const bool vec = g->dim % 8 == 0 && rows_on(a.x, a.ld_x, n, ex, 16) && rows_on(a.h, a.ld_h, n, ey, 16) && on(a.w_pre, 16) &&
-                     on(a.b_pre, 16) && (!a.y || (rows_on(a.y, a.ld_y, n, ey, 16) && rows_on(a.x_new, a.ld_x_new, n, ex, 16) &&
-                     on(a.w_post, 16) && on(a.b_post, 16))) && (!gated || (matrix ? rows_on(a.gate, a.ld_gate, n, ey, 16) : on(a.gate, 16)));
+    const bool vec = g->dim % 8 == 0 && rows_on(g->x, g->ld_x, n, ex, 16) && rows_on(g->h, g->ld_h, n, ey, 16) && on(a.w_pre, 16) &&
+                     on(a.b_pre, 16) && (!g->y || (rows_on(g->y, g->ld_y, n, ey, 16) && rows_on(g->x_new, g->ld_x_new, n, ex, 16))) &&
+                     on(a.w_post, 16) && on(a.b_post, 16) && on(a.gate_channel, 16) && rows_on(a.gate.p, g->ld_gate, n, ey, 16);
     cudaStream_t s = (cudaStream_t)cuda_stream;
+    a.stage_bytes = row_bytes(a.x, a.dim) + row_bytes(a.y, a.dim) + row_bytes(a.gate, a.dim);
     if (g->x_dtype == ADASCALE_F32)
-        OPS_CU(g->y_dtype == ADASCALE_F32 ? launch_boundary<float, float>(a, vec, sms, s) : launch_boundary<float, bf16>(a, vec, sms, s));
+        OPS_CU(g->y_dtype == ADASCALE_F32 ? launch_boundary<kF32, kF32>(a, vec, sms, s) : launch_boundary<kF32, kBf16>(a, vec, sms, s));
     else
-        OPS_CU(g->y_dtype == ADASCALE_F32 ? launch_boundary<bf16, float>(a, vec, sms, s) : launch_boundary<bf16, bf16>(a, vec, sms, s));
+        OPS_CU(g->y_dtype == ADASCALE_F32 ? launch_boundary<kBf16, kF32>(a, vec, sms, s) : launch_boundary<kBf16, kBf16>(a, vec, sms, s));
     return ADASCALE_OK;
 }
 
-// One row of partial sums of each kind per group of threads.
+// One row of partial sums of each kind per block.
 int64_t adascale_residual_norm_grad_workspace(int64_t n_rows, int64_t dim)
 {
     if (n_rows < 0 || n_rows > kMaxRows || dim < 1 || dim > ADASCALE_NORM_MAX_DIM) return 0;
     const long long rows = n_rows < kMaxPartials ? n_rows : kMaxPartials;
-    return rows * kSets * ceil_div(dim, 8) * 8 * (long long)sizeof(float);
+    return rows * kSums * ceil_div(dim, 8) * 8 * (long long)sizeof(float);
 }
 
 adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_args *g, void *cuda_stream)
@@ -524,32 +766,25 @@ adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_ar
     const int sms = sm_count();
     if (!sms) return ADASCALE_ERR_CUDA;
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    long long partials = 0;
+    int partials = 0;
     const int ld_partial = (int)(ceil_div(g->dim, 8) * 8);
     if (g->n_rows > 0) {
         GradArgs a = {};
-        a.x = g->x_new;
-        a.y = g->y;
-        a.dx_new = g->dx_new;
-        a.dh = g->dh;
-        a.gate = g->gate;
-        a.w_post = g->w_post;
+        a.x = rows(g->x_new, g->ld_x_new, g->x_dtype);
+        a.y = rows(g->y, g->ld_y, g->y_dtype);
+        a.dx_new = rows(g->dx_new, g->ld_dx_new, g->x_dtype);
+        a.dh = rows(g->dh, g->ld_dh, g->y_dtype);
+        a.gate = rows(matrix ? g->gate : nullptr, g->ld_gate, g->y_dtype);
+        a.dx = rows(g->dx, g->ld_dx, g->x_dtype);
+        a.dy = rows(g->dy, g->ld_dy, g->y_dtype);
+        a.dgate = rows(matrix ? g->dgate : nullptr, g->ld_dgate, g->y_dtype);
+        a.gate_channel = gated && !matrix ? static_cast<const float *>(g->gate) : nullptr;
+        a.w_post = post ? g->w_post : nullptr;
         a.b_post = g->post == ADASCALE_NORM_LAYER ? g->b_post : nullptr;
         a.w_pre = g->w_pre;
-        a.dx = g->dx;
-        a.dy = g->dy;
-        a.dgate = g->dgate;
         a.partial = static_cast<float *>(g->workspace);
         a.n = g->n_rows;
-        a.ld_x = g->ld_x_new;
-        a.ld_y = g->ld_y;
-        a.ld_dx_new = g->ld_dx_new;
-        a.ld_dh = g->ld_dh;
-        a.ld_gate = g->ld_gate;
-        a.ld_dx = g->ld_dx;
-        a.ld_dy = g->ld_dy;
-        a.ld_dgate = g->ld_dgate;
-        a.dim = (int)g->dim;
+            a.dim = (int)g->dim;
         a.ld_partial = ld_partial;
         a.post = g->post;
         a.pre = g->pre;
@@ -558,16 +793,16 @@ adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_ar
         a.res_scale = g->res_scale;
         a.eps = g->eps;
         const long long n = g->n_rows;
-        const bool vec = g->dim % 8 == 0 && rows_on(a.x, a.ld_x, n, ex, 16) && rows_on(a.dh, a.ld_dh, n, ey, 16) &&
-                         rows_on(a.dx, a.ld_dx, n, ex, 16) && rows_on(a.dx_new, a.ld_dx_new, n, ex, 16) && on(a.w_pre, 16) &&
-                         (!a.y || (rows_on(a.y, a.ld_y, n, ey, 16) && rows_on(a.dy, a.ld_dy, n, ey, 16) && on(a.w_post, 16) && on(a.b_post, 16))) &&
-                         (!gated || (matrix ? rows_on(a.gate, a.ld_gate, n, ey, 16) && rows_on(a.dgate, a.ld_dgate, n, ey, 16) : on(a.gate, 16)));
+        const bool vec = g->dim % 8 == 0 && rows_on(g->x_new, g->ld_x_new, n, ex, 16) && rows_on(g->dh, g->ld_dh, n, ey, 16) &&
+                         rows_on(g->dx, g->ld_dx, n, ex, 16) && rows_on(g->dx_new, g->ld_dx_new, n, ex, 16) && on(a.w_pre, 16) &&
+                         (!g->y || (rows_on(g->y, g->ld_y, n, ey, 16) && rows_on(g->dy, g->ld_dy, n, ey, 16))) && on(a.w_post, 16) &&
+                         on(a.b_post, 16) && on(a.gate_channel, 16) && rows_on(a.gate.p, g->ld_gate, n, ey, 16) &&
+                         rows_on(a.dgate.p, g->ld_dgate, n, ey, 16);
+        a.stage_bytes = row_bytes(a.x, a.dim) + row_bytes(a.dh, a.dim) + row_bytes(a.dx_new, a.dim) + row_bytes(a.y, a.dim) + row_bytes(a.gate, a.dim);
         if (g->x_dtype == ADASCALE_F32)
-            OPS_CU(g->y_dtype == ADASCALE_F32 ? launch_grad<float, float>(a, vec, sms, s, partials)
-                                              : launch_grad<float, bf16>(a, vec, sms, s, partials));
+            OPS_CU(g->y_dtype == ADASCALE_F32 ? launch_grad<kF32, kF32>(a, vec, sms, s, partials) : launch_grad<kF32, kBf16>(a, vec, sms, s, partials));
         else
-            OPS_CU(g->y_dtype == ADASCALE_F32 ? launch_grad<bf16, float>(a, vec, sms, s, partials)
-                                              : launch_grad<bf16, bf16>(a, vec, sms, s, partials));
+            OPS_CU(g->y_dtype == ADASCALE_F32 ? launch_grad<kBf16, kF32>(a, vec, sms, s, partials) : launch_grad<kBf16, kBf16>(a, vec, sms, s, partials));
     }
     ColumnArgs b = {};
     b.partial = static_cast<const float *>(g->workspace);
@@ -578,10 +813,10 @@ adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_ar
     b.out[kDgate] = gated && !matrix ? g->dgate : nullptr;
     b.dim = (int)g->dim;
     b.ld_partial = ld_partial;
-    b.n_partials = (int)partials;
+    b.n_partials = partials;
     b.bf16_out = g->wgrad_dtype == ADASCALE_BF16;
     if (b.out[0] || b.out[1] || b.out[2] || b.out[3] || b.out[4])
-        OPS_CU(launch(k_columns, kSets * ceil_div(g->dim, 32), kColumnWarps * 32, 0, s, b));
+        OPS_CU(launch(k_columns, kSums * ceil_div(g->dim, 32), kColumnWarps * 32, 0, s, b));
     return ADASCALE_OK;
 }
 
