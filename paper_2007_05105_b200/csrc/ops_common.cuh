@@ -185,18 +185,27 @@ __device__ __forceinline__ void mbar_expect_tx(u64 *bar, unsigned bytes)
 }
 // Makes initialised barriers known to the copy engine.
 __device__ __forceinline__ void mbar_publish() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
-// False if the phase did not complete within kWaitNs.
-__device__ __forceinline__ bool mbar_wait(u64 *bar, unsigned parity)
+// One poll.  CLUSTER: what other blocks of the cluster wrote before they arrived is seen.
+template <bool CLUSTER> __device__ __forceinline__ bool mbar_poll(unsigned addr, unsigned parity)
 {
-    const unsigned addr = smem_u32(bar);
-    u64 t0 = 0;
-    for (unsigned spin = 0; spin < 1u << 22; ++spin) {
-        unsigned done;
+    unsigned done;
+    if constexpr (CLUSTER)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done)
+                     : "r"(addr), "r"(parity), "r"(kWaitHintNs)
+                     : "memory");
+    else
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done)
                      : "r"(addr), "r"(parity), "r"(kWaitHintNs)
                      : "memory");
-        if (done) return true;
+    return done;
+}
+template <bool CLUSTER> __device__ __noinline__ bool mbar_wait_long(unsigned addr, unsigned parity)
+{
+    u64 t0 = 0;
+    for (unsigned spin = 0; spin < 1u << 22; ++spin) {
+        if (mbar_poll<CLUSTER>(addr, parity)) return true;
         if ((spin & 63u) == 63u) {
             u64 now;
             asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
@@ -206,6 +215,23 @@ __device__ __forceinline__ bool mbar_wait(u64 *bar, unsigned parity)
     }
     return false;
 }
+// False if the phase did not complete within kWaitNs.
+template <bool CLUSTER = false> __device__ __forceinline__ bool mbar_wait(u64 *bar, unsigned parity)
+{
+    const unsigned addr = smem_u32(bar);
+    return mbar_poll<CLUSTER>(addr, parity) || mbar_wait_long<CLUSTER>(addr, parity);
+}
+// Orders this thread's writes to shared memory before copies out of it that start after a barrier.
+__device__ __forceinline__ void copy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// shared -> global, by the thread's bulk groups
+__device__ __forceinline__ void bulk_store(void *dst, const void *src, unsigned bytes)
+{
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// until at most N groups have not read their shared memory yet; until all writes are done
+template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // global -> shared; both addresses and the size are multiples of 16
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, unsigned bytes, u64 *bar)
 {

@@ -204,7 +204,8 @@ def distill_reference(z, t, ids, labels, T, alpha, beta, weight):
     """Loss per row and gradient in 64 bits from the formulas, and the magnitudes that the tolerances need."""
     n, vocab = z.shape
     z = z.double()
-    z = torch.where(torch.isinf(z) & (z < 0), torch.full_like(z, -1e6), z)  # the same to the last bit: exp(-1e6 + 88) = 0
+    some = ~torch.isneginf(z).all(dim=1)  # rows that have logits
+    z = torch.where(some[:, None], z, torch.zeros_like(z))
     d = z - z.max(dim=1, keepdim=True).values
     row = torch.zeros(n, dtype=torch.float64, device=DEV)
     row_mag, grad, grad_mag = row.clone(), torch.zeros_like(z), torch.zeros_like(z)
@@ -216,12 +217,12 @@ def distill_reference(z, t, ids, labels, T, alpha, beta, weight):
     eps = 2.0 ** -20 + 2.0 ** -22 * reach * max(1.0, 1.0 / T32) + (vocab / 512 + 45) * U
     if alpha and t is not None and t.shape[1]:
         valid = (ids >= 0) & (ids < vocab) & ~torch.isneginf(t.double())
-        has = valid.any(dim=1)
+        has = valid.any(dim=1) & some
         td = t.double().masked_fill(~valid, float("-inf")) / T32
-        q = torch.softmax(td, dim=1).masked_fill(~has[:, None], 0.0).masked_fill(~valid, 0.0)
+        q = torch.softmax(td, dim=1).masked_fill(~has[:, None] | ~valid, 0.0)
         at = ids.long().clamp(0, vocab - 1)
         lse = torch.logsumexp(d / T32, dim=1)
-        dk = d.gather(1, at) / T32
+        dk = (d.gather(1, at) / T32).masked_fill(q == 0, 0.0)  # -inf where a wanted entry is masked: an infinite loss
         log_q = torch.where(q > 0, q, 1.0).log()
         row += torch.where(has, a32 * T32 ** 2 * (q * (log_q - dk)).sum(1) + a32 * T32 ** 2 * lse, 0.0)
         spread = (td.masked_fill(~valid, 0.0).abs().max(dim=1).values * 2 + 1)
@@ -233,7 +234,7 @@ def distill_reference(z, t, ids, labels, T, alpha, beta, weight):
         grad += coef * (p - qs)
         grad_mag += coef * (p * eps + qs * (spread[:, None] * 2 ** -22 + 2 ** -21))
     if beta and labels is not None:
-        has = (labels >= 0) & (labels < vocab)
+        has = (labels >= 0) & (labels < vocab) & some
         y = labels.long().clamp(0, vocab - 1)
         lse = torch.logsumexp(d, dim=1)
         dy = d.gather(1, y[:, None])[:, 0]
@@ -274,7 +275,7 @@ def distill_inputs(n, vocab, k, dtype, seed, t_dtype=F32, id_dtype=torch.int32):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("T,alpha,beta", [(1.0, 1.0, 0.0), (1.0, 0.3, 0.7), (2.0, 0.5, 0.5), (4.0, 0.9, 0.1), (1.5, 0.5, 0.5),
+@pytest.mark.parametrize("T,alpha,beta", [(1.0, 1.0, 0.0), (1.0, 0.3, 0.7), (2.0, 0.5, 0.5), (4.0, 0.9, 0.1), (1.5, 0.5, 0.5), (3.0, 0.5, 0.5), (1.3, 0.5, 0.5),
                                           (0.5, 0.6, 0.4), (3.0, 1.0, 0.0), (2.0, 0.0, 1.0)])
 @pytest.mark.parametrize("n,vocab,k", [(1, 1, 1), (1, 5, 0), (3, 17, 4), (7, 1000, 64), (40, 4099, 33), (2, 50257, 64), (170, 12345, 9),
                                        (9, 33000, 1024)])
@@ -687,3 +688,50 @@ def test_wrong_shapes_and_types_are_refused():
         with pytest.raises(AdaScaleError) as e:
             call()
         assert e.value.status == 1
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,alpha,beta", [(1.0, 0.3, 0.7), (2.0, 0.5, 0.5), (4.0, 0.9, 0.1), (1.5, 0.5, 0.5), (3.0, 0.5, 0.5), (1.3, 0.5, 0.5),
+                                          (3.0, 1.0, 0.0), (2.0, 0.0, 1.0)])
+@pytest.mark.parametrize("n,vocab,k", [(900, 20001, 17), (911, 50257, 64), (890, 90003, 128), (80, 300007, 5)])
+def test_distill_many_long_rows(n, vocab, k, T, alpha, beta, dtype):
+    """Enough of them that rows stay in shared memory between the two walks; over several blocks where one cannot hold them."""
+    z, t, ids, labels, weight = distill_inputs(n, vocab, k, dtype, n + vocab)
+    z[5] = float("-inf")
+    z[9, 1::2] = float("-inf")
+    z[11] = LOWEST[dtype]
+    ids[13], labels[13] = -1, -100
+    weight[[5, 9, 11, 13]] = 1.0
+    ids[17] = ids[17, 0]  # one id all over
+    labels[18] = ids[18, 0]
+    labels[[19, 20]] = torch.tensor([0, vocab - 1], device=DEV)
+    got = ops.distill(z, t, ids, labels=labels, T=T, alpha=alpha, beta=beta, row_weight=weight)
+    rows = torch.arange(n, device=DEV).split(100)
+    for part in rows:  # the reference's temporaries are large
+        check_distill(ops.Distilled(got.row_loss[part].sum(), got.row_loss[part], got.dlogits[part]), z[part], t[part], ids[part],
+                      labels[part], T, alpha, beta, weight[part], "long rows")
+    assert float(got.loss) == math.inf if bool(torch.isinf(got.row_loss).any()) else \
+        abs(float(got.loss.double() - got.row_loss.double().sum())) <= 2 * U * float(got.row_loss.double().abs().sum())
+    again = ops.distill(z, t, ids, labels=labels, T=T, alpha=alpha, beta=beta, row_weight=weight)
+    assert torch.equal(again.loss, got.loss) and torch.equal(again.dlogits, got.dlogits)
+    place = z.clone()
+    ops.distill(place, t, ids, labels=labels, T=T, alpha=alpha, beta=beta, row_weight=weight, dlogits=place)
+    assert torch.equal(place, got.dlogits)
+
+
+@pytest.mark.parametrize("dtype,vocab", [(BF16, 33001), (F32, 30001), (F32, 40001)])
+def test_distill_many_long_rows_most_of_them_masked(dtype, vocab):
+    """Rows that are skipped between rows that are not; NaN in what is skipped."""
+    n, k = 900, 9
+    z, t, ids, labels, weight = distill_inputs(n, vocab, k, dtype, 77)
+    weight[:] = 0.5
+    weight[(torch.arange(n, device=DEV) * 7) % 11 < 8] = 0.0
+    z[weight == 0] = float("nan")
+    got = ops.distill(z, t, ids, labels=labels, T=2.0, alpha=0.5, beta=0.5, row_weight=weight)
+    live = weight != 0
+    assert not got.row_loss[~live].any() and not got.dlogits[~live].any()
+    check_distill(ops.Distilled(got.row_loss[live].sum(), got.row_loss[live], got.dlogits[live]), z[live], t[live], ids[live], labels[live],
+                  2.0, 0.5, 0.5, weight[live], "masked")
+    z[3], weight[3] = float("nan"), 1.0
+    got = ops.distill(z, t, ids, labels=labels, T=2.0, alpha=0.5, beta=0.5, row_weight=weight)
+    assert math.isnan(float(got.row_loss[3])) and bool(torch.isnan(got.dlogits[3]).all()) and not torch.isnan(got.dlogits[4:]).any()
