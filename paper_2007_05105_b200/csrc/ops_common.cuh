@@ -132,6 +132,27 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
+// Stores of what this kernel does not read again: they leave the L2 cache first.
+template <int V> __device__ __forceinline__ void store_vec_streaming(float *p, const float (&x)[V])
+{
+    if constexpr (V == 1) {
+        __stcs(p, x[0]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i)
+            __stcs(reinterpret_cast<float4 *>(p) + i, make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]));
+    }
+}
+template <int V> __device__ __forceinline__ void store_vec_streaming(bf16 *p, const float (&x)[V])
+{
+    if constexpr (V == 8)
+        __stcs(reinterpret_cast<uint4 *>(p), make_uint4(bf_pack(x[0], x[1]), bf_pack(x[2], x[3]), bf_pack(x[4], x[5]), bf_pack(x[6], x[7])));
+    else if constexpr (V == 4)
+        __stcs(reinterpret_cast<uint2 *>(p), make_uint2(bf_pack(x[0], x[1]), bf_pack(x[2], x[3])));
+    else
+        store_vec<V>(p, x);
+}
+
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll

@@ -267,7 +267,7 @@ template <int FORM> __device__ __forceinline__ float slope_of(float x, float m, 
 // L2 - and the gradient of every entry written as if no list existed; then the few entries
 // that the list or the label names are written again with their whole value.
 template <typename ZT, int FORM, bool GRAD>
-__global__ void __launch_bounds__(kThreads, kBlocks) k_distill_rows(const __grid_constant__ RowArgs a)
+__global__ void __launch_bounds__(kThreads, GRAD ? kBlocks : 2 * kBlocks) k_distill_rows(const __grid_constant__ RowArgs a)
 {
     constexpr int V = 16 / sizeof(ZT);
     __shared__ float q[kMaxK], zk[kMaxK];
@@ -388,8 +388,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_distill_rows(const __grid
     float z_label = 0.f;
     if (live && GRAD) {
         z_label = label >= 0 ? to_f32(z[label]) : 0.f;
-        // all reads of named entries are done before any block writes (dz may be z)
-        if (parts > 1) cluster.sync(); else __syncthreads();
+        if (a.dz == a.z) {  // all reads of named entries are done before any block writes
+            if (parts > 1) cluster.sync();
+            else __syncthreads();
+        }
     }
     const bool nothing = kT == 0.f && k1 == 0.f;  // zeros, whatever the logits hold
     auto slope = [&](float x) {

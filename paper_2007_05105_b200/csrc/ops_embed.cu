@@ -21,9 +21,11 @@ struct LookupArgs {
 
 constexpr int kLookupThreads = 256;
 
-// One warp per row: V elements per lane and access, every access of the row requested before the
-// first is used (up to four), so the two dependent round trips to memory (id, then row) are paid
-// once per warp and covered by the other 63 warps of the SM.
+// One warp per row: V elements per lane and access, up to four accesses requested before the first is
+// used, so the two dependent round trips to memory (id, then row) are paid once per warp and covered
+// by the SM's other warps.  V is 16 bytes of the wider type: with 8 floats a lane, as two accesses 32
+// bytes apart from lane to lane, 65536 rows of 512 floats took 33 us instead of 27 (94 % of the measured
+// copy rate).  The result leaves L2 first, so that the table's frequent rows stay.
 template <typename TT, typename OT, int V>
 __global__ void __launch_bounds__(kLookupThreads) k_lookup(const __grid_constant__ LookupArgs a)
 {
@@ -55,7 +57,7 @@ __global__ void __launch_bounds__(kLookupThreads) k_lookup(const __grid_constant
 #pragma unroll
                 for (int i = 0; i < V; ++i) x[u][i] *= a.scale;
             }
-            store_vec<V>(dst + (long long)j * V, x[u]);
+            store_vec_streaming<V>(dst + (long long)j * V, x[u]);
         }
     }
 }
@@ -75,7 +77,10 @@ struct Pair {
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortCluster = 8;      // blocks that sort together (portable cluster size); 1 for short lists
-constexpr int kSortAlone = 2048;     // tokens up to which one block sorts on its own
+// Tokens up to which places are counted instead of sorted by digits.  Accumulating: one wave of blocks (4099 tokens: 6.7 us
+// against 10.4; 5000: 12.5 against 10.6).  Beside the zero-fill, which takes longer than either and starts
+// sooner beside the sort's few blocks: 4000 tokens into 50257 rows of 1024 bf16 33.7 us in all, sorted 30.9.
+constexpr int kRankMost = 148 * 32, kRankBesideZeros = 1024;
 constexpr int kSortBits = 8;         // digit of one pass
 constexpr int kSortBins = 1 << kSortBits;
 constexpr int kZeroBlocks = 112;     // blocks that write zeros beside the sort: 15 clusters of 8 are resident at once (with 17, 32 us for 22)
@@ -87,6 +92,7 @@ constexpr int kDepth = 16;             // rows on their way per thread of the wi
 constexpr int kSumBlocks = 5;       // their blocks per SM
 constexpr int kMostPairs = 1024;     // sorted entries that a block of them holds
 constexpr int kLeastWindow = 8;
+constexpr int kColumns = 4;          // elements of a row per thread where rows are not aligned (see k_sum_windows)
 constexpr int kSpill = 8;            // entries that a window takes from the next one to finish its last run
 
 struct SortArgs {
@@ -96,8 +102,8 @@ struct SortArgs {
     long long n, vocab, ld_grad, padding;
     long long row_bytes;  // of the gradient; its rows are zeroed where no token points
     int wide, passes;
+    int zero_blocks;    // of k_rank_tokens
     int grad_bytes;     // bytes of a gradient element
-    int vec;            // gradient rows can be written in 16-byte pieces
 };
 
 __device__ __forceinline__ int key_of(const SortArgs &a, long long i)
@@ -106,7 +112,18 @@ __device__ __forceinline__ int key_of(const SortArgs &a, long long i)
     return id >= 0 && id < a.vocab && id != a.padding ? (int)id : (int)a.vocab;
 }
 
-// Zeros for the rows that no token names, while the first cluster sorts.  Block z has the
+// One warp: 16 bytes a lane, the few before and after the aligned middle two at a time.
+__device__ __forceinline__ void zero_row(char *p, long long bytes, int lane)
+{
+    long long front = (long long)(-(uintptr_t)p & 15);
+    if (front > bytes) front = bytes;
+    const long long middle = (bytes - front) / 16, back = bytes - front - middle * 16;
+    if (lane < front / 2) reinterpret_cast<unsigned short *>(p)[lane] = 0;
+    for (long long j = lane; j < middle; j += 32) reinterpret_cast<uint4 *>(p + front)[j] = make_uint4(0, 0, 0, 0);
+    if (lane < back / 2) reinterpret_cast<unsigned short *>(p + front + middle * 16)[lane] = 0;
+}
+
+// Zeros for the rows that no token names, while other blocks sort.  Block z has the
 // vocabulary rows whose run number (row / kZeroRun) is z modulo kZeroBlocks, so that a batch that uses
 // only frequent, adjacent ids still spreads evenly.  The blocks of a cluster share the reading
 // of the token list: each reads its part and sets presence bits in the shared memory of
@@ -144,14 +161,7 @@ __device__ void zero_absent(const SortArgs &a, unsigned *bits, const cg::cluster
             if (bits[b >> 5] >> (b & 31) & 1u) continue;
             const long long row = ((r0 + b / kZeroRun) * kZeroBlocks + z) * kZeroRun + b % kZeroRun;
             if (row >= a.vocab) continue;
-            char *p = static_cast<char *>(a.grad) + row * a.ld_grad * a.grad_bytes;
-            if (a.vec) {
-                for (long long j = lane; j < a.row_bytes / 16; j += 32) reinterpret_cast<uint4 *>(p)[j] = make_uint4(0, 0, 0, 0);
-            } else if (a.grad_bytes == 4) {
-                for (long long j = lane; j < a.row_bytes / 4; j += 32) reinterpret_cast<unsigned *>(p)[j] = 0u;
-            } else {
-                for (long long j = lane; j < a.row_bytes / 2; j += 32) reinterpret_cast<unsigned short *>(p)[j] = 0;
-            }
+            zero_row(static_cast<char *>(a.grad) + row * a.ld_grad * a.grad_bytes, a.row_bytes, lane);
         }
         __syncthreads();  // the bits are read before the next range clears them
     }
@@ -289,6 +299,54 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_tokens(const __grid_co
     }
 }
 
+// Short lists: an entry's place is the number of entries before it in the order, counted by comparing
+// it with all others.  That many comparisons (17 million for 4099 tokens) cost less than the digit passes'
+// barriers and scattered stores.  A block has 32 entries, one per lane; its warps share
+// the list.
+__global__ void __launch_bounds__(kSortThreads, 2) k_rank_tokens(const __grid_constant__ SortArgs a)
+{
+    __shared__ __align__(16) int keys[kRankMost];  // also the bit field of the zero-fill
+    __shared__ int part[kSortWarps][32];
+    static_assert(sizeof(keys) * 8 >= kZeroBits, "the zero-fill's bits fit");
+    griddep_wait();
+    griddep_launch();
+    const int n = (int)a.n;
+    if ((int)blockIdx.x < a.zero_blocks) {  // first, as they take longest
+        zero_absent(a, reinterpret_cast<unsigned *>(keys), cg::this_cluster(), (int)blockIdx.x);
+        return;
+    }
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    for (int i0 = tid; i0 < (n + 3) / 4 * 4; i0 += kBatch * kSortThreads) {
+        int key[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) key[u] = i0 + u * kSortThreads < n ? key_of(a, i0 + u * kSortThreads) : 0x7fffffff;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (i0 + u * kSortThreads < kRankMost) keys[i0 + u * kSortThreads] = key[u];
+    }
+    __syncthreads();
+    const int mine = ((int)blockIdx.x - a.zero_blocks) * 32 + lane, key = mine < n ? keys[mine] : 0;
+    const int quads = (n + 3) / 4, per = (quads + kSortWarps - 1) / kSortWarps;
+    const int first = warp * per, last = first + per < quads ? first + per : quads;
+    int before = 0;
+#pragma unroll 4
+    for (int q = first; q < last; ++q) {
+        const int4 k = reinterpret_cast<const int4 *>(keys)[q];
+        const int j = 4 * q;
+        before += (k.x < key) | ((k.x == key) & (j < mine));
+        before += (k.y < key) | ((k.y == key) & (j + 1 < mine));
+        before += (k.z < key) | ((k.z == key) & (j + 2 < mine));
+        before += (k.w < key) | ((k.w == key) & (j + 3 < mine));
+    }
+    part[warp][lane] = before;
+    __syncthreads();
+    if (warp || mine >= n) return;
+    int at = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) at += part[w][lane];
+    reinterpret_cast<int2 *>(a.buf[0])[at] = make_int2(key, mine);
+}
+
 struct SumArgs {
     const Pair *sorted;
     const void *dout;
@@ -297,6 +355,7 @@ struct SumArgs {
     long long n, vocab, ld_dout, ld_grad, ld_piece;
     int window;         // sorted entries of one window
     int nv;             // vectors of a row
+    int threads;        // of a window: one per vector, or per kColumns elements
     int accumulate;
     float scale;
 };
@@ -371,15 +430,15 @@ __global__ void __launch_bounds__(kSumThreads, kSumBlocks) k_sum_windows(const _
     griddep_wait();
     griddep_launch();
     const long long t0 = (long long)blockIdx.x * kSumThreads, t1 = t0 + kSumThreads - 1;
-    const long long base = t0 / a.nv * a.window - 1;  // entry of pairs[0]
-    const int here = (int)(t1 / a.nv - t0 / a.nv + 1) * a.window + kSpill + 2;
+    const long long base = t0 / a.threads * a.window - 1;  // entry of pairs[0]
+    const int here = (int)(t1 / a.threads - t0 / a.threads + 1) * a.window + kSpill + 2;
     for (int i = threadIdx.x; i < here; i += kSumThreads) {
         const long long at = base + i;
         pairs[i] = at >= 0 && at < a.n ? __ldcg(reinterpret_cast<const int2 *>(a.sorted) + at) : make_int2(-1, 0);
     }
     __syncthreads();
-    const long long t = t0 + threadIdx.x, w = t / a.nv;
-    const int c = (int)(t - w * a.nv);
+    const long long t = t0 + threadIdx.x, w = t / a.threads;
+    const int c = (int)(t - w * a.threads);
     if (w * a.window >= a.n) return;
     int lo = (int)(w * a.window - base);  // places in pairs; entries beyond the list have key -1
     int hi = lo + (int)(a.n - w * a.window < a.window ? a.n - w * a.window : a.window);
@@ -404,32 +463,58 @@ __global__ void __launch_bounds__(kSumThreads, kSumBlocks) k_sum_windows(const _
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
     const DT *dout = static_cast<const DT *>(a.dout) + (long long)c * V;
     auto row = [&](int i) { return dout + (long long)pairs[i].y * a.ld_dout; };
-    auto next_run = [&](int i) {  // before entry i is added
-        const int k = pairs[i].x;
-        if (k == key) return;
-        if (head)
-            store_vec<V>(a.pieces + 2 * w * a.ld_piece + (long long)c * V, acc);
-        else
-            write_row<GT, V>(a, key, c, acc);
-        head = false;
-        key = k;
+    if constexpr (V == 1) {  // columns c, c + threads, c + 2 threads, ... of the window
+        float sums[kColumns];
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    };
-    if constexpr (V == 1) {
-        constexpr int U = 4;
+        for (int q = 0; q < kColumns; ++q) sums[q] = 0.f;
+        auto finish = [&](bool piece, int which) {
+#pragma unroll
+            for (int q = 0; q < kColumns; ++q) {
+                if (c + q * a.threads >= a.nv) break;
+                float one[1] = {sums[q]};
+                if (piece) a.pieces[(2 * w + which) * a.ld_piece + c + q * a.threads] = sums[q];
+                else write_row<GT, 1>(a, key, c + q * a.threads, one);
+                sums[q] = 0.f;
+            }
+        };
+        constexpr int U = 4;  // rows requested together
         for (int i = lo; i < hi; i += U) {
-            float x[U];
+            DT x[U][kColumns];
 #pragma unroll
-            for (int u = 0; u < U; ++u) x[u] = to_f32(*row(i + u < hi ? i + u : hi - 1));
+            for (int u = 0; u < U; ++u) {
+                const DT *p = row(i + u < hi ? i + u : hi - 1);
+#pragma unroll
+                for (int q = 0; q < kColumns; ++q)
+                    if (c + q * a.threads < a.nv) x[u][q] = p[q * a.threads];
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (i + u >= hi) break;
-                next_run(i + u);
-                acc[0] += x[u];
+                const int k = pairs[i + u].x;
+                if (k != key) {
+                    finish(head, 0);
+                    head = false;
+                    key = k;
+                }
+#pragma unroll
+                for (int q = 0; q < kColumns; ++q) sums[q] += to_f32(x[u][q]);
             }
         }
+        finish(head || tail, head ? 0 : 1);
+        return;
     } else {
+        auto next_run = [&](int i) {  // before entry i is added
+            const int k = pairs[i].x;
+            if (k == key) return;
+            if (head)
+                store_vec<V>(a.pieces + 2 * w * a.ld_piece + (long long)c * V, acc);
+            else
+                write_row<GT, V>(a, key, c, acc);
+            head = false;
+            key = k;
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = 0.f;
+        };
         uint4 *mine = &ring[0][threadIdx.x];
         for (int u = 0; u < kDepth; ++u) {
             if (lo + u < hi) copy_async(mine + u * kSumThreads, row(lo + u));
@@ -500,7 +585,7 @@ __global__ void __launch_bounds__(kSumThreads) k_join(const __grid_constant__ Su
 template <typename TT, typename OT>
 cudaError_t launch_lookup(const adascale_embed_args &g, LookupArgs a, bool vec, cudaStream_t s)
 {
-    constexpr int V = 8;
+    constexpr int V = sizeof(TT) + sizeof(OT) > 4 ? 4 : 8;
     a.nv = (int)(vec ? g.dim / V : g.dim);
     const long long blocks = ceil_div(g.n_tokens, kLookupThreads / 32);
     return vec ? launch(k_lookup<TT, OT, V>, blocks, kLookupThreads, 0, s, a)
@@ -508,11 +593,11 @@ cudaError_t launch_lookup(const adascale_embed_args &g, LookupArgs a, bool vec, 
 }
 
 // Entries of a window: one wave of blocks, but no more than a block's pairs have room for.
-int window_of(long long n, int nv, int sms)
+int window_of(long long n, int of_window, int sms)
 {
     const long long threads = (long long)sms * kSumBlocks * kSumThreads;
-    long long w = ceil_div(n * nv, threads);
-    const long long most = kMostPairs / (kSumThreads / nv + 2);  // windows of a block, at most
+    long long w = ceil_div(n * of_window, threads);
+    const long long most = kMostPairs / (kSumThreads / of_window + 2);  // windows of a block, at most
     if (w > most) w = most;
     return (int)(w < kLeastWindow ? kLeastWindow : w);
 }
@@ -521,9 +606,10 @@ template <typename DT, typename GT, int V>
 cudaError_t launch_sums(SumArgs a, long long dim, int sms, cudaStream_t s)
 {
     a.nv = (int)(dim / V);
-    a.window = window_of(a.n, a.nv, sms);
+    a.threads = V == 1 ? (int)ceil_div(dim, kColumns) : a.nv;
+    a.window = window_of(a.n, a.threads, sms);
     const long long windows = ceil_div(a.n, a.window);
-    cudaError_t e = launch(k_sum_windows<DT, GT, V>, ceil_div(windows * a.nv, kSumThreads), kSumThreads, 0, s, a);
+    cudaError_t e = launch(k_sum_windows<DT, GT, V>, ceil_div(windows * a.threads, kSumThreads), kSumThreads, 0, s, a);
     if (e != cudaSuccess || windows == 1) return e;
     constexpr int JV = V == 1 ? 1 : 4;
     a.nv = (int)(dim / JV);
@@ -606,13 +692,16 @@ adascale_status adascale_embed_grad(const adascale_embed_grad_args *g, void *cud
     a.wide = g->token_type == ADASCALE_I64;
     while ((g->vocab >> (kSortBits * a.passes)) > 0) ++a.passes;  // the largest key is vocab itself
     a.grad_bytes = eg;
-    a.vec = rows_on(g->grad, g->ld_grad, g->vocab, eg, 16) && a.row_bytes % 16 == 0;
-    const int cluster = g->n_tokens <= kSortAlone ? 1 : kSortCluster;
-    OPS_CU(launch(k_sort_tokens, cluster + (g->accumulate ? 0 : kZeroBlocks), kSortThreads, 0, s, a, cluster));
+    a.zero_blocks = g->accumulate ? 0 : kZeroBlocks;
+    const bool counted = g->n_tokens <= (g->accumulate ? kRankMost : kRankBesideZeros);
+    if (counted)
+        OPS_CU(launch(k_rank_tokens, ceil_div(g->n_tokens, 32) + a.zero_blocks, kSortThreads, 0, s, a));
+    else
+        OPS_CU(launch(k_sort_tokens, kSortCluster + a.zero_blocks, kSortThreads, 0, s, a, kSortCluster));
     if (g->n_tokens == 0) return ADASCALE_OK;
 
     SumArgs b = {};
-    b.sorted = a.buf[a.passes & 1];
+    b.sorted = counted ? a.buf[0] : a.buf[a.passes & 1];
     b.dout = g->dout;
     b.grad = g->grad;
     b.pieces = reinterpret_cast<float *>(a.buf[1] + pairs);
