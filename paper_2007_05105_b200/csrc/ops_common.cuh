@@ -306,6 +306,19 @@ inline int sm_count()
     return n;
 }
 
+// Lets a kernel have `smem` bytes of dynamic shared memory on the current device.  `known` (of the kernel, zero at first)
+// remembers per device what it may have already; threads that race ask for it twice.
+inline cudaError_t allow_smem(const void *kernel, size_t smem, int (&known)[64])
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64 && known[dev] >= (int)smem) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess && dev >= 0 && dev < 64) known[dev] = (int)smem;
+    return e;
+}
+
 inline bool is_dtype(int d) { return d == ADASCALE_F32 || d == ADASCALE_BF16; }
 inline bool is_itype(int d) { return d == ADASCALE_I32 || d == ADASCALE_I64; }
 inline int elem_bytes(int dtype) { return dtype == ADASCALE_F32 ? 4 : 2; }

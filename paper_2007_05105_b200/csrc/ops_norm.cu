@@ -252,30 +252,40 @@ struct NormArgs {
     int dim;
     int post, pre, gate_kind;
     unsigned stage_bytes;
+    unsigned weight_bytes;  // of the vectors' copies in shared memory; 0: read where they are
     float inv_dim, res_scale, eps;
 };
 
 // Threads of a block: of its one group, or four warps that are groups of their own.
 __host__ __device__ constexpr int threads_of(int group) { return group == 32 ? 128 : group; }
+// Forward, most of a block: sixteen warps, fewer where their stages do not fit or there are few rows.
+__host__ __device__ constexpr int forward_threads(int group) { return group == 32 ? 512 : group; }
 // Blocks that an SM holds: as many as leave a thread the registers that it needs.  Gradient, 16384 x 1024 (f32
 // stream, bf16 block, layer norms, channel gate): 384 threads an SM (168 registers) 61 us, 256 (180) 68, 512 (128) 81.
-constexpr int forward_blocks(int group) { return group <= 128 ? 512 / threads_of(group) : group <= 256 ? 2 : 1; }
+constexpr int forward_blocks(int group) { return group == 32 ? 1 : group <= 256 ? 512 / group : 1; }
 constexpr int gradient_blocks(int group) { return group <= 128 ? 384 / threads_of(group) : 1; }
 
-template <int XT, int YT, int V, bool FULL, int GROUP>
-__global__ void __launch_bounds__(threads_of(GROUP), forward_blocks(GROUP)) k_boundary(const __grid_constant__ NormArgs a)
+// Rows by bulk copies ahead of the work where both types are bf16 and a row is a warp's (16384 x 1024: 28 us against
+// 32); otherwise each row is loaded when its turn comes (f32 stream: 39 us against 42; 16384 x 2048: 74 against 83).
+template <int XT, int YT, int V> __host__ __device__ constexpr bool forward_staged(int group)
 {
-    constexpr int E = kForwardElems, kGroups = threads_of(GROUP) / GROUP;
-    constexpr bool kStaged = V == 4 && GROUP * E <= kStageMost;
+    return V == 4 && group == 32 && XT == kBf16 && YT == kBf16;
+}
+
+template <int XT, int YT, int V, bool FULL, int GROUP, int E>
+__global__ void __launch_bounds__(forward_threads(GROUP), forward_blocks(GROUP)) k_boundary(const __grid_constant__ NormArgs a)
+{
+    constexpr int kMostGroups = forward_threads(GROUP) / GROUP;
+    constexpr bool kStaged = forward_staged<XT, YT, V>(GROUP);
     extern __shared__ __align__(128) char room[];
     __shared__ __align__(8) float scratch[2][GROUP / 32][2];
-    __shared__ u64 full[kGroups][kStages];
-    const int mine = threadIdx.x / GROUP;
+    __shared__ u64 full[kMostGroups][kStages];
+    const int mine = threadIdx.x / GROUP, groups = blockDim.x / GROUP;
     const Place<E, V, FULL> at = {GROUP, (int)threadIdx.x % GROUP, a.dim};
-    const long long all = (long long)gridDim.x * kGroups;
-    const Stages stages = {room + mine * kStages * a.stage_bytes, full[mine], a.stage_bytes};
+    const long long all = (long long)gridDim.x * groups;
+    const Stages stages = {room + a.weight_bytes + mine * kStages * a.stage_bytes, full[mine], a.stage_bytes};
     GroupSum<GROUP> sum = {scratch, 0};
-    long long row = (long long)blockIdx.x * kGroups + mine;
+    long long row = (long long)blockIdx.x * groups + mine;
     if (kStaged && at.t == 0) {
         for (int s = 0; s < kStages; ++s) mbar_init(full[mine] + s, 1);
         mbar_publish();
@@ -283,6 +293,20 @@ __global__ void __launch_bounds__(threads_of(GROUP), forward_blocks(GROUP)) k_bo
     group_barrier<GROUP>();
     griddep_wait();
     griddep_launch();
+    const float *w_post = a.w_post, *b_post = a.b_post, *channel = a.gate_channel, *w_pre = a.w_pre, *b_pre = a.b_pre;
+    if (a.weight_bytes) {  // many rows: the vectors over the columns in shared memory
+        float *at_room = reinterpret_cast<float *>(room);
+        const float **all_of_them[5] = {&w_post, &b_post, &channel, &w_pre, &b_pre};
+#pragma unroll
+        for (int k = 0; k < 5; ++k) {
+            const float *&w = *all_of_them[k];
+            if (!w) continue;
+            for (int c = threadIdx.x; c < a.dim; c += blockDim.x) at_room[c] = w[c];
+            w = at_room;
+            at_room += (a.dim + 3) / 4 * 4;
+        }
+        __syncthreads();
+    }
     const Rows *const arrays[3] = {&a.x, &a.y, &a.gate};
     if (kStaged && at.t == 0)
         for (int s = 0; s < kStages; ++s)
@@ -317,16 +341,16 @@ __global__ void __launch_bounds__(threads_of(GROUP), forward_blocks(GROUP)) k_bo
                 s = products<E>(y, y);
                 sum(s);
                 scale<E>(y, rsqrtf(fmaf(s, a.inv_dim, a.eps)));
-                read<E, V, FULL>(at, a.w_post, w);
+                read<E, V, FULL>(at, w_post, w);
                 times<E>(y, w);
-                if (a.b_post) {
-                    read<E, V, FULL>(at, a.b_post, w);
+                if (b_post) {
+                    read<E, V, FULL>(at, b_post, w);
                     plus<E>(y, w);
                 }
             }
             if (a.gate_kind != ADASCALE_GATE_NONE) {
                 if (a.gate_kind == ADASCALE_GATE_CHANNEL) {
-                    read<E, V, FULL>(at, a.gate_channel, w);
+                    read<E, V, FULL>(at, channel, w);
                 } else {
                     read<E, V, FULL>(at, pg, is_bf16<YT>(a.gate), w);
                     sigmoids<E>(w);
@@ -352,10 +376,10 @@ __global__ void __launch_bounds__(threads_of(GROUP), forward_blocks(GROUP)) k_bo
         s = products<E>(x, x);
         sum(s);
         scale<E>(x, rsqrtf(fmaf(s, a.inv_dim, a.eps)));
-        read<E, V, FULL>(at, a.w_pre, w);
+        read<E, V, FULL>(at, w_pre, w);
         times<E>(x, w);
-        if (a.b_pre) {
-            read<E, V, FULL>(at, a.b_pre, w);
+        if (b_pre) {
+            read<E, V, FULL>(at, b_pre, w);
             plus<E>(x, w);
         }
         write<E, V, FULL>(at, a.h.row(row), is_bf16<YT>(a.h), x);
@@ -601,43 +625,45 @@ unsigned row_bytes(const Rows &m, int dim) { return !m.p ? 0 : (unsigned)dim * (
 // Blocks of a persistent launch: `most` an SM, fewer where their stages do not fit.
 long long resident(int sms, int most, size_t smem)
 {
-    const long long fit = (long long)(224 * 1024 / (smem + 2 * 1024));
+    const long long fit = (long long)(227 * 1024 / (smem + 1280));
     return (long long)sms * (fit < most ? (fit < 1 ? 1 : fit) : most);
 }
 
-// Shared memory beyond the 48 KB that need no permission, what the kernel declares itself included.
-template <typename Args> cudaError_t launch_staged(void (*kernel)(Args), long long blocks, int threads, size_t smem, cudaStream_t s, const Args &a)
+// Where a row is a warp's: few rows, blocks of four warps that read the vectors where they are; many rows, blocks of
+// sixteen with a copy of the vectors in shared memory (in L1 they are evicted between rows: 42 us for 39).
+template <int XT, int YT, int V, bool FULL, int GROUP, int E> cudaError_t launch_boundary(NormArgs a, int sms, cudaStream_t s)
 {
-    if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
+    const int vectors = (a.w_post != nullptr) + (a.b_post != nullptr) + (a.gate_channel != nullptr) + 1 + (a.b_pre != nullptr);
+    const unsigned copies = (unsigned)(vectors * ((a.dim + 3) / 4 * 4) * sizeof(float));
+    const size_t stages = forward_staged<XT, YT, V>(GROUP) ? (size_t)kStages * a.stage_bytes : 0;  // of a group
+    int groups = GROUP == 32 ? 4 : 1;
+    if (GROUP == 32 && a.n >= 64LL * sms) {
+        groups = forward_threads(GROUP) / GROUP;
+        a.weight_bytes = copies;
     }
-    return launch(kernel, blocks, threads, smem, s, a);
+    const size_t smem = groups * stages + a.weight_bytes;
+    const long long need = ceil_div(a.n, groups), most = resident(sms, 512 / (groups * GROUP) > 1 ? 512 / (groups * GROUP) : 1, smem);
+    static int known[64] = {0};
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary<XT, YT, V, FULL, GROUP, E>), smem, known);
+    return e != cudaSuccess ? e : launch(k_boundary<XT, YT, V, FULL, GROUP, E>, need < most ? need : most, groups * GROUP, smem, s, a);
 }
-
-template <int XT, int YT, int V, bool FULL, int GROUP> cudaError_t launch_boundary(const NormArgs &a, int sms, cudaStream_t s)
-{
-    constexpr int kGroups = threads_of(GROUP) / GROUP;
-    constexpr bool kStaged = V == 4 && GROUP * kForwardElems <= kStageMost;
-    const size_t smem = kStaged ? (size_t)kGroups * kStages * a.stage_bytes : 0;
-    const long long need = ceil_div(a.n, kGroups), most = resident(sms, forward_blocks(GROUP), smem);
-    return launch_staged(k_boundary<XT, YT, V, FULL, GROUP>, need < most ? need : most, threads_of(GROUP), smem, s, a);
-}
-template <int XT, int YT, int V, bool FULL> cudaError_t launch_boundary(const NormArgs &a, int group, int sms, cudaStream_t s)
+template <int XT, int YT, int V, bool FULL> cudaError_t launch_boundary(const NormArgs &a, int group, int per, int sms, cudaStream_t s)
 {
     switch (group) {
-    case 32: return launch_boundary<XT, YT, V, FULL, 32>(a, sms, s);
-    case 64: return launch_boundary<XT, YT, V, FULL, 64>(a, sms, s);
-    case 128: return launch_boundary<XT, YT, V, FULL, 128>(a, sms, s);
-    case 256: return launch_boundary<kAny, kAny, V, FULL, 256>(a, sms, s);
+    case 32:
+        if (per == 8) return launch_boundary<XT, YT, V, FULL, 32, 8>(a, sms, s);
+        return per == 16 ? launch_boundary<XT, YT, V, FULL, 32, 16>(a, sms, s) : launch_boundary<XT, YT, V, FULL, 32, 32>(a, sms, s);
+    case 64: return launch_boundary<XT, YT, V, FULL, 64, 32>(a, sms, s);
+    case 128: return launch_boundary<XT, YT, V, FULL, 128, 32>(a, sms, s);
+    case 256: return launch_boundary<kAny, kAny, V, FULL, 256, 32>(a, sms, s);
     }
-    return launch_boundary<kAny, kAny, V, FULL, 512>(a, sms, s);
+    return launch_boundary<kAny, kAny, V, FULL, 512, 32>(a, sms, s);
 }
 template <int XT, int YT> cudaError_t launch_boundary(const NormArgs &a, bool vec, int sms, cudaStream_t s)
 {
-    const int group = group_of(a.dim, kForwardElems);
-    if (!vec) return launch_boundary<kAny, kAny, 1, false>(a, group, sms, s);
-    return group * kForwardElems == a.dim ? launch_boundary<XT, YT, 4, true>(a, group, sms, s) : launch_boundary<XT, YT, 4, false>(a, group, sms, s);
+    const int per = a.dim <= 256 ? 8 : a.dim <= 512 ? 16 : kForwardElems, group = group_of(a.dim, per);
+    if (!vec) return launch_boundary<XT, YT, 1, false>(a, group, per, sms, s);
+    return group * per == a.dim ? launch_boundary<XT, YT, 4, true>(a, group, per, sms, s) : launch_boundary<XT, YT, 4, false>(a, group, per, sms, s);
 }
 
 template <int XT, int YT, int V, bool FULL, int GROUP> cudaError_t launch_grad(const GradArgs &a, int sms, cudaStream_t s, int &partials)
@@ -652,7 +678,9 @@ template <int XT, int YT, int V, bool FULL, int GROUP> cudaError_t launch_grad(c
     if (blocks > kMaxPartials) blocks = kMaxPartials;
     if (blocks > need) blocks = need;
     partials = (int)blocks;
-    return launch_staged(k_boundary_grad<XT, YT, V, FULL, GROUP>, blocks, threads_of(GROUP), smem, s, a);
+    static int known[64] = {0};
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary_grad<XT, YT, V, FULL, GROUP>), smem, known);
+    return e != cudaSuccess ? e : launch(k_boundary_grad<XT, YT, V, FULL, GROUP>, blocks, threads_of(GROUP), smem, s, a);
 }
 template <int XT, int YT, int V, bool FULL> cudaError_t launch_grad(const GradArgs &a, int group, int sms, cudaStream_t s, int &partials)
 {
@@ -668,7 +696,7 @@ template <int XT, int YT, int V, bool FULL> cudaError_t launch_grad(const GradAr
 template <int XT, int YT> cudaError_t launch_grad(const GradArgs &a, bool vec, int sms, cudaStream_t s, int &partials)
 {
     const int group = group_of(a.dim, kGradElems);
-    if (!vec) return launch_grad<kAny, kAny, 1, false>(a, group, sms, s, partials);
+    if (!vec) return launch_grad<XT, YT, 1, false>(a, group, sms, s, partials);
     return group * kGradElems == a.dim ? launch_grad<XT, YT, 4, true>(a, group, sms, s, partials)
                                        : launch_grad<XT, YT, 4, false>(a, group, sms, s, partials);
 }
@@ -717,9 +745,12 @@ adascale_status adascale_residual_norm(const adascale_residual_norm_args *g, voi
     a.res_scale = g->res_scale;
     a.eps = g->eps;
     const long long n = g->n_rows;
-    const bool vec = g->dim % 8 == 0 && rows_on(g->x, g->ld_x, n, ex, 16) && rows_on(g->h, g->ld_h, n, ey, 16) && on(a.w_pre, 16) &&
-                     on(a.b_pre, 16) && (!g->y || (rows_on(g->y, g->ld_y, n, ey, 16) && rows_on(g->x_new, g->ld_x_new, n, ex, 16))) &&
-                     on(a.w_post, 16) && on(a.b_post, 16) && on(a.gate_channel, 16) && rows_on(a.gate.p, g->ld_gate, n, ey, 16);
+    // four elements an access; bulk copies, where the kernel for the types uses them, want 16 bytes
+    const bool bulk = forward_staged<kBf16, kBf16, 4>(32) && ex == 2 && ey == 2;
+    const int bx = bulk ? 16 : 4 * ex, by = bulk ? 16 : 4 * ey;
+    const bool vec = g->dim % (bulk ? 8 : 4) == 0 && rows_on(g->x, g->ld_x, n, ex, bx) && rows_on(g->h, g->ld_h, n, ey, by) && on(a.w_pre, 16) &&
+                     on(a.b_pre, 16) && (!g->y || (rows_on(g->y, g->ld_y, n, ey, by) && rows_on(g->x_new, g->ld_x_new, n, ex, bx))) &&
+                     on(a.w_post, 16) && on(a.b_post, 16) && on(a.gate_channel, 16) && rows_on(a.gate.p, g->ld_gate, n, ey, by);
     cudaStream_t s = (cudaStream_t)cuda_stream;
     a.stage_bytes = row_bytes(a.x, a.dim) + row_bytes(a.y, a.dim) + row_bytes(a.gate, a.dim);
     if (g->x_dtype == ADASCALE_F32)
