@@ -17,6 +17,7 @@
 
 #include <cstdarg>
 #include <cstdio>
+#include <optional>
 #include <string>
 
 namespace {
@@ -136,6 +137,28 @@ at::Tensor make(at::IntArrayRef shape, at::ScalarType type, at::Device device)
 {
     return at::detail::empty_cuda(shape, type, device, std::nullopt);
 }
+// Vectors that are made together share one allocation: each of its own cost 0.8 us, of the 13.7 us of a
+// gradient call of the block boundary.  Starts are 256 bytes apart.
+class Together {
+  public:
+    Together(int count, int64_t n, at::ScalarType type, at::Device device)
+        : n_(n), step_((n + 127) / 128 * 128), base_(make({count * step_}, type, device))
+    {
+    }
+    at::Tensor next(bool scalar = false)
+    {
+        at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base_.storage()), base_.key_set(), base_.dtype());
+        t.unsafeGetTensorImpl()->set_storage_offset(used_++ * step_);
+        if (scalar) t.unsafeGetTensorImpl()->set_sizes_contiguous({});
+        else t.unsafeGetTensorImpl()->set_sizes_contiguous({n_});
+        return t;
+    }
+
+  private:
+    int64_t n_, step_, used_ = 0;
+    at::Tensor base_;
+};
+
 // The given tensor, or a new one.
 at::Tensor given_or_new(const at::Tensor *t, at::IntArrayRef shape, at::ScalarType type, at::Device device, const char *what)
 {
@@ -290,7 +313,8 @@ PyObject *distill(PyObject *const *o)
         a.dlogits = m.p;
         a.ld_dlogits = m.ld;
     }
-    const at::Tensor row_loss = make({shape.n}, at::kFloat, device), loss = make({}, at::kFloat, device);
+    Together room(2, shape.n > 0 ? shape.n : 1, at::kFloat, device);
+    const at::Tensor loss = room.next(true), row_loss = shape.n > 0 ? room.next() : make({0}, at::kFloat, device);
     a.row_loss = static_cast<float *>(row_loss.data_ptr());
     a.loss = static_cast<float *>(loss.data_ptr());
     const adascale_status s = adascale_distill(&a, stream_of(device));
@@ -393,8 +417,15 @@ PyObject *residual_norm_grad(PyObject *const *o)
         p = rows(t, type, what, ld);
         return t;
     };
+    std::optional<Together> vectors;
     auto new_vector = [&](bool asked, PyObject *given, const char *what, void *&p) {
         if (!asked) return at::Tensor();
+        if (given == Py_None) {
+            if (!vectors) vectors.emplace(5, shape.d, wtype, device);
+            const at::Tensor t = vectors->next();
+            p = t.data_ptr();
+            return t;
+        }
         const at::Tensor t = given_or_new(tensor(given, what), {shape.d}, wtype, device, what);
         p = vector(t, shape.d, device, what);
         return t;
