@@ -76,14 +76,18 @@ struct Pair {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortCluster = 8;      // blocks that sort together (portable cluster size); 1 for short lists
+// Blocks that sort together: sixteen (beyond the portable cluster size) for long lists, eight for short ones, whose barriers
+// cost less.  32768 tokens accumulating 56 us, with eight 60; 65536: 84, 94; 8000: 25, 24.
+constexpr int kSortCluster = 8, kSortWide = 16, kSortWideFrom = 16384;
 // Tokens up to which places are counted instead of sorted by digits.  Accumulating: one wave of blocks (4099 tokens: 6.7 us
 // against 10.4; 5000: 12.5 against 10.6).  Beside the zero-fill, which takes longer than either and starts
 // sooner beside the sort's few blocks: 4000 tokens into 50257 rows of 1024 bf16 33.7 us in all, sorted 30.9.
 constexpr int kRankMost = 148 * 32, kRankBesideZeros = 1024;
 constexpr int kSortBits = 8;         // digit of one pass
 constexpr int kSortBins = 1 << kSortBits;
-constexpr int kZeroBlocks = 112;     // blocks that write zeros beside the sort: 15 clusters of 8 are resident at once (with 17, 32 us for 22)
+// Blocks that write zeros beside the sort: with it, the clusters that are resident at once (15 of eight, 7 of
+// sixteen; with two of eight more the last ones started when the first were done, 32 us for 22).
+constexpr int kZeroBlocks = 112, kZeroWide = 96;
 constexpr int kZeroRun = 16;         // adjacent vocabulary rows that belong to one of them
 constexpr int kZeroBits = 32 * 1024; // rows that a block keeps presence bits of at a time
 constexpr int kBatch = 8;            // tokens that a thread requests together
@@ -102,7 +106,7 @@ struct SortArgs {
     long long n, vocab, ld_grad, padding;
     long long row_bytes;  // of the gradient; its rows are zeroed where no token points
     int wide, passes;
-    int zero_blocks;    // of k_rank_tokens
+    int zero_blocks;    // 0 when accumulating
     int grad_bytes;     // bytes of a gradient element
 };
 
@@ -124,7 +128,7 @@ __device__ __forceinline__ void zero_row(char *p, long long bytes, int lane)
 }
 
 // Zeros for the rows that no token names, while other blocks sort.  Block z has the
-// vocabulary rows whose run number (row / kZeroRun) is z modulo kZeroBlocks, so that a batch that uses
+// vocabulary rows whose run number (row / kZeroRun) is z modulo their number, so that a batch that uses
 // only frequent, adjacent ids still spreads evenly.  The blocks of a cluster share the reading
 // of the token list: each reads its part and sets presence bits in the shared memory of
 // the block that has the row; then every block writes its absent rows.
@@ -132,7 +136,8 @@ __device__ void zero_absent(const SortArgs &a, unsigned *bits, const cg::cluster
 {
     const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const long long runs = ceil_div(a.vocab, kZeroRun);
-    const long long most = ceil_div(runs, kZeroBlocks);  // runs of a block
+    const int Z = a.zero_blocks;
+    const long long most = ceil_div(runs, Z);  // runs of a block
     constexpr int kRuns = kZeroBits / kZeroRun;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long part = ceil_div(a.n, blocks), from = part * rank, to = from + part < a.n ? from + part : a.n;
@@ -149,8 +154,8 @@ __device__ void zero_absent(const SortArgs &a, unsigned *bits, const cg::cluster
             }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-                const unsigned run = key[u] / kZeroRun, owner = run % kZeroBlocks;
-                const long long local = (long long)(run / kZeroBlocks) - r0;
+                const unsigned run = key[u] / kZeroRun, owner = run % (unsigned)Z;
+                const long long local = (long long)(run / (unsigned)Z) - r0;
                 if (owner / blocks != (unsigned)(z / blocks) || local < 0 || local >= here || key[u] == (unsigned)a.vocab) continue;
                 const int b = (int)local * kZeroRun + (int)(key[u] % kZeroRun);
                 atomicOr(cluster.map_shared_rank(&bits[b >> 5], owner % blocks), 1u << (b & 31));
@@ -159,7 +164,7 @@ __device__ void zero_absent(const SortArgs &a, unsigned *bits, const cg::cluster
         cluster.sync();
         for (int b = warp; b < here * kZeroRun; b += kSortWarps) {
             if (bits[b >> 5] >> (b & 31) & 1u) continue;
-            const long long row = ((r0 + b / kZeroRun) * kZeroBlocks + z) * kZeroRun + b % kZeroRun;
+            const long long row = ((r0 + b / kZeroRun) * Z + z) * kZeroRun + b % kZeroRun;
             if (row >= a.vocab) continue;
             zero_row(static_cast<char *>(a.grad) + row * a.ld_grad * a.grad_bytes, a.row_bytes, lane);
         }
@@ -692,12 +697,21 @@ adascale_status adascale_embed_grad(const adascale_embed_grad_args *g, void *cud
     a.wide = g->token_type == ADASCALE_I64;
     while ((g->vocab >> (kSortBits * a.passes)) > 0) ++a.passes;  // the largest key is vocab itself
     a.grad_bytes = eg;
-    a.zero_blocks = g->accumulate ? 0 : kZeroBlocks;
-    const bool counted = g->n_tokens <= (g->accumulate ? kRankMost : kRankBesideZeros);
-    if (counted)
+    const bool counted = g->n_tokens <= (g->accumulate ? kRankMost : kRankBesideZeros), wide = g->n_tokens >= kSortWideFrom;
+    a.zero_blocks = g->accumulate ? 0 : wide ? kZeroWide : kZeroBlocks;
+    if (counted) {
         OPS_CU(launch(k_rank_tokens, ceil_div(g->n_tokens, 32) + a.zero_blocks, kSortThreads, 0, s, a));
-    else
-        OPS_CU(launch(k_sort_tokens, kSortCluster + a.zero_blocks, kSortThreads, 0, s, a, kSortCluster));
+    } else {
+        static bool allowed[64] = {false};  // per device; threads that race ask twice
+        int dev = 0;
+        OPS_CU(cudaGetDevice(&dev));
+        if (wide && (dev < 0 || dev >= 64 || !allowed[dev])) {
+            OPS_CU(cudaFuncSetAttribute(k_sort_tokens, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+            if (dev >= 0 && dev < 64) allowed[dev] = true;
+        }
+        const int cluster = wide ? kSortWide : kSortCluster;
+        OPS_CU(launch(k_sort_tokens, cluster + a.zero_blocks, kSortThreads, 0, s, a, cluster));
+    }
     if (g->n_tokens == 0) return ADASCALE_OK;
 
     SumArgs b = {};
