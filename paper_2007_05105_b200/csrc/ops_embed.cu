@@ -520,9 +520,20 @@ __global__ void __launch_bounds__(kSumThreads, kSumBlocks) k_sum_windows(const _
 #pragma unroll
             for (int e = 0; e < V; ++e) acc[e] = 0.f;
         };
+        // bf16 rows that are added to: the old row of a run that ends kDepth entries on is asked for into L2 (32768 x 1024
+        // accumulating: 54 us for 57)
+        auto early = [&](int i) {
+            if constexpr (sizeof(GT) == 2) {
+                if (!a.accumulate || pairs[i].x == pairs[i + 1].x) return;
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<GT *>(a.grad) + (long long)pairs[i].x * a.ld_grad + (long long)c * V));
+            }
+        };
         uint4 *mine = &ring[0][threadIdx.x];
         for (int u = 0; u < kDepth; ++u) {
-            if (lo + u < hi) copy_async(mine + u * kSumThreads, row(lo + u));
+            if (lo + u < hi) {
+                copy_async(mine + u * kSumThreads, row(lo + u));
+                early(lo + u);
+            }
             copy_commit();
         }
         for (int i = lo, slot = 0; i < hi; ++i, slot = slot + 1 == kDepth ? 0 : slot + 1) {
@@ -530,7 +541,10 @@ __global__ void __launch_bounds__(kSumThreads, kSumBlocks) k_sum_windows(const _
             const uint4 x = mine[slot * kSumThreads];
             next_run(i);
             add_to<DT, V>(acc, x);
-            if (i + kDepth < hi) copy_async(mine + slot * kSumThreads, row(i + kDepth));
+            if (i + kDepth < hi) {
+                copy_async(mine + slot * kSumThreads, row(i + kDepth));
+                early(i + kDepth);
+            }
             copy_commit();
         }
     }
