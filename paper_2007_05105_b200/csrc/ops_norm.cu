@@ -6,23 +6,22 @@
 // so both directions of a row need its elements and a handful of sums over them.
 //
 // Both kernels are bound by memory: every array is read or written once, and a row's elements
-// stay in registers between the sums.  A row belongs to a group of threads with up to 32 (gradient: 16)
-// elements each; persistent groups walk over the rows, and the next row of every array
+// stay in registers between the sums.  A row belongs to a group of threads: a warp with up to 40 (gradient: 16)
+// elements a lane, which needs no barrier, or a block of as many warps as the row fills; persistent groups walk over
+// the rows.  In the gradient, and forward where it pays, the next row of every array
 // arrives in shared memory by one bulk copy each while the group works on the current one.  What had
 // to be brought down is the number of instructions: with 8 elements a thread, plain loads and the
 // kinds of matrix and row told apart at run time, a row of 1024 cost 2400 warp instructions forward and 3500 backward
 // (the SM issues at most 2100 and 3100 in the time that the row's bytes take).  Hence work on packed pairs, many
-// elements a thread, kernels compiled for the types and for rows that fill the group.
+// elements a thread, kernels compiled for the types and for how far rows fill their groups.
 #include "ops_common.cuh"
 
 namespace {
 
-constexpr int kForwardElems = 32;   // of a row per thread
-constexpr int kGradElems = 16;      // fewer: up to five column sums of each stay in registers
 constexpr int kSums = 5;            // dw_pre, db_pre, dw_post, db_post, dgate
 enum { kDwPre, kDbPre, kDwPost, kDbPost, kDgate };
 constexpr int kStages = 2;
-constexpr int kStageMost = 4096;    // widest row that is staged
+constexpr size_t kStageMost = 224 * 1024;  // bytes of stages in a block, at most
 
 struct Rows {
     char *p;
@@ -39,17 +38,35 @@ template <int T> __device__ __forceinline__ bool is_bf16(const Rows &m)
     return T == kBf16;
 }
 
-// A thread's elements are E / V sets of V adjacent ones: set j starts at column (j * group + t) * V.  V = 4 where
-// rows start on 16-byte boundaries (16 or 8 bytes an access, adjacent over the lanes), 1 otherwise.  FULL: the
-// group has exactly the row's columns.  Elements are kept as pairs.
-template <int E, int V, bool FULL> struct Place {
-    int group, t, dim;
-    __device__ __forceinline__ int column(int j) const { return (j * group + t) * V; }
-    __device__ __forceinline__ bool has(int j) const { return FULL || column(j) < dim; }
+__host__ __device__ constexpr int sure_of(int e) { return e - (e > 16 ? 8 : 4); }
+
+// A thread's elements are E / V sets of V adjacent ones: set j starts at column (j * stride + t) * V.  V = 4 where
+// rows start on 16-byte boundaries (16 or 8 bytes an access, adjacent over the lanes), 1 otherwise.  How far the group's
+// places are filled: kFull, the row has exactly as many columns; kMostly, only the last 4 (E > 16: 8) elements of a
+// thread can lie beyond the row, and the others are not asked (with all of them asked a gradient of 16800000 elements took
+// 102 us at 768 columns, 70 so); kAsk, any may.  The sets of a thread are as far apart as its group has threads; with kAsk
+// each warp has adjacent columns, so that the distance is a constant.  Elements are kept as pairs.
+enum { kAsk, kMostly, kFull };
+template <int E, int V, int FILL> struct Place {
+    static constexpr int kSure = FILL == kFull ? E : FILL == kMostly ? sure_of(E) : 0;
+    int stride, t, dim;
+    __device__ __forceinline__ int column(int j) const { return (j * stride + t) * V; }
+    __device__ __forceinline__ bool has(int j) const { return (j + 1) * V <= kSure || column(j) < dim; }
 };
 
+// Groups: a warp (any number of them in a block, each for itself), a block of a number of threads that is
+// known at compile time, or kBlock, a block of any number of warps.
+constexpr int kBlock = 0;
+template <int E, int V, int FILL, int GROUP> __device__ __forceinline__ Place<E, V, FILL> place_of(int dim)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if constexpr (GROUP == 32) return {32, lane, dim};
+    else if constexpr (FILL == kAsk) return {32, warp * (32 * E / V) + lane, dim};
+    else return {GROUP == kBlock ? (int)blockDim.x : GROUP, (int)threadIdx.x, dim};
+}
+
 // The thread's elements of the row at p; those that it does not have become `none`.
-template <int E, int V, bool FULL> __device__ __forceinline__ void read(const Place<E, V, FULL> &at, const char *p, bool bf, f2 (&x)[E / 2], float none = 0.f)
+template <int E, int V, int FILL> __device__ __forceinline__ void read(const Place<E, V, FILL> &at, const char *p, bool bf, f2 (&x)[E / 2], float none = 0.f)
 {
     if constexpr (V == 4) {
 #pragma unroll
@@ -78,12 +95,12 @@ template <int E, int V, bool FULL> __device__ __forceinline__ void read(const Pl
     }
 }
 // The thread's columns of a float32 vector.
-template <int E, int V, bool FULL> __device__ __forceinline__ void read(const Place<E, V, FULL> &at, const float *p, f2 (&x)[E / 2])
+template <int E, int V, int FILL> __device__ __forceinline__ void read(const Place<E, V, FILL> &at, const float *p, f2 (&x)[E / 2])
 {
-    read<E, V, FULL>(at, reinterpret_cast<const char *>(p), false, x);
+    read<E, V, FILL>(at, reinterpret_cast<const char *>(p), false, x);
 }
 
-template <int E, int V, bool FULL> __device__ __forceinline__ void write(const Place<E, V, FULL> &at, char *p, bool bf, const f2 (&x)[E / 2])
+template <int E, int V, int FILL> __device__ __forceinline__ void write(const Place<E, V, FILL> &at, char *p, bool bf, const f2 (&x)[E / 2])
 {
     float v[E];
 #pragma unroll
@@ -120,10 +137,12 @@ __device__ __forceinline__ float warp_sum_pair(float a, float b, int lane)
     return mine;
 }
 
-// Sums over a row's group: a warp (any number of them in a block, each for itself), or the whole
-// block, with one barrier (consecutive calls use alternate halves of the scratch).
-template <int GROUP> struct GroupSum {
-    float (*scratch)[GROUP / 32][2];  // [2][warps][2]
+__host__ __device__ constexpr int scratch_warps(int group, int most) { return group == kBlock ? (most / 32 + 3) / 4 * 4 : group / 32; }
+
+// Sums over a row's group; in a block with one barrier (consecutive calls use alternate halves of the scratch,
+// which has zeros where the block has no warp).
+template <int GROUP, int WARPS> struct GroupSum {
+    float (*scratch)[WARPS][2];  // [2]
     int turn;
 
     __device__ __forceinline__ void operator()(float &a, float &b)
@@ -136,14 +155,25 @@ template <int GROUP> struct GroupSum {
         } else {
             if ((lane & 15) == 0) scratch[turn][threadIdx.x >> 5][lane >> 4] = mine;
             __syncthreads();
-            constexpr int kPer = GROUP / 32;
-            const float2 v = *reinterpret_cast<const float2 *>(scratch[turn][lane & (kPer - 1)]);
-            a = v.x;
-            b = v.y;
+            if constexpr (GROUP != kBlock) {
+                const float2 v = *reinterpret_cast<const float2 *>(scratch[turn][lane & (WARPS - 1)]);
+                a = v.x;
+                b = v.y;
 #pragma unroll
-            for (int o = kPer / 2; o > 0; o >>= 1) {
-                a += __shfl_xor_sync(0xffffffffu, a, o);
-                b += __shfl_xor_sync(0xffffffffu, b, o);
+                for (int o = WARPS / 2; o > 0; o >>= 1) {
+                    a += __shfl_xor_sync(0xffffffffu, a, o);
+                    b += __shfl_xor_sync(0xffffffffu, b, o);
+                }
+            } else if (blockDim.x <= 128) {
+                const float4 *two = reinterpret_cast<const float4 *>(scratch[turn]);
+                const float4 p = two[0], q = two[1];
+                a = p.x + p.z + (q.x + q.z);
+                b = p.y + p.w + (q.y + q.w);
+            } else {
+                const float2 v = lane < WARPS ? *reinterpret_cast<const float2 *>(scratch[turn][lane]) : make_float2(0.f, 0.f);
+                const float sum = warp_sum_pair(v.x, v.y, lane);
+                a = __shfl_sync(0xffffffffu, sum, 0);
+                b = __shfl_sync(0xffffffffu, sum, 16);
             }
             turn ^= 1;
         }
@@ -178,12 +208,12 @@ template <int E> __device__ __forceinline__ float products(const f2 (&v)[E / 2],
     return a + b;
 }
 // v - mean; elements that the thread does not have stay 0.
-template <int E, int V, bool FULL> __device__ __forceinline__ void centre(const Place<E, V, FULL> &at, f2 (&v)[E / 2], float mean)
+template <int E, int V, int FILL> __device__ __forceinline__ void centre(const Place<E, V, FILL> &at, f2 (&v)[E / 2], float mean)
 {
     const f2 m = pack2(-mean, -mean);
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) v[i] = add2(v[i], m);
-    if constexpr (!FULL) {
+    if constexpr (FILL != kFull) {
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
             float a, b;
@@ -256,38 +286,37 @@ struct NormArgs {
     float inv_dim, res_scale, eps;
 };
 
-// Threads of a block: of its one group, or four warps that are groups of their own.
-__host__ __device__ constexpr int threads_of(int group) { return group == 32 ? 128 : group; }
-// Forward, most of a block: sixteen warps, fewer where their stages do not fit or there are few rows.
-__host__ __device__ constexpr int forward_threads(int group) { return group == 32 ? 512 : group; }
-// Blocks that an SM holds: as many as leave a thread the registers that it needs.  Gradient, 16384 x 1024 (f32
-// stream, bf16 block, layer norms, channel gate): 384 threads an SM (168 registers) 61 us, 256 (180) 68, 512 (128) 81.
-constexpr int forward_blocks(int group) { return group == 32 ? 1 : group <= 256 ? 512 / group : 1; }
-constexpr int gradient_blocks(int group) { return group <= 128 ? 384 / threads_of(group) : 1; }
+// Threads that an SM holds: as many as leave one the registers that it needs for its elements.  Gradient, 16384 x 1024
+// (f32 stream, bf16 block, layer norms, channel gate), E = 16: 384 threads (168 registers) 61 us, 512 (128) 81.  Forward,
+// E = 24: rows of 640 columns by warps, 640 threads 41 us, 512 46; of 1280 by blocks, 640 threads 54 us, 512 51.
+__host__ __device__ constexpr int forward_threads(int e, int group) { return e > 32 ? 384 : e > 24 ? 512 : e > 16 ? group == 32 ? 640 : 512 : e > 8 ? 768 : 1024; }
+__host__ __device__ constexpr int gradient_threads(int e) { return e > 12 ? 384 : e > 8 ? 512 : e > 4 ? 640 : 896; }
+constexpr int kGradientBlock = 128;  // of a block whose warps are groups of their own
 
 // Rows by bulk copies ahead of the work where both types are bf16 and a row is a warp's (16384 x 1024: 28 us against
 // 32); otherwise each row is loaded when its turn comes (f32 stream: 39 us against 42; 16384 x 2048: 74 against 83).
-template <int XT, int YT, int V> __host__ __device__ constexpr bool forward_staged(int group)
+template <int XT, int YT, int V, int GROUP> __host__ __device__ constexpr bool forward_staged()
 {
-    return V == 4 && group == 32 && XT == kBf16 && YT == kBf16;
+    return V == 4 && GROUP == 32 && XT == kBf16 && YT == kBf16;
 }
 
-template <int XT, int YT, int V, bool FULL, int GROUP, int E>
-__global__ void __launch_bounds__(forward_threads(GROUP), forward_blocks(GROUP)) k_boundary(const __grid_constant__ NormArgs a)
+template <int XT, int YT, int V, int FILL, int GROUP, int E>
+__global__ void __launch_bounds__(forward_threads(E, GROUP), 1) k_boundary(const __grid_constant__ NormArgs a)
 {
-    constexpr int kMostGroups = forward_threads(GROUP) / GROUP;
-    constexpr bool kStaged = forward_staged<XT, YT, V>(GROUP);
+    constexpr int kMostWarps = forward_threads(E, GROUP) / 32, kScratch = scratch_warps(GROUP, forward_threads(E, GROUP));
+    constexpr bool kWarp = GROUP == 32, kStaged = forward_staged<XT, YT, V, GROUP>();
     extern __shared__ __align__(128) char room[];
-    __shared__ __align__(8) float scratch[2][GROUP / 32][2];
-    __shared__ u64 full[kMostGroups][kStages];
-    const int mine = threadIdx.x / GROUP, groups = blockDim.x / GROUP;
-    const Place<E, V, FULL> at = {GROUP, (int)threadIdx.x % GROUP, a.dim};
+    __shared__ __align__(16) float scratch[2][kScratch][2];
+    __shared__ u64 full[kStaged ? kMostWarps : 1][kStages];
+    const int mine = kWarp ? threadIdx.x / 32 : 0, groups = kWarp ? blockDim.x / 32 : 1;
+    const Place<E, V, FILL> at = place_of<E, V, FILL, GROUP>(a.dim);
     const long long all = (long long)gridDim.x * groups;
-    const Stages stages = {room + a.weight_bytes + mine * kStages * a.stage_bytes, full[mine], a.stage_bytes};
-    GroupSum<GROUP> sum = {scratch, 0};
+    const Stages stages = {room + a.weight_bytes + mine * kStages * a.stage_bytes, full[kStaged ? mine : 0], a.stage_bytes};
+    GroupSum<GROUP, kScratch> sum = {scratch, 0};
+    for (int i = threadIdx.x; GROUP == kBlock && i < 4 * kScratch; i += blockDim.x) (&scratch[0][0][0])[i] = 0.f;
     long long row = (long long)blockIdx.x * groups + mine;
     if (kStaged && at.t == 0) {
-        for (int s = 0; s < kStages; ++s) mbar_init(full[mine] + s, 1);
+        for (int s = 0; s < kStages; ++s) mbar_init(stages.full + s, 1);
         mbar_publish();
     }
     group_barrier<GROUP>();
@@ -316,11 +345,11 @@ __global__ void __launch_bounds__(forward_threads(GROUP), forward_blocks(GROUP))
     for (; row < a.n; row += all) {
         const char *px = a.x.row(row), *py = a.y.row(row), *pg = a.gate.row(row);
         if constexpr (kStaged) {
-            if (!mbar_wait(full[mine] + stage, parity)) {
+            if (!mbar_wait(stages.full + stage, parity)) {
                 f2 lost[E / 2];
                 fill<E>(lost, __int_as_float(0x7fffffff));
-                write<E, V, FULL>(at, a.h.row(row), is_bf16<YT>(a.h), lost);
-                mbar_wait(full[mine] + (stage ^ 1), parity ^ (stage == 1));  // the other copy in flight
+                write<E, V, FILL>(at, a.h.row(row), is_bf16<YT>(a.h), lost);
+                mbar_wait(stages.full + (stage ^ 1), parity ^ (stage == 1));  // the other copy in flight
                 break;
             }
             px = stages.base + stage * stages.bytes;
@@ -329,30 +358,30 @@ __global__ void __launch_bounds__(forward_threads(GROUP), forward_blocks(GROUP))
         }
         f2 x[E / 2], y[E / 2], w[E / 2];
         float s;
-        read<E, V, FULL>(at, px, is_bf16<XT>(a.x), x);
+        read<E, V, FILL>(at, px, is_bf16<XT>(a.x), x);
         if (a.y.p) {
-            read<E, V, FULL>(at, py, is_bf16<YT>(a.y), y);
+            read<E, V, FILL>(at, py, is_bf16<YT>(a.y), y);
             if (a.post != ADASCALE_NORM_NONE) {
                 if (a.post == ADASCALE_NORM_LAYER) {
                     s = total<E>(y);
                     sum(s);
-                    centre<E, V, FULL>(at, y, s * a.inv_dim);
+                    centre<E, V, FILL>(at, y, s * a.inv_dim);
                 }
                 s = products<E>(y, y);
                 sum(s);
                 scale<E>(y, rsqrtf(fmaf(s, a.inv_dim, a.eps)));
-                read<E, V, FULL>(at, w_post, w);
+                read<E, V, FILL>(at, w_post, w);
                 times<E>(y, w);
                 if (b_post) {
-                    read<E, V, FULL>(at, b_post, w);
+                    read<E, V, FILL>(at, b_post, w);
                     plus<E>(y, w);
                 }
             }
             if (a.gate_kind != ADASCALE_GATE_NONE) {
                 if (a.gate_kind == ADASCALE_GATE_CHANNEL) {
-                    read<E, V, FULL>(at, channel, w);
+                    read<E, V, FILL>(at, channel, w);
                 } else {
-                    read<E, V, FULL>(at, pg, is_bf16<YT>(a.gate), w);
+                    read<E, V, FILL>(at, pg, is_bf16<YT>(a.gate), w);
                     sigmoids<E>(w);
                 }
                 times<E>(y, w);
@@ -360,7 +389,7 @@ __global__ void __launch_bounds__(forward_threads(GROUP), forward_blocks(GROUP))
             const f2 rs = pack2(a.res_scale, a.res_scale);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) x[i] = fma2(rs, y[i], x[i]);
-            write<E, V, FULL>(at, a.x_new.row(row), is_bf16<XT>(a.x_new), x);
+            write<E, V, FILL>(at, a.x_new.row(row), is_bf16<XT>(a.x_new), x);
         }
         if constexpr (kStaged) {  // everything of the stage has been read
             group_barrier<GROUP>();
@@ -371,18 +400,18 @@ __global__ void __launch_bounds__(forward_threads(GROUP), forward_blocks(GROUP))
         if (a.pre == ADASCALE_NORM_LAYER) {
             s = total<E>(x);
             sum(s);
-            centre<E, V, FULL>(at, x, s * a.inv_dim);
+            centre<E, V, FILL>(at, x, s * a.inv_dim);
         }
         s = products<E>(x, x);
         sum(s);
         scale<E>(x, rsqrtf(fmaf(s, a.inv_dim, a.eps)));
-        read<E, V, FULL>(at, w_pre, w);
+        read<E, V, FILL>(at, w_pre, w);
         times<E>(x, w);
         if (b_pre) {
-            read<E, V, FULL>(at, b_pre, w);
+            read<E, V, FILL>(at, b_pre, w);
             plus<E>(x, w);
         }
-        write<E, V, FULL>(at, a.h.row(row), is_bf16<YT>(a.h), x);
+        write<E, V, FILL>(at, a.h.row(row), is_bf16<YT>(a.h), x);
     }
 }
 
@@ -401,22 +430,23 @@ struct GradArgs {
 // warps of a block are added in order, where they are groups, and the block leaves one row of partial
 // sums.  The sums over a row come in pairs (x and y, twice; the two of each norm's gradient): four
 // barriers a row, none where a row is one warp's.
-template <int XT, int YT, int V, bool FULL, int GROUP>
-__global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_boundary_grad(const __grid_constant__ GradArgs a)
+template <int XT, int YT, int V, int FILL, int GROUP, int E, int MOST>
+__global__ void __launch_bounds__(MOST, 1) k_boundary_grad(const __grid_constant__ GradArgs a)
 {
-    constexpr int E = kGradElems, kGroups = threads_of(GROUP) / GROUP;
-    constexpr bool kStaged = V == 4 && GROUP * E <= kStageMost;
+    constexpr int kGroups = GROUP == 32 ? kGradientBlock / 32 : 1, kScratch = scratch_warps(GROUP, MOST);
+    constexpr bool kWarp = GROUP == 32, kStaged = V == 4 && XT != kAny;
     extern __shared__ __align__(128) char room[];
-    __shared__ __align__(8) float scratch[2][GROUP / 32][2];
+    __shared__ __align__(16) float scratch[2][kScratch][2];
     __shared__ u64 full[kGroups][kStages];
-    const int mine = threadIdx.x / GROUP;
-    const Place<E, V, FULL> at = {GROUP, (int)threadIdx.x % GROUP, a.dim};
+    const int mine = kWarp ? threadIdx.x / 32 : 0;
+    const Place<E, V, FILL> at = place_of<E, V, FILL, GROUP>(a.dim);
     const long long all = (long long)gridDim.x * kGroups;
     const Stages stages = {room + mine * kStages * a.stage_bytes, full[mine], a.stage_bytes};
-    GroupSum<GROUP> sum = {scratch, 0};
+    GroupSum<GROUP, kScratch> sum = {scratch, 0};
+    for (int i = threadIdx.x; GROUP == kBlock && i < 4 * kScratch; i += blockDim.x) (&scratch[0][0][0])[i] = 0.f;
     long long row = (long long)blockIdx.x * kGroups + mine;
     if (kStaged && at.t == 0) {
-        for (int s = 0; s < kStages; ++s) mbar_init(full[mine] + s, 1);
+        for (int s = 0; s < kStages; ++s) mbar_init(stages.full + s, 1);
         mbar_publish();
     }
     group_barrier<GROUP>();
@@ -436,9 +466,9 @@ __global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_b
     for (; row < a.n; row += all) {
         const char *px = a.x.row(row), *ph = a.dh.row(row), *pd = a.dx_new.row(row), *py = a.y.row(row), *pg = a.gate.row(row);
         if constexpr (kStaged) {
-            if (!mbar_wait(full[mine] + stage, parity)) {
+            if (!mbar_wait(stages.full + stage, parity)) {
                 fill<E>(acc[kDwPre], __int_as_float(0x7fffffff));
-                mbar_wait(full[mine] + (stage ^ 1), parity ^ (stage == 1));  // the other copy in flight
+                mbar_wait(stages.full + (stage ^ 1), parity ^ (stage == 1));  // the other copy in flight
                 break;
             }
             px = stages.base + stage * stages.bytes;
@@ -449,16 +479,16 @@ __global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_b
         }
         f2 x[E / 2], y[E / 2], dx[E / 2], dh[E / 2], w[E / 2];
         float s0, s1;
-        read<E, V, FULL>(at, px, is_bf16<XT>(a.x), x);
-        read<E, V, FULL>(at, ph, is_bf16<YT>(a.dh), dh);
-        if (has_y) read<E, V, FULL>(at, py, is_bf16<YT>(a.y), y);
+        read<E, V, FILL>(at, px, is_bf16<XT>(a.x), x);
+        read<E, V, FILL>(at, ph, is_bf16<YT>(a.dh), dh);
+        if (has_y) read<E, V, FILL>(at, py, is_bf16<YT>(a.y), y);
         else fill<E>(y, 0.f);
         if (centre_x || centre_y) {
             s0 = total<E>(x);
             s1 = total<E>(y);
             sum(s0, s1);
-            if (centre_x) centre<E, V, FULL>(at, x, s0 * a.inv_dim);
-            if (centre_y) centre<E, V, FULL>(at, y, s1 * a.inv_dim);
+            if (centre_x) centre<E, V, FILL>(at, x, s0 * a.inv_dim);
+            if (centre_y) centre<E, V, FILL>(at, y, s1 * a.inv_dim);
         }
         s0 = products<E>(x, x);
         s1 = products<E>(y, y);
@@ -467,7 +497,7 @@ __global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_b
 
         // dx = dx' + pre^T(dh)
         scale<E>(x, rx);
-        read<E, V, FULL>(at, a.w_pre, w);
+        read<E, V, FILL>(at, a.w_pre, w);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
             acc[kDwPre][i] = fma2(dh[i], x[i], acc[kDwPre][i]);
@@ -477,7 +507,7 @@ __global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_b
         s0 = products<E>(dh, x);
         s1 = total<E>(dh);
         sum(s0, s1);
-        if (arrives) read<E, V, FULL>(at, pd, is_bf16<XT>(a.dx_new), dx);
+        if (arrives) read<E, V, FILL>(at, pd, is_bf16<XT>(a.dx_new), dx);
         else fill<E>(dx, 0.f);
         {
             const float mean = centre_x ? s1 * a.inv_dim : 0.f;
@@ -485,7 +515,7 @@ __global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_b
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) dx[i] = fma2(r, fma2(x[i], share, add2(dh[i], minus)), dx[i]);
         }
-        write<E, V, FULL>(at, a.dx.row(row), is_bf16<XT>(a.dx), dx);
+        write<E, V, FILL>(at, a.dx.row(row), is_bf16<XT>(a.dx), dx);
 
         if (has_y) {  // gate and post; x, dh are free
             if (post) scale<E>(y, ry);
@@ -495,31 +525,31 @@ __global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_b
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) u[i] = y[i];
                 if (post) {
-                    read<E, V, FULL>(at, a.w_post, w);
+                    read<E, V, FILL>(at, a.w_post, w);
                     times<E>(u, w);
                     if (a.b_post) {
-                        read<E, V, FULL>(at, a.b_post, w);
+                        read<E, V, FILL>(at, a.b_post, w);
                         plus<E>(u, w);
                     }
                 }
                 times<E>(u, dx);  // gradient of the gate
                 if (a.gate_kind == ADASCALE_GATE_SIGMOID) {
-                    read<E, V, FULL>(at, pg, is_bf16<YT>(a.gate), w);
+                    read<E, V, FILL>(at, pg, is_bf16<YT>(a.gate), w);
                     sigmoids<E>(w);
                     if (a.dgate.p) {
                         const f2 one = pack2(1.f, 1.f), minus_one = pack2(-1.f, -1.f);
 #pragma unroll
                         for (int i = 0; i < E / 2; ++i) u[i] = mul2(mul2(u[i], w[i]), fma2(w[i], minus_one, one));
-                        write<E, V, FULL>(at, a.dgate.row(row), is_bf16<YT>(a.dgate), u);
+                        write<E, V, FILL>(at, a.dgate.row(row), is_bf16<YT>(a.dgate), u);
                     }
                 } else {
-                    read<E, V, FULL>(at, a.gate_channel, w);
+                    read<E, V, FILL>(at, a.gate_channel, w);
                     plus<E>(acc[kDgate], u);
                 }
                 times<E>(dx, w);
             }
             if (post) {
-                read<E, V, FULL>(at, a.w_post, w);
+                read<E, V, FILL>(at, a.w_post, w);
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) {
                     acc[kDwPost][i] = fma2(dx[i], y[i], acc[kDwPost][i]);
@@ -534,7 +564,7 @@ __global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_b
 #pragma unroll
                 for (int i = 0; i < E / 2; ++i) dx[i] = mul2(r, fma2(y[i], share, add2(dx[i], minus)));
             }
-            if (a.dy.p) write<E, V, FULL>(at, a.dy.row(row), is_bf16<YT>(a.dy), dx);
+            if (a.dy.p) write<E, V, FILL>(at, a.dy.row(row), is_bf16<YT>(a.dy), dx);
         }
         if constexpr (kStaged) {
             group_barrier<GROUP>();
@@ -550,12 +580,12 @@ __global__ void __launch_bounds__(threads_of(GROUP), gradient_blocks(GROUP)) k_b
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
         if constexpr (kGroups == 1) {
-            write<E, V, FULL>(at, to + (size_t)k * a.ld_partial * 4, false, acc[k]);
+            write<E, V, FILL>(at, to + (size_t)k * a.ld_partial * 4, false, acc[k]);
         } else {
             __syncthreads();
-            write<E, V, FULL>(at, reinterpret_cast<char *>(gather + mine * a.ld_partial), false, acc[k]);
+            write<E, V, FILL>(at, reinterpret_cast<char *>(gather + mine * a.ld_partial), false, acc[k]);
             __syncthreads();
-            for (int c = threadIdx.x; c < a.dim; c += threads_of(GROUP)) {
+            for (int c = threadIdx.x; c < a.dim; c += kGradientBlock) {
                 float s = gather[c];
                 for (int q = 1; q < kGroups; ++q) s += gather[q * a.ld_partial + c];
                 reinterpret_cast<float *>(to)[k * a.ld_partial + c] = s;
@@ -606,13 +636,25 @@ __global__ void __launch_bounds__(kColumnWarps * 32) k_columns(const __grid_cons
 
 constexpr int kMaxPartials = 148 * 16;  // blocks of a gradient launch, at most
 
-// Threads per row for `per` elements each.
-int group_of(long long dim, int per)
+// Elements a thread and threads of a row's group.  A warp has a row as long as its elements fit (1280 columns forward,
+// bf16: 31 us, by a block 45; with 48 elements a lane 1536 columns of f32 took 49 us, by a block 46); beyond that a
+// block of warps, from a list of E and most threads, that leaves the fewest places empty, of equals the
+// one with more elements a thread.
+struct Split {
+    int e, group;
+};
+template <int N, int M> Split split_of(long long dim, const int (&by_warp)[N], const Split (&by_block)[M])
 {
-    int g = 32;
-    while ((long long)g * per < dim) g *= 2;
-    return g;
+    for (int e : by_warp)
+        if (32LL * e >= dim) return {e, 32};
+    Split best = {0, 0};
+    for (const Split b : by_block) {
+        const int g = (int)ceil_div(dim, 32 * b.e) * 32;
+        if ((long long)sure_of(b.e) * g <= dim && g <= b.group && (!best.e || b.e * g <= best.e * best.group)) best = {b.e, g};
+    }
+    return best;
 }
+bool power_of_two(long long v) { return v > 0 && !(v & (v - 1)); }
 
 bool norm_kind(int k, bool none_too) { return k == ADASCALE_NORM_RMS || k == ADASCALE_NORM_LAYER || (none_too && k == ADASCALE_NORM_NONE); }
 
@@ -629,76 +671,130 @@ long long resident(int sms, int most, size_t smem)
     return (long long)sms * (fit < most ? (fit < 1 ? 1 : fit) : most);
 }
 
-// Where a row is a warp's: few rows, blocks of four warps that read the vectors where they are; many rows, blocks of
-// sixteen with a copy of the vectors in shared memory (in L1 they are evicted between rows: 42 us for 39).
-template <int XT, int YT, int V, bool FULL, int GROUP, int E> cudaError_t launch_boundary(NormArgs a, int sms, cudaStream_t s)
+// Where a row is a warp's: few rows, blocks of four warps that read the vectors where they are; many rows, blocks that
+// fill an SM with a copy of the vectors in shared memory (in L1 they are evicted between rows: 42 us for 39).
+template <int XT, int YT, int V, int FILL, int GROUP, int E> cudaError_t launch_boundary(NormArgs a, int group, int sms, cudaStream_t s)
 {
+    constexpr bool kWarp = GROUP == 32;
     const int vectors = (a.w_post != nullptr) + (a.b_post != nullptr) + (a.gate_channel != nullptr) + 1 + (a.b_pre != nullptr);
     const unsigned copies = (unsigned)(vectors * ((a.dim + 3) / 4 * 4) * sizeof(float));
-    const size_t stages = forward_staged<XT, YT, V>(GROUP) ? (size_t)kStages * a.stage_bytes : 0;  // of a group
-    int groups = GROUP == 32 ? 4 : 1;
-    if (GROUP == 32 && a.n >= 64LL * sms) {
-        groups = forward_threads(GROUP) / GROUP;
+    const size_t stages = forward_staged<XT, YT, V, GROUP>() ? (size_t)kStages * a.stage_bytes : 0;  // of a group
+    int groups = kWarp ? 4 : 1;
+    if (kWarp && a.n >= forward_threads(E, GROUP) / 8LL * sms) {
+        groups = forward_threads(E, GROUP) / 32;
         a.weight_bytes = copies;
     }
     const size_t smem = groups * stages + a.weight_bytes;
-    const long long need = ceil_div(a.n, groups), most = resident(sms, 512 / (groups * GROUP) > 1 ? 512 / (groups * GROUP) : 1, smem);
+    const long long need = ceil_div(a.n, groups), most = resident(sms, forward_threads(E, GROUP) / (groups * group), smem);
     static int known[64] = {0};
-    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary<XT, YT, V, FULL, GROUP, E>), smem, known);
-    return e != cudaSuccess ? e : launch(k_boundary<XT, YT, V, FULL, GROUP, E>, need < most ? need : most, groups * GROUP, smem, s, a);
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary<XT, YT, V, FILL, GROUP, E>), smem, known);
+    return e != cudaSuccess ? e : launch(k_boundary<XT, YT, V, FILL, GROUP, E>, need < most ? need : most, groups * group, smem, s, a);
 }
-template <int XT, int YT, int V, bool FULL> cudaError_t launch_boundary(const NormArgs &a, int group, int per, int sms, cudaStream_t s)
+template <int XT, int YT, int V, int FILL> cudaError_t launch_by_warp(const NormArgs &a, int e, int sms, cudaStream_t s)
+{
+    switch (e) {
+    case 4: return launch_boundary<XT, YT, V, FILL, 32, 4>(a, 32, sms, s);
+    case 8: return launch_boundary<XT, YT, V, FILL, 32, 8>(a, 32, sms, s);
+    case 12: return launch_boundary<XT, YT, V, FILL, 32, 12>(a, 32, sms, s);
+    case 16: return launch_boundary<XT, YT, V, FILL, 32, 16>(a, 32, sms, s);
+    case 24: return launch_boundary<XT, YT, V, FILL, 32, 24>(a, 32, sms, s);
+    case 40: return launch_boundary<XT, YT, V, FILL, 32, 40>(a, 32, sms, s);
+    }
+    return launch_boundary<XT, YT, V, FILL, 32, 32>(a, 32, sms, s);
+}
+// Rows that fill a power of two: the group's size is a constant (2048 columns 41 us, with kBlock 48).
+template <int XT, int YT> cudaError_t launch_by_power(const NormArgs &a, int group, int sms, cudaStream_t s)
 {
     switch (group) {
-    case 32:
-        if (per == 8) return launch_boundary<XT, YT, V, FULL, 32, 8>(a, sms, s);
-        return per == 16 ? launch_boundary<XT, YT, V, FULL, 32, 16>(a, sms, s) : launch_boundary<XT, YT, V, FULL, 32, 32>(a, sms, s);
-    case 64: return launch_boundary<XT, YT, V, FULL, 64, 32>(a, sms, s);
-    case 128: return launch_boundary<XT, YT, V, FULL, 128, 32>(a, sms, s);
-    case 256: return launch_boundary<kAny, kAny, V, FULL, 256, 32>(a, sms, s);
+    case 64: return launch_boundary<XT, YT, 4, kFull, 64, 32>(a, group, sms, s);
+    case 128: return launch_boundary<XT, YT, 4, kFull, 128, 32>(a, group, sms, s);
+    case 256: return launch_boundary<XT, YT, 4, kFull, 256, 32>(a, group, sms, s);
     }
-    return launch_boundary<kAny, kAny, V, FULL, 512, 32>(a, sms, s);
+    return launch_boundary<XT, YT, 4, kFull, 512, 32>(a, group, sms, s);
+}
+template <int XT, int YT, int FILL> cudaError_t launch_by_block(const NormArgs &a, Split p, int sms, cudaStream_t s)
+{
+    return p.e == 24 ? launch_boundary<XT, YT, 4, FILL, kBlock, 24>(a, p.group, sms, s) : launch_boundary<XT, YT, 4, FILL, kBlock, 32>(a, p.group, sms, s);
 }
 template <int XT, int YT> cudaError_t launch_boundary(const NormArgs &a, bool vec, int sms, cudaStream_t s)
 {
-    const int per = a.dim <= 256 ? 8 : a.dim <= 512 ? 16 : kForwardElems, group = group_of(a.dim, per);
-    if (!vec) return launch_boundary<XT, YT, 1, false>(a, group, per, sms, s);
-    return group * per == a.dim ? launch_boundary<XT, YT, 4, true>(a, group, per, sms, s) : launch_boundary<XT, YT, 4, false>(a, group, per, sms, s);
+    const Split p = split_of(a.dim, {4, 8, 12, 16, 24, 32, 40}, {{24, 512}, {32, 512}});
+    const bool full = p.group * p.e == a.dim;
+    if (p.group == 32) {
+        if (!vec) return launch_by_warp<XT, YT, 1, kMostly>(a, p.e, sms, s);
+        return full ? launch_by_warp<XT, YT, 4, kFull>(a, p.e, sms, s) : launch_by_warp<XT, YT, 4, kMostly>(a, p.e, sms, s);
+    }
+    if (!vec) return launch_boundary<XT, YT, 1, kAsk, kBlock, 32>(a, (int)ceil_div(a.dim, 1024) * 32, sms, s);
+    if (power_of_two(a.dim)) return launch_by_power<XT, YT>(a, a.dim / 32, sms, s);
+    return full ? launch_by_block<XT, YT, kFull>(a, p, sms, s) : launch_by_block<XT, YT, kMostly>(a, p, sms, s);
 }
 
-template <int XT, int YT, int V, bool FULL, int GROUP> cudaError_t launch_grad(const GradArgs &a, int sms, cudaStream_t s, int &partials)
+template <int XT, int YT, int V, int FILL, int GROUP, int E, int MOST>
+cudaError_t launch_grad(const GradArgs &a, int group, int sms, cudaStream_t s, int &partials)
 {
-    constexpr int kGroups = threads_of(GROUP) / GROUP;
-    constexpr bool kStaged = V == 4 && GROUP * kGradElems <= kStageMost;
+    constexpr int kGroups = GROUP == 32 ? kGradientBlock / 32 : 1;
+    constexpr bool kStaged = V == 4 && XT != kAny;
+    const int threads = kGroups * group;
     const long long need = ceil_div(a.n, kGroups);
     size_t smem = kStaged ? (size_t)kGroups * kStages * a.stage_bytes : 0;
     const size_t gather = (size_t)kGroups * a.ld_partial * sizeof(float);
     if (kGroups > 1 && smem < gather) smem = gather;
-    long long blocks = resident(sms, gradient_blocks(GROUP), smem);
+    long long blocks = resident(sms, MOST / threads, smem);
     if (blocks > kMaxPartials) blocks = kMaxPartials;
     if (blocks > need) blocks = need;
     partials = (int)blocks;
     static int known[64] = {0};
-    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary_grad<XT, YT, V, FULL, GROUP>), smem, known);
-    return e != cudaSuccess ? e : launch(k_boundary_grad<XT, YT, V, FULL, GROUP>, blocks, threads_of(GROUP), smem, s, a);
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary_grad<XT, YT, V, FILL, GROUP, E, MOST>), smem, known);
+    return e != cudaSuccess ? e : launch(k_boundary_grad<XT, YT, V, FILL, GROUP, E, MOST>, blocks, threads, smem, s, a);
 }
-template <int XT, int YT, int V, bool FULL> cudaError_t launch_grad(const GradArgs &a, int group, int sms, cudaStream_t s, int &partials)
+template <int XT, int YT, int V, int FILL> cudaError_t launch_by_warp(const GradArgs &a, int e, int sms, cudaStream_t s, int &partials)
+{
+    switch (e) {
+    case 4: return launch_grad<XT, YT, V, FILL, 32, 4, gradient_threads(4)>(a, 32, sms, s, partials);
+    case 8: return launch_grad<XT, YT, V, FILL, 32, 8, gradient_threads(8)>(a, 32, sms, s, partials);
+    case 12: return launch_grad<XT, YT, V, FILL, 32, 12, gradient_threads(12)>(a, 32, sms, s, partials);
+    }
+    return launch_grad<XT, YT, V, FILL, 32, 16, 384>(a, 32, sms, s, partials);
+}
+template <int XT, int YT> cudaError_t launch_by_power(const GradArgs &a, int group, int sms, cudaStream_t s, int &partials)
 {
     switch (group) {
-    case 32: return launch_grad<XT, YT, V, FULL, 32>(a, sms, s, partials);
-    case 64: return launch_grad<XT, YT, V, FULL, 64>(a, sms, s, partials);
-    case 128: return launch_grad<XT, YT, V, FULL, 128>(a, sms, s, partials);
-    case 256: return launch_grad<XT, YT, V, FULL, 256>(a, sms, s, partials);
-    case 512: return launch_grad<kAny, kAny, V, FULL, 512>(a, sms, s, partials);
+    case 64: return launch_grad<XT, YT, 4, kFull, 64, 16, 384>(a, group, sms, s, partials);
+    case 128: return launch_grad<XT, YT, 4, kFull, 128, 16, 384>(a, group, sms, s, partials);
+    case 256: return launch_grad<XT, YT, 4, kFull, 256, 16, 256>(a, group, sms, s, partials);
     }
-    return launch_grad<kAny, kAny, V, FULL, 1024>(a, sms, s, partials);
+    return launch_grad<XT, YT, 4, kFull, 512, 16, 512>(a, group, sms, s, partials);
+}
+// Rows that are too wide for stages: one kernel for all types.
+template <int V> cudaError_t launch_wide(const GradArgs &a, int group, int sms, cudaStream_t s, int &partials)
+{
+    if constexpr (V == 4)
+        if (group <= 512) return launch_grad<kAny, kAny, V, kAsk, kBlock, 16, 512>(a, group, sms, s, partials);
+    return launch_grad<kAny, kAny, V, kAsk, kBlock, 16, 1024>(a, group, sms, s, partials);
+}
+template <int XT, int YT, int FILL> cudaError_t launch_by_block(const GradArgs &a, Split p, int sms, cudaStream_t s, int &partials)
+{
+    if (p.e == 12) return launch_grad<XT, YT, 4, FILL, kBlock, 12, 384>(a, p.group, sms, s, partials);
+    return p.group <= 384 ? launch_grad<XT, YT, 4, FILL, kBlock, 16, 384>(a, p.group, sms, s, partials)
+                          : launch_grad<XT, YT, 4, FILL, kBlock, 16, 512>(a, p.group, sms, s, partials);
 }
 template <int XT, int YT> cudaError_t launch_grad(const GradArgs &a, bool vec, int sms, cudaStream_t s, int &partials)
 {
-    const int group = group_of(a.dim, kGradElems);
-    if (!vec) return launch_grad<XT, YT, 1, false>(a, group, sms, s, partials);
-    return group * kGradElems == a.dim ? launch_grad<XT, YT, 4, true>(a, group, sms, s, partials)
-                                       : launch_grad<XT, YT, 4, false>(a, group, sms, s, partials);
+    const Split p = split_of(a.dim, {4, 8, 12, 16}, {{12, 384}, {16, 512}});
+    const bool full = p.group * p.e == a.dim;
+    if (p.group == 32) {
+        if (!vec) return launch_by_warp<XT, YT, 1, kMostly>(a, p.e, sms, s, partials);
+        return full ? launch_by_warp<XT, YT, 4, kFull>(a, p.e, sms, s, partials) : launch_by_warp<XT, YT, 4, kMostly>(a, p.e, sms, s, partials);
+    }
+    const int group = (int)ceil_div(a.dim, 512) * 32;
+    if (!vec) {
+        if (group <= 384) return launch_grad<XT, YT, 1, kAsk, kBlock, 16, 384>(a, group, sms, s, partials);
+        if (group <= 512) return launch_grad<XT, YT, 1, kAsk, kBlock, 16, 512>(a, group, sms, s, partials);
+        return launch_wide<1>(a, group, sms, s, partials);
+    }
+    if (!p.group || kStages * (size_t)a.stage_bytes > kStageMost) return launch_wide<4>(a, group, sms, s, partials);
+    if (power_of_two(a.dim)) return launch_by_power<XT, YT>(a, a.dim / 16, sms, s, partials);
+    return full ? launch_by_block<XT, YT, kFull>(a, p, sms, s, partials) : launch_by_block<XT, YT, kMostly>(a, p, sms, s, partials);
 }
 
 }  // namespace
@@ -746,7 +842,7 @@ adascale_status adascale_residual_norm(const adascale_residual_norm_args *g, voi
     a.eps = g->eps;
     const long long n = g->n_rows;
     // four elements an access; bulk copies, where the kernel for the types uses them, want 16 bytes
-    const bool bulk = forward_staged<kBf16, kBf16, 4>(32) && ex == 2 && ey == 2;
+    const bool bulk = ex == 2 && ey == 2 && g->dim <= 1024;
     const int bx = bulk ? 16 : 4 * ex, by = bulk ? 16 : 4 * ey;
     const bool vec = g->dim % (bulk ? 8 : 4) == 0 && rows_on(g->x, g->ld_x, n, ex, bx) && rows_on(g->h, g->ld_h, n, ey, by) && on(a.w_pre, 16) &&
                      on(a.b_pre, 16) && (!g->y || (rows_on(g->y, g->ld_y, n, ey, by) && rows_on(g->x_new, g->ld_x_new, n, ex, bx))) &&
@@ -815,7 +911,7 @@ adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_ar
         a.w_pre = g->w_pre;
         a.partial = static_cast<float *>(g->workspace);
         a.n = g->n_rows;
-            a.dim = (int)g->dim;
+        a.dim = (int)g->dim;
         a.ld_partial = ld_partial;
         a.post = g->post;
         a.pre = g->pre;

@@ -506,6 +506,15 @@ def test_boundary_and_its_gradient(pre, post, gate, n, d, x_t, y_t):
             check(got.dy, du, C * du_mag + du.abs() * rounding(y_t), "dy")
 
 
+@pytest.mark.parametrize("x_t,y_t", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("n,d", [(5000, 72), (3000, 384), (2500, 640), (1500, 768), (1100, 1280), (700, 1536), (700, 2144), (330, 4352),
+                                 (160, 4800), (160, 6144), (1700, 333), (1500, 771), (900, 1279), (450, 2049), (170, 4099),
+                                 (160, 8191), (4, 9000), (4, 9001), (3, 12000)])
+@pytest.mark.parametrize("pre,post,gate", [("rms", "rms", "none"), ("layer", "layer", "channel"), ("rms", "layer", "element")])
+def test_boundary_of_other_widths(pre, post, gate, n, d, x_t, y_t):
+    test_boundary_and_its_gradient(pre, post, gate, n, d, x_t, y_t)
+
+
 @pytest.mark.parametrize("pad,shift", [(8, 8), (1, 3)])
 @pytest.mark.parametrize("d", [64, 1000, 2600])
 def test_boundary_strides_places_and_slots(d, pad, shift):
