@@ -462,31 +462,33 @@ __global__ void __launch_bounds__(kThreads, GRAD ? kBlocks : 2 * kBlocks) k_dist
 // Rows kept in shared memory
 // ---------------------------------------------------------------------------------------------
 // The kernel above reads a row twice, the second time from L2, and a block does nothing else while a
-// row's first pieces or its sums are on their way.  Here a row is read once: one block per SM (or a cluster of
+// row's first pieces or its sums are on their way.  Here a row is read once: a block (or a cluster of
 // them for rows that do not fit one) keeps it in a ring of shared-memory slots.  Five jobs run
 // side by side and hand over through mbarriers:
 //   loader    one thread: bulk copies of the next row's pieces into slots as they become free
-//   lists     four warps, rows ahead, each its own: weight, label, the teacher's list turned into q
-//   workers   sixteen warps: maximum and sums as the pieces arrive; then the gradient of every entry, over the row in its slots
+//   lists     two or four warps, rows ahead, each its own: weight, label, the teacher's list turned into q
+//   workers   four, eight or sixteen warps: maximum and sums as the pieces arrive; then the gradient of every entry, over the row in its slots
 //   storer    one warp: the named entries' whole values into the slots, bulk copies out, slots back to the loader; the row's loss
 // Every wait is bounded; a job that gives up leaves NaN as the row's loss and ends.
 constexpr int kStagedMaxK = 128;  // list entries: a lists' warp has a few rows' time for them
 constexpr int kPiecesEach = 2;    // 16-byte pieces of a slot per worker thread
 
-// Two shapes.  Eight worker warps and two blocks per SM, where the ring takes a whole row: while
+// Three shapes.  Four worker warps and four blocks per SM for short rows, whose time is the jobs' latency: more rows are
+// on their way, and the jobs may be eight rows apart (8192 x 4000 bf16, K = 16: 55 us; eight warps 99; four rows apart 59,
+// two 66; three blocks of fifteen slots 72).  Eight worker warps and two blocks per SM, where the ring takes a whole row: while
 // one block joins its sums or waits for its row the other computes (323 us on 8192 x 50257 bf16, T = 2; one block of sixteen
 // 360 before the forms of exps(), two blocks that share rows with another SM 420).  Sixteen and one block for longer rows, whose
 // parts fill two thirds of the ring and leave the rest to the next row (2048 x 32768 f32: 93 us).
 template <int WORKERS> struct Shape {
     static constexpr int kBlocks = 16 / WORKERS;                    // per SM
-    static constexpr int kListWarps = WORKERS / 4;
+    static constexpr int kListWarps = WORKERS == 16 ? 4 : 2;
     static constexpr int kInfos = WORKERS == 8 ? 2 : 8;             // rows that the jobs may be apart: a power of two, a multiple of kListWarps
     static constexpr int kWorkerThreads = WORKERS * 32;
     static constexpr int kThreads = kWorkerThreads + (kListWarps + 2) * 32;
     static constexpr int kSlotPieces = kWorkerThreads * kPiecesEach;
     static constexpr int kSlotBytes = kSlotPieces * 16;
-    static constexpr int kSlots = WORKERS == 8 ? 13 : 12;
-    static constexpr int kPartPieces = (WORKERS == 8 ? 13 : 8) * kSlotPieces;  // of a row that one block takes, at most
+    static constexpr int kSlots = WORKERS == 4 ? 9 : WORKERS == 8 ? 13 : 12;
+    static constexpr int kPartPieces = (WORKERS == 16 ? 8 : kSlots) * kSlotPieces;  // of a row that one block takes, at most
 };
 constexpr float kHeadroom = 40.f;                       // powers of two that an entry may exceed the reference by
 
@@ -500,6 +502,7 @@ struct RowInfo {
     float q[kStagedMaxK];     // 0: not valid
     float mass[kStagedMaxK];  // q of all entries with this id, at the first of them; < 0 at the others
     float zk[kStagedMaxK];
+    float loose[16];          // logits before and after the aligned pieces
 };
 
 template <int WORKERS> struct StagedShared {
@@ -643,6 +646,8 @@ __global__ void __launch_bounds__(Shape<kWorkers>::kThreads, Shape<kWorkers>::kB
                 if (id[u] >= 0) top = fmaxf(top, r.t[u]);
             }
             const float z_label = r.weight != 0.f && label >= 0 ? to_f32(z[label]) : 0.f;
+            const Part p = part_of(row);
+            const float z_loose = r.weight != 0.f && lane < loose_of(p) ? to_f32(z[loose_at(p, lane)]) : 0.f;
             any = __any_sync(0xffffffffu, any);
             top = warp_max(top);
             float sum = 0.f;
@@ -695,6 +700,7 @@ __global__ void __launch_bounds__(Shape<kWorkers>::kThreads, Shape<kWorkers>::kB
             }
 #pragma unroll
             for (int u = 0; u < kMine; ++u) f.mass[lane + 32 * u] = mass[u];
+            if (lane < 16) f.loose[lane] = z_loose;
             float ref = label >= 0 ? z_label : -FLT_MAX;
 #pragma unroll
             for (int u = 0; u < kMine; ++u)
@@ -723,7 +729,7 @@ __global__ void __launch_bounds__(Shape<kWorkers>::kThreads, Shape<kWorkers>::kB
                 const Part p = part_of(row);
                 ZT *dz = static_cast<ZT *>(a.dz) + row * a.ld_dz;
                 const int loose = loose_of(p);
-                const float z_loose = lane < loose ? to_f32(p.z[loose_at(p, lane)]) : 0.f;
+                const float z_loose = lane < loose ? f.loose[lane] : 0.f;
                 ok = mbar_wait(sh.stats_full + b, (unsigned)i / kInfos & 1);
                 const float m = f.m, kT = f.kT, k1 = f.k1, aT = f.aT, b1 = f.b1;
                 auto slope = [&](float x) {
@@ -841,7 +847,7 @@ __global__ void __launch_bounds__(Shape<kWorkers>::kThreads, Shape<kWorkers>::kB
             const float ref = f.ref;
             run.m = ref;
             const bool loose = tid < loose_of(p);
-            const float z_loose = loose ? to_f32(p.z[loose_at(p, tid)]) : 0.f;
+            const float z_loose = loose ? f.loose[tid] : 0.f;
             const int mine = p.v1 - p.v0;  // pieces
             bool ok = true;
             for (int c = 0; c < p.pieces; ++c, advance()) {
@@ -1001,12 +1007,12 @@ template <typename ZT, int WORKERS> cudaError_t launch_staged(const RowArgs &a, 
 
 // Rows in shared memory where a gradient is asked for, its rows lie as the logits' do and the lists are
 // not long; and where it measured faster than reading them twice (us; staged, twice):
-//   rows, 50257 bf16: 900: 50, 51; 1200: 61, 68; 450: 33, 27.  32768 f32: 900: 50, 57; 450: 31, 28
-//   length, 8192 rows bf16: 8000: 128, 161; 4000: 110, 126; 2048 rows f32: 4000: 30, 32; 2000: 26, 22
+//   rows, 50257 bf16: 900: 50, 51; 1200: 61, 68; 450: 33, 27.  32768 f32: 900: 50, 57; 450: 31, 28.  1000 bf16: 1200: 12, 14; 600: 10, 10; 300: 9, 6
+//   length, 8192 rows bf16: 8000: 80, 161; 520: 42, 57; 200: 42, 56
 //   blocks that share a row: two: 177, 191 (2048 x 50257 f32); four: 620, 464 (2048 x 120000 f32)
 //   two evaluations an entry (T = 1.3): bf16 472, 441; f32 98, 117
 constexpr int kStagedRows = 6;     // per SM
-constexpr int kStagedLeast = 512;  // pieces of a row
+constexpr int kStagedLeast = 16;   // pieces of a row
 constexpr int kStagedParts = 2;
 template <typename ZT> bool staged(RowArgs a, int form, int sms, cudaStream_t s, cudaError_t &e)
 {
@@ -1014,6 +1020,10 @@ template <typename ZT> bool staged(RowArgs a, int form, int sms, cudaStream_t s,
     if (!a.dz || !a.aligned_out || a.k > kStagedMaxK || a.n < (long long)sms * kStagedRows || pieces < kStagedLeast ||
         pieces > (long long)kStagedParts * Shape<16>::kPartPieces || (form == kAnyT && sizeof(ZT) == 2))
         return false;
+    if (pieces <= Shape<4>::kPartPieces) {
+        e = launch_staged<ZT, 4>(a, form, 1, sms, s);
+        return true;
+    }
     if (pieces <= Shape<8>::kPartPieces) {
         e = launch_staged<ZT, 8>(a, form, 1, sms, s);
         return true;

@@ -711,7 +711,7 @@ def test_distill_many_long_rows(n, vocab, k, T, alpha, beta, dtype):
     z[11] = LOWEST[dtype]
     ids[13], labels[13] = -1, -100
     weight[[5, 9, 11, 13]] = 1.0
-    ids[17] = ids[17, 0]  # one id all over
+    ids[17] = ids[17, 0].clone()  # one id all over
     labels[18] = ids[18, 0]
     labels[[19, 20]] = torch.tensor([0, vocab - 1], device=DEV)
     got = ops.distill(z, t, ids, labels=labels, T=T, alpha=alpha, beta=beta, row_weight=weight)
@@ -728,7 +728,14 @@ def test_distill_many_long_rows(n, vocab, k, T, alpha, beta, dtype):
     assert torch.equal(place, got.dlogits)
 
 
-@pytest.mark.parametrize("dtype,vocab", [(BF16, 33001), (F32, 30001), (F32, 40001)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,alpha,beta", [(1.0, 0.3, 0.7), (2.0, 0.5, 0.5), (1.5, 0.9, 0.1), (1.3, 0.5, 0.5), (4.0, 1.0, 0.0)])
+@pytest.mark.parametrize("n,vocab,k", [(3000, 140, 5), (2600, 1000, 128), (2500, 5421, 50), (1300, 9001, 1), (900, 18433, 20)])
+def test_distill_many_short_rows(n, vocab, k, T, alpha, beta, dtype):
+    test_distill_many_long_rows(n, vocab, k, T, alpha, beta, dtype)
+
+
+@pytest.mark.parametrize("dtype,vocab", [(BF16, 33001), (F32, 30001), (F32, 40001), (BF16, 3001), (F32, 1001)])
 def test_distill_many_long_rows_most_of_them_masked(dtype, vocab):
     """Rows that are skipped between rows that are not; NaN in what is skipped."""
     n, k = 900, 9
