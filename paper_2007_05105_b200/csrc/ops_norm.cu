@@ -654,6 +654,7 @@ template <int N, int M> Split split_of(long long dim, const int (&by_warp)[N], c
     }
     return best;
 }
+Split forward_split(long long dim) { return split_of(dim, {4, 8, 12, 16, 24, 32, 40}, {{24, 512}, {32, 512}}); }
 bool power_of_two(long long v) { return v > 0 && !(v & (v - 1)); }
 
 bool norm_kind(int k, bool none_too) { return k == ADASCALE_NORM_RMS || k == ADASCALE_NORM_LAYER || (none_too && k == ADASCALE_NORM_NONE); }
@@ -718,7 +719,7 @@ template <int XT, int YT, int FILL> cudaError_t launch_by_block(const NormArgs &
 }
 template <int XT, int YT> cudaError_t launch_boundary(const NormArgs &a, bool vec, int sms, cudaStream_t s)
 {
-    const Split p = split_of(a.dim, {4, 8, 12, 16, 24, 32, 40}, {{24, 512}, {32, 512}});
+    const Split p = forward_split(a.dim);
     const bool full = p.group * p.e == a.dim;
     if (p.group == 32) {
         if (!vec) return launch_by_warp<XT, YT, 1, kMostly>(a, p.e, sms, s);
@@ -845,8 +846,8 @@ adascale_status adascale_residual_norm(const adascale_residual_norm_args *g, voi
     a.res_scale = g->res_scale;
     a.eps = g->eps;
     const long long n = g->n_rows;
-    // four elements an access; bulk copies, where the kernel for the types uses them, want 16 bytes
-    const bool bulk = ex == 2 && ey == 2 && g->dim <= 1024;
+    // four elements an access; bulk copies want 16 bytes: forward_staged() for the types and the group that the width gets
+    const bool bulk = ex == 2 && ey == 2 && forward_split(g->dim).group == 32;
     const int bx = bulk ? 16 : 4 * ex, by = bulk ? 16 : 4 * ey;
     const bool vec = g->dim % (bulk ? 8 : 4) == 0 && rows_on(g->x, g->ld_x, n, ex, bx) && rows_on(g->h, g->ld_h, n, ey, by) && on(a.w_pre, 16) &&
                      on(a.b_pre, 16) && (!g->y || (rows_on(g->y, g->ld_y, n, ey, by) && rows_on(g->x_new, g->ld_x_new, n, ex, bx))) &&

@@ -1,0 +1,54 @@
+"""The language-model operators at the edges of what their kernels take: alignments at which one kernel hands over to another,
+batches that are mostly padding, arguments that are refused.  Tolerances and helpers are those of test_gpu_ops.py."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("needs a CUDA device", allow_module_level=True)
+
+import test_gpu_ops as T  # noqa: E402
+from paper_2007_05105_b200 import ops  # noqa: E402
+
+DEV, F32, BF16, U = T.DEV, T.F32, T.BF16, T.U
+
+
+# --------------------------------------------------------------------------
+# block boundary, bf16 on both sides: rows on 16 bytes go through bulk copies, others may not
+# --------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("pre,post,gate", [("rms", None, "none"), ("layer", "layer", "channel"), ("rms", "layer", "element")])
+@pytest.mark.parametrize("n,d", [(6, 1020), (6, 1024), (6, 1028), (6, 1032), (6, 1100), (6, 1276), (6, 1280), (6, 1284), (7200, 1028), (7200, 1280)])
+def test_boundary_widths_around_the_widest_row_of_a_warp(pre, post, gate, n, d):
+    """n = 7200: blocks that fill an SM and keep the vectors in shared memory."""
+    T.test_boundary_and_its_gradient(pre, post, gate, n, d, BF16, BF16)
+
+
+@pytest.mark.parametrize("pad,shift", [(0, 4), (4, 0), (4, 4), (8, 4), (8, 8), (1, 3)])
+@pytest.mark.parametrize("d", [72, 512, 1024, 1028, 1032, 1100, 1276, 1280, 1536])
+def test_boundary_bf16_strides_shifts_and_places(d, pad, shift):
+    n = 21
+    for pre, post, kind in (("layer", "layer", "element"), ("rms", None, "none")):
+        s = T.boundary_inputs(n, d, BF16, BF16, pre, post, kind, 14)
+        kw = dict(pre=pre, post=post, w_pre=s["w_pre"], b_pre=s["b_pre"], w_post=s["w_post"], b_post=s["b_post"], res_scale=T.SCALE, eps=T.EPS)
+        want = ops.residual_norm(s["x"], s["y"], gate=s["gate"], **kw)
+        x, ix = T.strided(s["x"], pad, shift)
+        y, iy = T.strided(s["y"], pad, shift)
+        gate, ig = T.strided(s["gate"], pad, shift) if s["gate"] is not None else (None, lambda: None)
+        got = ops.residual_norm(x, y, gate=gate, x_new=x, h=y, **kw)
+        assert got[0] is x and got[1] is y
+        # kernels that add in another order: results one rounding apart
+        near = lambda t: 2 * T.rounding(BF16) * t.double().abs() + 64 * U * (1 + t.double().abs())  # noqa: E731
+        T.check(x, want[0], near(want[0]), "x in place")
+        T.check(y, want[1], near(want[1]), "h in place")
+        for intact in (ix, iy, ig):
+            intact()
+    # the norm alone
+    x, ix = T.strided(s["x"], pad, shift)
+    h, ih = T.empty_strided_out(n, d, BF16, pad, shift)
+    ops.residual_norm(x, None, s["w_pre"], pre="rms", eps=T.EPS, h=h)
+    want = T.norm64(T.wide(s["x"]), "rms", T.wide(s["w_pre"]), None, T.EPS)[0]
+    T.check(h, want, 80 * U * 8 * (1 + want.abs()) + T.BF * want.abs(), "norm alone")
+    ix(), ih()
