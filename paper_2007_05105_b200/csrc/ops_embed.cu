@@ -459,9 +459,11 @@ __global__ void __launch_bounds__(kSumThreads, kSumBlocks) k_sum_windows(const _
     if (key == absent) return;  // entries without a part come last in the list
     const int back = pairs[hi - 1].x;
     const bool tail = back != absent && pairs[hi].x == back && pairs[hi + kSpill].x == back;
-    if (!tail)
+    if (back == absent) {  // of those there may be any number, and none is added
+        while (pairs[hi - 1].x == absent) --hi;
+    } else if (!tail) {  // the run ends within kSpill entries
         while (pairs[hi].x == back) ++hi;
-    while (pairs[hi - 1].x == absent) --hi;
+    }
 
     float acc[V];
 #pragma unroll

@@ -52,3 +52,30 @@ def test_boundary_bf16_strides_shifts_and_places(d, pad, shift):
     want = T.norm64(T.wide(s["x"]), "rms", T.wide(s["w_pre"]), None, T.EPS)[0]
     T.check(h, want, 80 * U * 8 * (1 + want.abs()) + T.BF * want.abs(), "norm alone")
     ix(), ih()
+
+
+# --------------------------------------------------------------------------
+# embedding gradient: batches of which most tokens have no part in it
+# --------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dout_t,grad_t", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("n,kept,vocab,d", [(4099, 99, 32768, 512), (1200, 60, 5, 8), (1200, 3, 5, 7), (2000, 1000, 300, 1), (33000, 17, 900, 24),
+                                            (33000, 33, 2, 16), (9001, 9000, 50257, 64), (40, 9, 3, 1024), (5000, 0, 70, 40)])
+def test_embed_grad_of_a_batch_that_is_mostly_padding(n, kept, vocab, d, dout_t, grad_t):
+    """Padding that fills windows, blocks and whole walks behind the tokens' last run; half of it by ids outside the table.  The same
+    list without a token that counts goes first, on the same multiprocessors."""
+    g = T.gen(n + kept)
+    tok = torch.full((n,), vocab - 1, device=DEV)  # the padding token
+    tok[1::2] = torch.randint(vocab, 2 * vocab, (n // 2,), device=DEV, generator=g)
+    nothing = tok.clone()
+    at = torch.randperm(n, device=DEV, generator=g)[:kept]
+    tok[at] = torch.randint(0, vocab, (kept,), device=DEV, generator=g)
+    dout = T.normal(g, n, d, dtype=dout_t)
+    for ids, accumulate in ((torch.int64, False), (torch.int32, True)):
+        base = T.normal(g, vocab, d, dtype=grad_t) if accumulate else torch.zeros(vocab, d, dtype=grad_t, device=DEV)
+        grad = base.clone()
+        ops.embed_grad(nothing.to(ids), dout, grad, scale=1.7, padding_idx=vocab - 1, accumulate=accumulate)
+        assert torch.equal(grad, base)
+        ops.embed_grad(tok.to(ids), dout, grad, scale=1.7, padding_idx=vocab - 1, accumulate=accumulate)
+        T.embed_grad_check(tok, dout, grad, base, 1.7, vocab - 1, accumulate, "mostly padding")
