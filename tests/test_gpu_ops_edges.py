@@ -79,3 +79,30 @@ def test_embed_grad_of_a_batch_that_is_mostly_padding(n, kept, vocab, d, dout_t,
         assert torch.equal(grad, base)
         ops.embed_grad(tok.to(ids), dout, grad, scale=1.7, padding_idx=vocab - 1, accumulate=accumulate)
         T.embed_grad_check(tok, dout, grad, base, 1.7, vocab - 1, accumulate, "mostly padding")
+
+
+# --------------------------------------------------------------------------
+# arguments
+# --------------------------------------------------------------------------
+
+
+def test_a_workspace_that_cannot_be_one_is_refused():
+    """On the host, of another type, with gaps: refused before anything is enqueued, results untouched."""
+    n, vocab, d = 40, 30, 16
+    tok, dout = torch.zeros(n, dtype=torch.int64, device=DEV), torch.ones(n, d, device=DEV)
+    x, vec = torch.ones(n, d, device=DEV), torch.ones(d, device=DEV)
+    need = max(ops.embed_grad_workspace(n, d), ops.residual_norm_grad_workspace(n, d))
+    good = torch.empty(need, dtype=torch.uint8, device=DEV)
+    for bad in (torch.empty(need, dtype=torch.uint8), torch.empty(need, dtype=torch.float32, device=DEV),
+                torch.empty(2 * need, dtype=torch.uint8, device=DEV)[::2], torch.empty(2, need, dtype=torch.uint8, device=DEV)[:, :need // 2 + 8]):
+        grad, dw = torch.full((vocab, d), 5.0, device=DEV), torch.full((d,), 5.0, device=DEV)
+        with pytest.raises(ValueError):
+            ops.embed_grad(tok, dout, grad, workspace=bad)
+        with pytest.raises(ValueError):
+            ops.residual_norm_grad(x, None, None, x, vec, dw_pre=dw, workspace=bad)
+        assert bool((grad == 5.0).all()) and bool((dw == 5.0).all())
+    with pytest.raises(TypeError):
+        ops.embed_grad(tok, dout, grad, workspace=need)
+    ops.embed_grad(tok, dout, grad, workspace=good)
+    assert bool((grad[0] == n).all()) and not grad[1:].any()
+    ops.residual_norm_grad(x, None, None, x, vec, dw_pre=dw, workspace=good.view(2, -1))
