@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 
@@ -296,26 +297,39 @@ cudaError_t launch(void (*kernel)(Args), long long n_blocks, int threads, size_t
 // Streaming multiprocessors of the current device (asked once per device).
 inline int sm_count()
 {
-    static int known[64] = {0};  // benign race: every thread writes the same number
-    int dev = 0;
+    static std::atomic<int> known[64];  // every thread writes the same number
+    int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    if (dev >= 0 && dev < 64 && known[dev]) return known[dev];
-    int n = 0;
+    if (dev >= 0 && dev < 64) n = known[dev].load(std::memory_order_relaxed);
+    if (n) return n;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    if (dev >= 0 && dev < 64) known[dev] = n;
+    if (dev >= 0 && dev < 64) known[dev].store(n, std::memory_order_relaxed);
     return n;
 }
 
-// Lets a kernel have `smem` bytes of dynamic shared memory on the current device.  `known` (of the kernel, zero at first)
-// remembers per device what it may have already; threads that race ask for it twice.
-inline cudaError_t allow_smem(const void *kernel, size_t smem, int (&known)[64])
+// Per device: whether a kernel's attributes have been set there.  Threads that race set them twice, to the same values.
+struct OncePerDevice {
+    std::atomic<bool> done[64];
+    // False where there is something to do for device `dev`; devices beyond the table are done every time.
+    bool has(int dev) const { return dev >= 0 && dev < 64 && done[dev].load(std::memory_order_acquire); }
+    void set(int dev)
+    {
+        if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
+    }
+};
+
+// Lets a kernel have as much dynamic shared memory on the current device as there is beside its static one.  The attribute
+// replaces what was set before, and calls from other threads may want other sizes of the same kernel: one value for all.
+inline cudaError_t allow_smem(const void *kernel, OncePerDevice &known)
 {
-    int dev = 0;
+    int dev = 0, most = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev >= 0 && dev < 64 && known[dev] >= (int)smem) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e == cudaSuccess && dev >= 0 && dev < 64) known[dev] = (int)smem;
+    if (e != cudaSuccess || known.has(dev)) return e;
+    cudaFuncAttributes f;
+    e = cudaFuncGetAttributes(&f, kernel);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most - (int)f.sharedSizeBytes);
+    if (e == cudaSuccess) known.set(dev);
     return e;
 }
 

@@ -987,8 +987,8 @@ template <typename ZT, int FORM, int WORKERS> cudaError_t launch_staged(const Ro
 {
     typedef Shape<WORKERS> S;
     constexpr size_t smem = (size_t)S::kSlots * S::kSlotBytes;
-    static int known[64] = {0};
-    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_distill_staged<ZT, FORM, WORKERS>), smem, known);
+    static OncePerDevice known;
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_distill_staged<ZT, FORM, WORKERS>), known);
     if (e != cudaSuccess) return e;
     const int most = sms * S::kBlocks / parts;
     return launch(k_distill_staged<ZT, FORM, WORKERS>, (a.n < most ? a.n : most) * parts, S::kThreads, smem, s, a, parts);

@@ -718,12 +718,12 @@ adascale_status adascale_embed_grad(const adascale_embed_grad_args *g, void *cud
     if (counted) {
         OPS_CU(launch(k_rank_tokens, ceil_div(g->n_tokens, 32) + a.zero_blocks, kSortThreads, 0, s, a));
     } else {
-        static bool allowed[64] = {false};  // per device; threads that race ask twice
+        static OncePerDevice allowed;
         int dev = 0;
         OPS_CU(cudaGetDevice(&dev));
-        if (wide && (dev < 0 || dev >= 64 || !allowed[dev])) {
+        if (wide && !allowed.has(dev)) {
             OPS_CU(cudaFuncSetAttribute(k_sort_tokens, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-            if (dev >= 0 && dev < 64) allowed[dev] = true;
+            allowed.set(dev);
         }
         const int cluster = wide ? kSortWide : kSortCluster;
         OPS_CU(launch(k_sort_tokens, cluster + a.zero_blocks, kSortThreads, 0, s, a, cluster));

@@ -687,8 +687,8 @@ template <int XT, int YT, int V, int FILL, int GROUP, int E> cudaError_t launch_
     }
     const size_t smem = groups * stages + a.weight_bytes;
     const long long need = ceil_div(a.n, groups), most = resident(sms, forward_threads(E, GROUP) / (groups * group), smem);
-    static int known[64] = {0};
-    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary<XT, YT, V, FILL, GROUP, E>), smem, known);
+    static OncePerDevice known;
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary<XT, YT, V, FILL, GROUP, E>), known);
     return e != cudaSuccess ? e : launch(k_boundary<XT, YT, V, FILL, GROUP, E>, need < most ? need : most, groups * group, smem, s, a);
 }
 template <int XT, int YT, int V, int FILL> cudaError_t launch_by_warp(const NormArgs &a, int e, int sms, cudaStream_t s)
@@ -748,8 +748,8 @@ cudaError_t launch_grad(const GradArgs &a, int group, int sms, cudaStream_t s, i
     if (blocks > kMaxPartials) blocks = kMaxPartials;
     if (blocks > need) blocks = need;
     partials = (int)blocks;
-    static int known[64] = {0};
-    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary_grad<XT, YT, V, FILL, GROUP, E, MOST>), smem, known);
+    static OncePerDevice known;
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_boundary_grad<XT, YT, V, FILL, GROUP, E, MOST>), known);
     return e != cudaSuccess ? e : launch(k_boundary_grad<XT, YT, V, FILL, GROUP, E, MOST>, blocks, threads, smem, s, a);
 }
 template <int XT, int YT, int V, int FILL> cudaError_t launch_by_warp(const GradArgs &a, int e, int sms, cudaStream_t s, int &partials)
