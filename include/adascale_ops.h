@@ -105,7 +105,8 @@ int64_t adascale_embed_grad_workspace(int64_t n_tokens, int64_t dim);
  * - A row with weight 0, or with neither part, or whose logits are all -inf, has loss 0 and a
  *   gradient of zeros whatever its logits hold; logits of weight-0 rows are not read.
  * - Masked vocabulary entries may hold -inf or the type's lowest value.  NaN or +inf in a live row
- *   make that row's loss and gradient NaN, and `loss` with it.
+ *   make that row's loss and gradient NaN, and `loss` with it.  NaN or +inf among the teacher's logits of valid
+ *   entries makes q NaN: the row's loss, and the gradient of every entry that the list names.
  * - dlogits (type of logits) may be NULL: the loss alone.  It may be logits itself (same ld).
  * - teacher_logits and teacher_ids may be NULL when n_top = 0; labels and weight may be NULL.
  */

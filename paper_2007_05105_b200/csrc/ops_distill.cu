@@ -441,18 +441,20 @@ __global__ void __launch_bounds__(kThreads, GRAD ? kBlocks : 2 * kBlocks) k_dist
         if (i < 0) continue;
         const bool middle = i >= head && i < head + (long long)nv * V;
         if (middle ? (i < c0 || i >= c1) : part != 0) continue;
-        bool first = true;
+        bool first = true, in_list = false;
         float mass = 0.f;
         if (aT != 0.f) {
             for (int j = 0; j < a.k; ++j) {
                 if (id[j] == i) {
                     if (j < k) first = false;
+                    in_list = true;
                     mass += q[j];
                 }
             }
         }
         if (!first) continue;
-        float g = slope(is_label ? z_label : zk[k]) - list_scale * mass;
+        float g = slope(is_label ? z_label : zk[k]);
+        if (in_list) g -= list_scale * mass;  // NaN where the teacher's logits make q NaN
         if (i == label) g -= b1;
         put(dz + i, g);
     }
@@ -753,7 +755,7 @@ __global__ void __launch_bounds__(Shape<kWorkers>::kThreads, Shape<kWorkers>::kB
                     if (is_label) {
                         if (lane == 0) at = f.label;
                         x = f.z_label;
-                    } else if (k < a.k && aT != 0.f && f.mass[k] >= 0.f) {
+                    } else if (k < a.k && aT != 0.f && !(f.mass[k] < 0.f)) {  // NaN counts
                         at = f.id[k];
                         mass = f.mass[k];
                         x = f.zk[k];

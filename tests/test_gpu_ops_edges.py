@@ -106,3 +106,33 @@ def test_a_workspace_that_cannot_be_one_is_refused():
     ops.embed_grad(tok, dout, grad, workspace=good)
     assert bool((grad[0] == n).all()) and not grad[1:].any()
     ops.residual_norm_grad(x, None, None, x, vec, dw_pre=dw, workspace=good.view(2, -1))
+
+
+# --------------------------------------------------------------------------
+# distillation: a teacher's list that is not finite
+# --------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,vocab,k", [(3, 5003, 6), (900, 5003, 6), (900, 20001, 40), (900, 50257, 6), (3, 5003, 200)])
+def test_distill_a_teacher_that_is_not_finite(n, vocab, k, dtype, bad):
+    """Rows read twice and rows kept in shared memory: the loss, and the gradient where the list names an entry, are NaN; the rest is
+    as if the list had been finite; other rows do not notice."""
+    z, t, ids, labels, _ = T.distill_inputs(n, vocab, k, dtype, 31)
+    ids[:] = torch.arange(k, device=DEV, dtype=ids.dtype) * 7 + 3
+    ids[:, -1] = ids[:, 0]    # named twice
+    ids[:, 2] = -1            # not an entry: its logit is not looked at
+    t[:, 2] = bad
+    labels[:] = 11            # no 7 m + 3
+    labels[0] = 3             # in the list
+    at = dict(labels=labels, T=2.0, alpha=0.5, beta=0.5)
+    want = ops.distill(z, t, ids, **at)
+    assert not torch.isnan(want.row_loss).any() and not torch.isnan(want.dlogits).any()
+    t[:2, 1] = bad
+    got = ops.distill(z, t, ids, **at)
+    named = torch.zeros(n, vocab, dtype=torch.bool, device=DEV)
+    named[:2, ids[0, ids[0] >= 0].long()] = True
+    assert torch.equal(torch.isnan(got.dlogits), named)
+    assert bool(torch.isnan(got.row_loss[:2]).all()) and bool(torch.isnan(got.loss))
+    assert torch.equal(got.row_loss[2:], want.row_loss[2:]) and torch.equal(got.dlogits[~named], want.dlogits[~named])
