@@ -40,6 +40,7 @@ extern "C" {
 typedef enum { ADASCALE_I32 = 0, ADASCALE_I64 = 1 } adascale_itype; /* token ids and labels */
 
 #define ADASCALE_OPS_MAX_ROWS 2147483647LL /* tokens or rows of one call, vocabulary size - 1 */
+#define ADASCALE_EMBED_MAX_DIM 1073741824LL /* width of a token table */
 #define ADASCALE_DISTILL_MAX_K 1024        /* entries of a teacher's list */
 #define ADASCALE_NORM_MAX_DIM 16384        /* width of a block boundary */
 

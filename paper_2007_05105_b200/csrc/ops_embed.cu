@@ -7,6 +7,10 @@ namespace {
 
 namespace cg = cooperative_groups;
 
+// Columns are counted in 32 bits, some beyond a row's last one: by steps of 128 (lookup), rounded up to 32 (join).
+constexpr long long kMaxDim = ADASCALE_EMBED_MAX_DIM;
+static_assert(kMaxDim + 1024 < 2147483648LL, "columns beyond a row's last one stay positive");
+
 // ---------------------------------------------------------------------------------------------
 // lookup
 // ---------------------------------------------------------------------------------------------
@@ -655,7 +659,7 @@ adascale_status adascale_embed(const adascale_embed_args *g, void *cuda_stream)
     if (!g || g->n_tokens < 0 || g->vocab < 1 || g->dim < 1 || !is_dtype(g->table_dtype) || !is_dtype(g->out_dtype) ||
         !is_itype(g->token_type) || !std::isfinite(g->scale))
         return ADASCALE_ERR_INVALID_ARG;
-    if (g->n_tokens > kMaxRows || g->vocab > kMaxRows || g->dim > kMaxRows) return ADASCALE_ERR_TOO_LARGE;
+    if (g->n_tokens > kMaxRows || g->vocab > kMaxRows || g->dim > kMaxDim) return ADASCALE_ERR_TOO_LARGE;
     if (g->n_tokens == 0) return ADASCALE_OK;
     if (!g->tokens || !g->table || !g->out || g->ld_table < g->dim || g->ld_out < g->dim) return ADASCALE_ERR_INVALID_ARG;
     const int et = elem_bytes(g->table_dtype), eo = elem_bytes(g->out_dtype);
@@ -675,7 +679,7 @@ adascale_status adascale_embed(const adascale_embed_args *g, void *cuda_stream)
 // Two lists of pairs and two rows of 32-bit sums per window.
 int64_t adascale_embed_grad_workspace(int64_t n_tokens, int64_t dim)
 {
-    if (n_tokens < 0 || n_tokens > kMaxRows || dim < 1 || dim > kMaxRows) return 0;
+    if (n_tokens < 0 || n_tokens > kMaxRows || dim < 1 || dim > kMaxDim) return 0;
     const long long pairs = ceil_div(n_tokens, 2) * 2;
     return 2 * pairs * (long long)sizeof(Pair) + ceil_div(n_tokens, kLeastWindow) * 2 * piece_stride(dim) * (long long)sizeof(float);
 }
@@ -685,7 +689,7 @@ adascale_status adascale_embed_grad(const adascale_embed_grad_args *g, void *cud
     if (!g || g->n_tokens < 0 || g->vocab < 1 || g->dim < 1 || !is_dtype(g->dout_dtype) || !is_dtype(g->grad_dtype) ||
         !is_itype(g->token_type) || !std::isfinite(g->scale) || !g->grad || g->ld_grad < g->dim)
         return ADASCALE_ERR_INVALID_ARG;
-    if (g->n_tokens > kMaxRows || g->vocab > kMaxRows || g->dim > kMaxRows) return ADASCALE_ERR_TOO_LARGE;
+    if (g->n_tokens > kMaxRows || g->vocab > kMaxRows || g->dim > kMaxDim) return ADASCALE_ERR_TOO_LARGE;
     const int ed = elem_bytes(g->dout_dtype), eg = elem_bytes(g->grad_dtype);
     if (!on(g->grad, eg)) return ADASCALE_ERR_ALIGNMENT;
     if (g->n_tokens == 0 && g->accumulate) return ADASCALE_OK;

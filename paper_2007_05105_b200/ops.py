@@ -39,6 +39,7 @@ EXPORTS = ("adascale_embed", "adascale_embed_grad", "adascale_embed_grad_workspa
 I32, I64 = 0, 1
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 GATE_NONE, GATE_CHANNEL, GATE_SIGMOID = 0, 1, 2
+EMBED_MAX_DIM = 1 << 30
 DISTILL_MAX_K = 1024
 NORM_MAX_DIM = 16384
 
