@@ -184,6 +184,12 @@ at::Tensor given_or_new(const at::Tensor *t, at::IntArrayRef shape, at::ScalarTy
     return *t;
 }
 
+// Tells torch that a tensor of the caller's has been written to: what was saved of it for a backward pass is not valid any more.
+void written(const at::Tensor *given)
+{
+    if (given && !given->is_inference()) given->unsafeGetTensorImpl()->bump_version();
+}
+
 void *stream_of(at::Device device) { return c10::cuda::getCurrentCUDAStream(device.index()).stream(); }
 
 PyObject *adascale_error = nullptr;  // binding.AdaScaleError
@@ -249,7 +255,9 @@ PyObject *embed(PyObject *const *o)
     a.ld_out = m.ld;
     a.scale = (float)number(o[2], "scale");
     const adascale_status s = adascale_embed(&a, stream_of(device));
-    return s == ADASCALE_OK ? wrap(out) : status_error(s);
+    if (s != ADASCALE_OK) return status_error(s);
+    written(given);
+    return wrap(out);
 }
 
 // tokens, dout, grad, scale, padding_idx, accumulate, workspace
@@ -281,6 +289,7 @@ PyObject *embed_grad(PyObject *const *o)
     a.workspace_bytes = room.bytes;
     const adascale_status s = adascale_embed_grad(&a, stream_of(device));
     if (s != ADASCALE_OK) return status_error(s);
+    written(&grad);
     Py_INCREF(o[2]);
     return o[2];
 }
@@ -334,7 +343,9 @@ PyObject *distill(PyObject *const *o)
     a.row_loss = static_cast<float *>(row_loss.data_ptr());
     a.loss = static_cast<float *>(loss.data_ptr());
     const adascale_status s = adascale_distill(&a, stream_of(device));
-    return s == ADASCALE_OK ? Py_BuildValue("(NNN)", wrap(loss), wrap(row_loss), wrap_or_none(dlogits)) : status_error(s);
+    if (s != ADASCALE_OK) return status_error(s);
+    written(given);
+    return Py_BuildValue("(NNN)", wrap(loss), wrap(row_loss), wrap_or_none(dlogits));
 }
 
 // A gate: a float32 vector over the channels, or a matrix of y's type.
@@ -396,6 +407,8 @@ PyObject *residual_norm(PyObject *const *o)
     a.b_post = f32_vector(b_post, shape.d, device, "b_post");
     const adascale_status s = adascale_residual_norm(&a, stream_of(device));
     if (s != ADASCALE_OK) return status_error(s);
+    if (y) written(given_x);
+    written(given_h);
     PyObject *new_x = y ? wrap(x_new) : (Py_INCREF(o[0]), o[0]);
     return Py_BuildValue("(NN)", new_x, wrap(h));
 }
@@ -428,8 +441,10 @@ PyObject *residual_norm_grad(PyObject *const *o)
         ld = m.ld;
         return m.p;
     };
+    c10::SmallVector<const at::Tensor *, 8> given_ones;
     auto new_rows = [&](PyObject *given, at::ScalarType type, const char *what, int64_t &ld, void *&p) {
-        const at::Tensor t = given_or_new(tensor(given, what), x.sizes(), type, device, what);
+        given_ones.push_back(tensor(given, what));
+        const at::Tensor t = given_or_new(given_ones.back(), x.sizes(), type, device, what);
         p = rows(t, type, what, ld);
         return t;
     };
@@ -442,7 +457,8 @@ PyObject *residual_norm_grad(PyObject *const *o)
             p = t.data_ptr();
             return t;
         }
-        const at::Tensor t = given_or_new(tensor(given, what), {shape.d}, wtype, device, what);
+        given_ones.push_back(tensor(given, what));
+        const at::Tensor t = given_or_new(given_ones.back(), {shape.d}, wtype, device, what);
         p = vector(t, shape.d, device, what);
         return t;
     };
@@ -470,6 +486,7 @@ PyObject *residual_norm_grad(PyObject *const *o)
     a.workspace_bytes = room.bytes;
     const adascale_status s = adascale_residual_norm_grad(&a, stream_of(device));
     if (s != ADASCALE_OK) return status_error(s);
+    for (const at::Tensor *t : given_ones) written(t);
     return Py_BuildValue("(NNNNNNN)", wrap(dx), wrap_or_none(dy), wrap_or_none(dgate), wrap_or_none(dw_post), wrap_or_none(db_post),
                          wrap(dw_pre), wrap_or_none(db_pre));
 }

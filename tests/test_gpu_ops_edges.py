@@ -136,3 +136,45 @@ def test_distill_a_teacher_that_is_not_finite(n, vocab, k, dtype, bad):
     assert torch.equal(torch.isnan(got.dlogits), named)
     assert bool(torch.isnan(got.row_loss[:2]).all()) and bool(torch.isnan(got.loss))
     assert torch.equal(got.row_loss[2:], want.row_loss[2:]) and torch.equal(got.dlogits[~named], want.dlogits[~named])
+
+
+def test_tensors_that_are_written_to_say_so():
+    """torch's version counters: up by each call that writes to a given tensor, not by one that only reads it or is refused."""
+    n, d = 8, 16
+    tok = torch.arange(n, device=DEV)
+    m = lambda: torch.ones(n, d, device=DEV)  # noqa: E731
+    v = lambda: torch.ones(d, device=DEV)  # noqa: E731
+    x, y, dx, dh, w, out, grad, z, gate = m(), m(), m(), m(), v(), m(), m(), m(), v()
+    gx, gy, ge, gw = m(), m(), m(), [v() for _ in range(5)]
+    calls = [
+        (lambda: ops.embed(tok, x, out=out), [out], [x, tok]),
+        (lambda: ops.embed_grad(tok, dx, grad), [grad], [dx]),
+        (lambda: ops.distill(z, labels=tok, alpha=0.0, beta=1.0, dlogits=z), [z], [tok]),
+        (lambda: ops.distill(z, labels=tok, alpha=0.0, beta=1.0), [], [z]),
+        (lambda: ops.residual_norm(x, y, w, gate=gate, x_new=x, h=y), [x, y], [w, gate]),
+        (lambda: ops.residual_norm(x, None, w, h=out), [out], [x, w]),
+        (lambda: ops.residual_norm_grad(x, y, dx, dh, w, w, w, pre="layer", post="layer", gate=gate, dx=dx, dy=dh, dgate=gw[0], dw_post=gw[1],
+                                        db_post=gw[2], dw_pre=gw[3], db_pre=gw[4]), [dx, dh] + gw, [x, y, w, gate]),
+        (lambda: ops.residual_norm_grad(x, y, dx, dh, w, gate=y, dx=gx, dy=gy, dgate=ge, dw_pre=gw[0]), [gx, gy, ge, gw[0]], [x, y, dx, dh, gw[1]]),
+    ]
+    for k, (call, writes, reads) in enumerate(calls):
+        before = [t._version for t in writes + reads]
+        call()
+        assert [t._version - b for t, b in zip(writes + reads, before)] == [1] * len(writes) + [0] * len(reads), k
+    row = torch.zeros(4 * d, device=DEV)  # a slot is part of its row
+    ops.residual_norm_grad(x, None, None, dh, w, dw_pre=row[d:2 * d])
+    assert row._version == 1
+    with pytest.raises(ValueError):
+        ops.embed(tok, x, out=out[:3])
+    with pytest.raises(ops.AdaScaleError):
+        ops.distill(z, T=0.0, dlogits=z)
+    assert out._version == 2 and z._version == 1
+    # what torch's own check makes of it
+    leaf = m().requires_grad_()
+    kept = leaf * 2.0
+    loss = (kept * kept).sum()
+    ops.embed(tok, x, out=kept.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():
+        ops.embed(tok, x, out=m())
