@@ -68,6 +68,13 @@ int64_t whole(PyObject *o, const char *what)
     return v;
 }
 
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw python_error();  // the error that is pending
+    return v;
+}
+
 int float_code(at::ScalarType t, const char *what)
 {
     if (t == at::kFloat) return ADASCALE_F32;
@@ -283,7 +290,7 @@ PyObject *embed_grad(PyObject *const *o)
     a.ld_grad = m.ld;
     a.scale = (float)number(o[3], "scale");
     a.padding_idx = whole(o[4], "padding_idx");
-    a.accumulate = PyObject_IsTrue(o[5]);
+    a.accumulate = truth(o[5]);
     const Room room(o[6], adascale_embed_grad_workspace(a.n_tokens, a.dim), device);
     a.workspace = room.p;
     a.workspace_bytes = room.bytes;
@@ -332,7 +339,7 @@ PyObject *distill(PyObject *const *o)
     a.alpha = (float)number(o[5], "alpha");
     a.beta = (float)number(o[6], "beta");
     at::Tensor dlogits;
-    if (given || PyObject_IsTrue(o[8])) {
+    if (given || truth(o[8])) {
         dlogits = given_or_new(given, logits.sizes(), logits.scalar_type(), device, "dlogits");
         m = matrix(dlogits, shape.n, shape.d, device, "dlogits");
         a.dlogits = m.p;

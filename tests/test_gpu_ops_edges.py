@@ -178,3 +178,18 @@ def test_tensors_that_are_written_to_say_so():
         loss.backward()
     with torch.inference_mode():
         ops.embed(tok, x, out=m())
+
+
+def test_flags_without_a_truth_value_are_refused():
+    class Neither:
+        def __bool__(self):
+            raise KeyError("neither")
+
+    tok, z = torch.zeros(3, dtype=torch.int64, device=DEV), torch.zeros(3, 8, device=DEV)
+    grad = torch.full((4, 8), 5.0, device=DEV)
+    for flag, error in ((Neither(), KeyError), (torch.zeros(2), RuntimeError)):
+        with pytest.raises(error):
+            ops.embed_grad(tok, z, grad, accumulate=flag)
+        with pytest.raises(error):
+            ops.distill(z, labels=tok, alpha=0.0, beta=1.0, want_grad=flag)
+    assert bool((grad == 5.0).all())
