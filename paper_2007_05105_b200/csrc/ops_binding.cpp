@@ -8,6 +8,7 @@
 #include "../../include/adascale_ops.h"
 
 #include <ATen/ATen.h>
+#include <ATen/TensorUtils.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -115,6 +116,7 @@ Matrix matrix(const at::Tensor &t, int64_t n, int64_t d, at::Device device, cons
     if (t.device() != device) refuse("%s is on %s, not on %s", what, t.device().str().c_str(), device.str().c_str());
     if (t.dim() != 2) {
         if (t.dim() == 0 || t.size(-1) != d || t.numel() != n * d) refuse("%s: not %lld rows of %lld", what, (long long)n, (long long)d);
+        if (!at::detail::computeStride(t.sizes(), t.strides(), c10::IntArrayRef({n, d}))) refuse("%s: its rows have no common stride", what);
         return matrix(t.view({n, d}), n, d, device, what);
     }
     if (t.size(0) != n || t.size(1) != d)

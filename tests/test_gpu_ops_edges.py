@@ -193,3 +193,17 @@ def test_flags_without_a_truth_value_are_refused():
         with pytest.raises(error):
             ops.distill(z, labels=tok, alpha=0.0, beta=1.0, want_grad=flag)
     assert bool((grad == 5.0).all())
+
+
+def test_leading_dimensions_that_are_not_one():
+    """Rows at a common stride are taken, whatever the dimensions before the last; others are refused as a wrong shape."""
+    tok = torch.randint(0, 9, (2, 5), device=DEV)
+    table, w = T.normal(T.gen(3), 9, 16), torch.ones(16, device=DEV)
+    wider, longer = torch.zeros(2, 5, 24, device=DEV)[..., :16], torch.zeros(2, 8, 16, device=DEV)[:, :5]
+    assert torch.equal(ops.embed(tok, table, out=wider), table[tok])
+    assert torch.equal(ops.residual_norm(wider, None, w)[1], ops.residual_norm(wider.contiguous(), None, w)[1])
+    for call in (lambda: ops.embed(tok, table, out=longer), lambda: ops.embed_grad(tok, longer, torch.zeros(9, 16, device=DEV)),
+                 lambda: ops.distill(longer), lambda: ops.distill(wider, dlogits=longer), lambda: ops.residual_norm(longer, longer, w),
+                 lambda: ops.residual_norm_grad(longer, None, None, wider, w), lambda: ops.residual_norm_grad(wider, None, longer, wider, w)):
+        with pytest.raises(ValueError, match="common stride"):
+            call()
