@@ -98,6 +98,8 @@ def _on(stream, t):
     """Makes another stream (an address or a torch.cuda.Stream) the current one of t's device."""
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream), device=t.device)
+    elif stream.device != t.device:
+        raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, t.device))
     return torch.cuda.stream(stream)
 
 

@@ -207,3 +207,17 @@ def test_leading_dimensions_that_are_not_one():
                  lambda: ops.residual_norm_grad(longer, None, None, wider, w), lambda: ops.residual_norm_grad(wider, None, longer, wider, w)):
         with pytest.raises(ValueError, match="common stride"):
             call()
+
+
+def test_a_stream_of_another_device_is_refused():
+    """It would leave the tensors' device on its own current stream."""
+    class Elsewhere:
+        device = torch.device("cuda", DEV.index + 1)
+
+    side = torch.cuda.Stream()
+    with pytest.raises(ValueError, match="the stream is on cuda:0"):
+        ops._on(side, Elsewhere())
+    with pytest.raises(ValueError):
+        ops.embed(torch.zeros(3, dtype=torch.int64), torch.zeros(4, 8), stream=side)  # tensors on the host
+    with ops._on(side, torch.zeros(1, device=DEV)):
+        assert torch.cuda.current_stream() == side
