@@ -471,7 +471,8 @@ __global__ void __launch_bounds__(kThreads, GRAD ? kBlocks : 2 * kBlocks) k_dist
 //   lists     two or four warps, rows ahead, each its own: weight, label, the teacher's list turned into q
 //   workers   four, eight or sixteen warps: maximum and sums as the pieces arrive; then the gradient of every entry, over the row in its slots
 //   storer    one warp: the named entries' whole values into the slots, bulk copies out, slots back to the loader; the row's loss
-// Every wait is bounded; a job that gives up leaves NaN as the row's loss and ends.
+// Every wait is bounded; a job that gives up leaves NaN as the row's loss and ends, and the others follow when their waits run
+// out.  The storer, which no row passes by, then leaves NaN as the loss and in the block's part of the gradient of all rows to come.
 constexpr int kStagedMaxK = 128;  // list entries: a lists' warp has a few rows' time for them
 constexpr int kPiecesEach = 2;    // 16-byte pieces of a slot per worker thread
 
@@ -818,7 +819,15 @@ __global__ void __launch_bounds__(Shape<kWorkers>::kThreads, Shape<kWorkers>::kB
                 }
             }
             if (!ok) {
-                if (lane == 0) lost(row);
+                if (lane == 0) bulk_wait_all();
+                __syncwarp();
+                for (; row < a.n; row += step) {
+                    const Part p = part_of(row);
+                    ZT *dz = static_cast<ZT *>(a.dz) + row * a.ld_dz;
+                    for (long long v = (long long)p.v0 * V + lane; v < (long long)p.v1 * V; v += 32) put(dz + p.head + v, __int_as_float(0x7fffffff));
+                    if (lane < loose_of(p)) put(dz + loose_at(p, lane), __int_as_float(0x7fffffff));
+                    if (lane == 0) lost(row);
+                }
                 break;
             }
             __syncwarp();

@@ -250,7 +250,8 @@ template <int E> __device__ __forceinline__ void sigmoids(f2 (&v)[E / 2])
 
 // The rows of a group in shared memory, kStages at a time: the arrays of a row one after another.  One thread
 // of the group asks for them; a stage is asked for again after a barrier of the group behind its last read.
-// A copy that does not arrive within the wait's bound is given up: the group stops and poisons its results.
+// A copy that does not arrive within the wait's bound is given up: the group stops, and its results from that row on
+// become NaN (Lost).
 struct Stages {
     char *base;       // the group's
     u64 *full;        // [kStages]
@@ -268,6 +269,28 @@ struct Stages {
         }
     }
 };
+
+// The row at which each group of a block gave up; kNone as a rule.  What follows a group's rows asks for it, so that nothing of
+// it is alive in the walk over them.
+template <int GROUPS> struct Lost {
+    static constexpr u64 kNone = ~0ull;
+    u64 row[GROUPS];
+    __device__ __forceinline__ void from(int group, long long r) { atomicMin(row + group, (u64)r); }
+    __device__ __forceinline__ bool any() const
+    {
+        bool some = false;
+        for (int q = 0; q < GROUPS; ++q) some |= row[q] != kNone;
+        return some;
+    }
+};
+__device__ __noinline__ void poison(const Rows &m, u64 row, long long n, long long step, int dim, int t, int threads)
+{
+    for (long long r = (long long)row; m.p && r < n; r += step)
+        for (int c = t; c < dim; c += threads) {
+            if (m.is_bf16) put(reinterpret_cast<bf16 *>(m.row(r)) + c, __int_as_float(0x7fffffff));
+            else put(reinterpret_cast<float *>(m.row(r)) + c, __int_as_float(0x7fffffff));
+        }
+}
 
 template <int GROUP> __device__ __forceinline__ void group_barrier()
 {
@@ -308,6 +331,7 @@ __global__ void __launch_bounds__(forward_threads(E, GROUP), 1) k_boundary(const
     extern __shared__ __align__(128) char room[];
     __shared__ __align__(16) float scratch[2][kScratch][2];
     __shared__ u64 full[kStaged ? kMostWarps : 1][kStages];
+    __shared__ Lost<kStaged ? kMostWarps : 1> lost;
     const int mine = kWarp ? threadIdx.x / 32 : 0, groups = kWarp ? blockDim.x / 32 : 1;
     const Place<E, V, FILL> at = place_of<E, V, FILL, GROUP>(a.dim);
     const long long all = (long long)gridDim.x * groups;
@@ -318,6 +342,7 @@ __global__ void __launch_bounds__(forward_threads(E, GROUP), 1) k_boundary(const
     if (kStaged && at.t == 0) {
         for (int s = 0; s < kStages; ++s) mbar_init(stages.full + s, 1);
         mbar_publish();
+        lost.row[mine] = lost.kNone;
     }
     group_barrier<GROUP>();
     griddep_wait();
@@ -346,9 +371,7 @@ __global__ void __launch_bounds__(forward_threads(E, GROUP), 1) k_boundary(const
         const char *px = a.x.row(row), *py = a.y.row(row), *pg = a.gate.row(row);
         if constexpr (kStaged) {
             if (!mbar_wait(stages.full + stage, parity)) {
-                f2 lost[E / 2];
-                fill<E>(lost, __int_as_float(0x7fffffff));
-                write<E, V, FILL>(at, a.h.row(row), is_bf16<YT>(a.h), lost);
+                lost.from(mine, row);
                 mbar_wait(stages.full + (stage ^ 1), parity ^ (stage == 1));  // the other copy in flight
                 break;
             }
@@ -413,6 +436,13 @@ __global__ void __launch_bounds__(forward_threads(E, GROUP), 1) k_boundary(const
         }
         write<E, V, FILL>(at, a.h.row(row), is_bf16<YT>(a.h), x);
     }
+    if constexpr (kStaged) {
+        group_barrier<GROUP>();
+        if (lost.row[mine] != lost.kNone) {
+            if (a.y.p) poison(a.x_new, lost.row[mine], a.n, all, a.dim, at.t, GROUP);
+            poison(a.h, lost.row[mine], a.n, all, a.dim, at.t, GROUP);
+        }
+    }
 }
 
 struct GradArgs {
@@ -438,6 +468,7 @@ __global__ void __launch_bounds__(MOST, 1) k_boundary_grad(const __grid_constant
     extern __shared__ __align__(128) char room[];
     __shared__ __align__(16) float scratch[2][kScratch][2];
     __shared__ u64 full[kGroups][kStages];
+    __shared__ Lost<kGroups> lost;
     const int mine = kWarp ? threadIdx.x / 32 : 0;
     const Place<E, V, FILL> at = place_of<E, V, FILL, GROUP>(a.dim);
     const long long all = (long long)gridDim.x * kGroups;
@@ -448,6 +479,7 @@ __global__ void __launch_bounds__(MOST, 1) k_boundary_grad(const __grid_constant
     if (kStaged && at.t == 0) {
         for (int s = 0; s < kStages; ++s) mbar_init(stages.full + s, 1);
         mbar_publish();
+        lost.row[mine] = lost.kNone;
     }
     group_barrier<GROUP>();
     griddep_wait();
@@ -467,7 +499,7 @@ __global__ void __launch_bounds__(MOST, 1) k_boundary_grad(const __grid_constant
         const char *px = a.x.row(row), *ph = a.dh.row(row), *pd = a.dx_new.row(row), *py = a.y.row(row), *pg = a.gate.row(row);
         if constexpr (kStaged) {
             if (!mbar_wait(stages.full + stage, parity)) {
-                fill<E>(acc[kDwPre], __int_as_float(0x7fffffff));
+                lost.from(mine, row);
                 mbar_wait(stages.full + (stage ^ 1), parity ^ (stage == 1));  // the other copy in flight
                 break;
             }
@@ -590,6 +622,18 @@ __global__ void __launch_bounds__(MOST, 1) k_boundary_grad(const __grid_constant
                 for (int q = 1; q < kGroups; ++q) s += gather[q * a.ld_partial + c];
                 reinterpret_cast<float *>(to)[k * a.ld_partial + c] = s;
             }
+        }
+    }
+    if constexpr (kStaged) {
+        __syncthreads();
+        if (lost.any()) {
+            if (lost.row[mine] != lost.kNone) {
+                const int t = kWarp ? threadIdx.x & 31 : threadIdx.x, threads = kWarp ? 32 : blockDim.x;
+                poison(a.dx, lost.row[mine], a.n, all, a.dim, t, threads);
+                poison(a.dy, lost.row[mine], a.n, all, a.dim, t, threads);
+                poison(a.dgate, lost.row[mine], a.n, all, a.dim, t, threads);
+            }
+            poison({to, a.ld_partial * 4LL, 0}, 0, kSums, 1, a.dim, threadIdx.x, blockDim.x);
         }
     }
 }
