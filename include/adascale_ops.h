@@ -21,6 +21,8 @@
  *     element's own size is accepted.
  *   - dtype fields are adascale_dtype (ADASCALE_F32, ADASCALE_BF16).  All arithmetic, sums and
  *     statistics are 32-bit or wider; a bf16 result is rounded once, to nearest even, when it is stored.
+ *   - What a gradient call has enqueued last does not let the stream's next kernel start before it has stored its results, so
+ *     adascale_step may follow directly, with ADASCALE_FLAG_GRADS_READY too.
  *   - Results are the same bits from run to run: no sum depends on the order in which blocks run.
  *   - Inputs and outputs must not overlap unless a field says so.
  *   - Errors: INVALID_ARG (null pointer, negative size, unknown enum, stride below the row's length,

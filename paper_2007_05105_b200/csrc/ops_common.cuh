@@ -175,7 +175,8 @@ __device__ __forceinline__ long long load_id(const void *p, int wide, long long 
 
 // ---- programmatic dependent launch ---------------------------------------------------------
 // The rule of adascale_kernels.cuh: a kernel lets its successor start early only after its own
-// wait has returned, and touches nothing in global memory before that wait.
+// wait has returned, and touches nothing in global memory before that wait.  A kernel that writes gradients lets only another
+// kernel of its call start early: a step that reads its rows ahead of the kernel before it (ADASCALE_FLAG_GRADS_READY) may come next.
 __device__ __forceinline__ void griddep_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -112,6 +112,7 @@ struct SortArgs {
     int wide, passes;
     int zero_blocks;    // 0 when accumulating
     int grad_bytes;     // bytes of a gradient element
+    int followed;       // by another kernel of the call
 };
 
 __device__ __forceinline__ int key_of(const SortArgs &a, long long i)
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_tokens(const __grid_co
     __shared__ unsigned scan[kSortBins / 32], start[kSortBins];
     static_assert(sizeof(count) * 8 >= kZeroBits, "the zero-fill's bits fit");
     griddep_wait();
-    griddep_launch();
+    if (a.followed) griddep_launch();
     const cg::cluster_group cluster = cg::this_cluster();
     const int blocks = (int)cluster.num_blocks();
     if ((int)blockIdx.x >= blocks) {
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(kSortThreads, 2) k_rank_tokens(const __grid_co
     __shared__ int part[kSortWarps][32];
     static_assert(sizeof(keys) * 8 >= kZeroBits, "the zero-fill's bits fit");
     griddep_wait();
-    griddep_launch();
+    if (a.followed) griddep_launch();
     const int n = (int)a.n;
     if ((int)blockIdx.x < a.zero_blocks) {  // first, as they take longest
         zero_absent(a, reinterpret_cast<unsigned *>(keys), cg::this_cluster(), (int)blockIdx.x);
@@ -366,6 +367,7 @@ struct SumArgs {
     int nv;             // vectors of a row
     int threads;        // of a window: one per vector, or per kColumns elements
     int accumulate;
+    int followed;       // by k_join
     float scale;
 };
 
@@ -437,7 +439,7 @@ __global__ void __launch_bounds__(kSumThreads, kSumBlocks) k_sum_windows(const _
     __shared__ uint4 ring[V == 1 ? 1 : kDepth][V == 1 ? 1 : kSumThreads];
     __shared__ int2 pairs[kMostPairs + kSpill + 2];
     griddep_wait();
-    griddep_launch();
+    if (a.followed) griddep_launch();
     const long long t0 = (long long)blockIdx.x * kSumThreads, t1 = t0 + kSumThreads - 1;
     const long long base = t0 / a.threads * a.window - 1;  // entry of pairs[0]
     const int here = (int)(t1 / a.threads - t0 / a.threads + 1) * a.window + kSpill + 2;
@@ -634,8 +636,9 @@ cudaError_t launch_sums(SumArgs a, long long dim, int sms, cudaStream_t s)
     a.threads = V == 1 ? (int)ceil_div(dim, kColumns) : a.nv;
     a.window = window_of(a.n, a.threads, sms);
     const long long windows = ceil_div(a.n, a.window);
+    a.followed = windows > 1;
     cudaError_t e = launch(k_sum_windows<DT, GT, V>, ceil_div(windows * a.threads, kSumThreads), kSumThreads, 0, s, a);
-    if (e != cudaSuccess || windows == 1) return e;
+    if (e != cudaSuccess || !a.followed) return e;
     constexpr int JV = V == 1 ? 1 : 4;
     a.nv = (int)(dim / JV);
     return launch(k_join<GT, JV>, ceil_div((windows - 1) * ceil_div(a.nv, 32), kSumThreads / 32), kSumThreads, 0, s, a);
@@ -717,6 +720,7 @@ adascale_status adascale_embed_grad(const adascale_embed_grad_args *g, void *cud
     a.wide = g->token_type == ADASCALE_I64;
     while ((g->vocab >> (kSortBits * a.passes)) > 0) ++a.passes;  // the largest key is vocab itself
     a.grad_bytes = eg;
+    a.followed = g->n_tokens > 0;
     const bool counted = g->n_tokens <= (g->accumulate ? kRankMost : kRankBesideZeros), wide = g->n_tokens >= kSortWideFrom;
     a.zero_blocks = g->accumulate ? 0 : wide ? kZeroWide : kZeroBlocks;
     if (counted) {

@@ -452,6 +452,7 @@ struct GradArgs {
     long long n;
     int dim, ld_partial;
     int post, pre, gate_kind;
+    int followed;  // by k_columns
     unsigned stage_bytes;
     float inv_dim, res_scale, eps;
 };
@@ -483,7 +484,7 @@ __global__ void __launch_bounds__(MOST, 1) k_boundary_grad(const __grid_constant
     }
     group_barrier<GROUP>();
     griddep_wait();
-    griddep_launch();
+    if (a.followed) griddep_launch();
     const Rows *const arrays[5] = {&a.x, &a.dh, &a.dx_new, &a.y, &a.gate};
     if (kStaged && at.t == 0)
         for (int s = 0; s < kStages; ++s)
@@ -942,6 +943,14 @@ adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_ar
     const int sms = sm_count();
     if (!sms) return ADASCALE_ERR_CUDA;
     cudaStream_t s = (cudaStream_t)cuda_stream;
+    ColumnArgs b = {};
+    b.partial = static_cast<const float *>(g->workspace);
+    b.out[kDwPre] = g->dw_pre;
+    b.out[kDbPre] = g->pre == ADASCALE_NORM_LAYER ? g->db_pre : nullptr;
+    b.out[kDwPost] = post ? g->dw_post : nullptr;
+    b.out[kDbPost] = post && g->post == ADASCALE_NORM_LAYER ? g->db_post : nullptr;
+    b.out[kDgate] = gated && !matrix ? g->dgate : nullptr;
+    const bool columns = b.out[0] || b.out[1] || b.out[2] || b.out[3] || b.out[4];
     int partials = 0;
     const int ld_partial = (int)(ceil_div(g->dim, 8) * 8);
     if (g->n_rows > 0) {
@@ -952,7 +961,7 @@ adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_ar
         a.dh = rows(g->dh, g->ld_dh, g->y_dtype);
         a.gate = rows(matrix ? g->gate : nullptr, g->ld_gate, g->y_dtype);
         a.dx = rows(g->dx, g->ld_dx, g->x_dtype);
-        a.dy = rows(g->dy, g->ld_dy, g->y_dtype);
+        a.dy = rows(g->y ? g->dy : nullptr, g->ld_dy, g->y_dtype);
         a.dgate = rows(matrix ? g->dgate : nullptr, g->ld_dgate, g->y_dtype);
         a.gate_channel = gated && !matrix ? static_cast<const float *>(g->gate) : nullptr;
         a.w_post = post ? g->w_post : nullptr;
@@ -962,6 +971,7 @@ adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_ar
         a.n = g->n_rows;
         a.dim = (int)g->dim;
         a.ld_partial = ld_partial;
+        a.followed = columns;
         a.post = g->post;
         a.pre = g->pre;
         a.gate_kind = gated ? g->gate_kind : ADASCALE_GATE_NONE;
@@ -980,18 +990,11 @@ adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_ar
         else
             OPS_CU(g->y_dtype == ADASCALE_F32 ? launch_grad<kBf16, kF32>(a, vec, sms, s, partials) : launch_grad<kBf16, kBf16>(a, vec, sms, s, partials));
     }
-    ColumnArgs b = {};
-    b.partial = static_cast<const float *>(g->workspace);
-    b.out[kDwPre] = g->dw_pre;
-    b.out[kDbPre] = g->pre == ADASCALE_NORM_LAYER ? g->db_pre : nullptr;
-    b.out[kDwPost] = post ? g->dw_post : nullptr;
-    b.out[kDbPost] = post && g->post == ADASCALE_NORM_LAYER ? g->db_post : nullptr;
-    b.out[kDgate] = gated && !matrix ? g->dgate : nullptr;
     b.dim = (int)g->dim;
     b.ld_partial = ld_partial;
     b.n_partials = partials;
     b.bf16_out = g->wgrad_dtype == ADASCALE_BF16;
-    if (b.out[0] || b.out[1] || b.out[2] || b.out[3] || b.out[4])
+    if (columns)
         OPS_CU(launch(k_columns, kSums * ceil_div(g->dim, 32), kColumnWarps * 32, 0, s, b));
     return ADASCALE_OK;
 }
