@@ -67,6 +67,8 @@ adascale_status adascale_embed(const adascale_embed_args *args, void *cuda_strea
  * Without `accumulate` the whole table's gradient is written, zeros where no token points; with it
  * the sums are added to what grad holds and rows of absent tokens are not touched (a tied table
  * whose output projection has already left its part, or several batches into one gradient row).
+ * Adding to a float32 grad is one addition per element by the L2 cache, which takes subnormal numbers for zeros: below
+ * 2^-126 what grad holds, or the result, may be lost.
  * Tokens equal to padding_idx (-1: none) or outside 0 .. vocab-1 have no part in it.
  * The tokens are sorted first (stable, so the order of every sum is fixed); a row with many
  * tokens is cut into pieces whose sums are joined in order.

@@ -372,8 +372,8 @@ struct SumArgs {
 };
 
 // A row's sums (V columns at c) to the gradient.  Accumulating into 32 bits is left to the L2
-// cache, which adds without making the walk wait for the old value (one thread has the element, so
-// the order is fixed); bf16 needs the one rounding of old + new and is read, added and written here.
+// cache, which adds without making the walk wait for the old value (one addition per element and call, so
+// the order is fixed; subnormal numbers count as zeros there); bf16 needs the one rounding of old + new and is read, added and written here.
 template <typename GT, int V>
 __device__ __forceinline__ void write_row(const SumArgs &a, int key, int c, float (&acc)[V])
 {

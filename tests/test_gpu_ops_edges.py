@@ -221,3 +221,31 @@ def test_a_stream_of_another_device_is_refused():
         ops.embed(torch.zeros(3, dtype=torch.int64), torch.zeros(4, 8), stream=side)  # tensors on the host
     with ops._on(side, torch.zeros(1, device=DEV)):
         assert torch.cuda.current_stream() == side
+
+
+# --------------------------------------------------------------------------
+# embedding gradient: what is added to is below the normal range
+# --------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("grad_t", [F32, BF16])
+@pytest.mark.parametrize("d", [7, 64])
+@pytest.mark.parametrize("n", [5, 4000])
+def test_embed_grad_added_to_subnormal_values(n, d, grad_t):
+    """Off by less than the least normal number where a token points, the same bits elsewhere; normal results unaffected."""
+    g = T.gen(n + d)
+    vocab, least = 40, 2.0 ** -126
+    base = (T.normal(g, vocab, d) * 2.0 ** -130).to(grad_t)
+    assert bool(((base != 0) & (base.double().abs() < least)).any())
+    tok = torch.randint(0, vocab // 2, (n,), device=DEV, generator=g)
+    dout = T.normal(g, n, d)
+    dout[:, 0] = 0.0
+    dout[:, 1] *= 2.0 ** -128
+    grad = base.clone()
+    ops.embed_grad(tok, dout, grad, accumulate=True)
+    sums = torch.zeros(vocab, d, dtype=torch.float64, device=DEV).index_add_(0, tok, dout.double())
+    mag = torch.zeros_like(sums).index_add_(0, tok, dout.double().abs())
+    want = base.double() + sums
+    # 128 terms in a row and the joins as in embed_grad_check; operand, result and their sum may each lose a subnormal part
+    T.check(grad, want, mag * (128 + n / 256 + 45) * U + want.abs() * T.rounding(grad_t) + 2 * least, "subnormal")
+    assert torch.equal(grad[vocab // 2:], base[vocab // 2:])
