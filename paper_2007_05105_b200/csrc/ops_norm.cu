@@ -251,7 +251,7 @@ template <int E> __device__ __forceinline__ void sigmoids(f2 (&v)[E / 2])
 // The rows of a group in shared memory, kStages at a time: the arrays of a row one after another.  One thread
 // of the group asks for them; a stage is asked for again after a barrier of the group behind its last read.
 // A copy that does not arrive within the wait's bound is given up: the group stops, and its results from that row on
-// become NaN (Lost).
+// become NaN.
 struct Stages {
     char *base;       // the group's
     u64 *full;        // [kStages]
@@ -270,8 +270,8 @@ struct Stages {
     }
 };
 
-// The row at which each group of a block gave up; kNone as a rule.  What follows a group's rows asks for it, so that nothing of
-// it is alive in the walk over them.
+// In the gradient: the row at which each group of a block gave up; kNone as a rule.  What follows a group's rows asks for it, so
+// that nothing of it is alive in the walk over them.  (With NaN written in the walk, kernels of 512 threads spilled 700 bytes for 424.)
 template <int GROUPS> struct Lost {
     static constexpr u64 kNone = ~0ull;
     u64 row[GROUPS];
@@ -331,7 +331,6 @@ __global__ void __launch_bounds__(forward_threads(E, GROUP), 1) k_boundary(const
     extern __shared__ __align__(128) char room[];
     __shared__ __align__(16) float scratch[2][kScratch][2];
     __shared__ u64 full[kStaged ? kMostWarps : 1][kStages];
-    __shared__ Lost<kStaged ? kMostWarps : 1> lost;
     const int mine = kWarp ? threadIdx.x / 32 : 0, groups = kWarp ? blockDim.x / 32 : 1;
     const Place<E, V, FILL> at = place_of<E, V, FILL, GROUP>(a.dim);
     const long long all = (long long)gridDim.x * groups;
@@ -342,7 +341,6 @@ __global__ void __launch_bounds__(forward_threads(E, GROUP), 1) k_boundary(const
     if (kStaged && at.t == 0) {
         for (int s = 0; s < kStages; ++s) mbar_init(stages.full + s, 1);
         mbar_publish();
-        lost.row[mine] = lost.kNone;
     }
     group_barrier<GROUP>();
     griddep_wait();
@@ -371,8 +369,13 @@ __global__ void __launch_bounds__(forward_threads(E, GROUP), 1) k_boundary(const
         const char *px = a.x.row(row), *py = a.y.row(row), *pg = a.gate.row(row);
         if constexpr (kStaged) {
             if (!mbar_wait(stages.full + stage, parity)) {
-                lost.from(mine, row);
                 mbar_wait(stages.full + (stage ^ 1), parity ^ (stage == 1));  // the other copy in flight
+                f2 lost[E / 2];
+                fill<E>(lost, __int_as_float(0x7fffffff));
+                for (; row < a.n; row += all) {
+                    if (a.y.p) write<E, V, FILL>(at, a.x_new.row(row), is_bf16<XT>(a.x_new), lost);
+                    write<E, V, FILL>(at, a.h.row(row), is_bf16<YT>(a.h), lost);
+                }
                 break;
             }
             px = stages.base + stage * stages.bytes;
@@ -436,13 +439,6 @@ __global__ void __launch_bounds__(forward_threads(E, GROUP), 1) k_boundary(const
         }
         write<E, V, FILL>(at, a.h.row(row), is_bf16<YT>(a.h), x);
     }
-    if constexpr (kStaged) {
-        group_barrier<GROUP>();
-        if (lost.row[mine] != lost.kNone) {
-            if (a.y.p) poison(a.x_new, lost.row[mine], a.n, all, a.dim, at.t, GROUP);
-            poison(a.h, lost.row[mine], a.n, all, a.dim, at.t, GROUP);
-        }
-    }
 }
 
 struct GradArgs {
@@ -456,6 +452,20 @@ struct GradArgs {
     unsigned stage_bytes;
     float inv_dim, res_scale, eps;
 };
+
+// NaN as the rows' results of the groups that gave up, and as the block's column sums.
+template <int GROUPS> __device__ __noinline__ void poison(const GradArgs &a, const Lost<GROUPS> &lost)
+{
+    for (int q = 0; q < GROUPS; ++q) {
+        if (lost.row[q] == lost.kNone) continue;
+        const long long step = (long long)gridDim.x * GROUPS;
+        poison(a.dx, lost.row[q], a.n, step, a.dim, threadIdx.x, blockDim.x);
+        poison(a.dy, lost.row[q], a.n, step, a.dim, threadIdx.x, blockDim.x);
+        poison(a.dgate, lost.row[q], a.n, step, a.dim, threadIdx.x, blockDim.x);
+    }
+    const Rows sums = {reinterpret_cast<char *>(a.partial + (long long)blockIdx.x * kSums * a.ld_partial), a.ld_partial * 4LL, 0};
+    poison(sums, 0, kSums, 1, a.dim, threadIdx.x, blockDim.x);
+}
 
 // Every thread keeps the column sums of its columns in registers over all its rows; at the end the
 // warps of a block are added in order, where they are groups, and the block leaves one row of partial
@@ -627,15 +637,7 @@ __global__ void __launch_bounds__(MOST, 1) k_boundary_grad(const __grid_constant
     }
     if constexpr (kStaged) {
         __syncthreads();
-        if (lost.any()) {
-            if (lost.row[mine] != lost.kNone) {
-                const int t = kWarp ? threadIdx.x & 31 : threadIdx.x, threads = kWarp ? 32 : blockDim.x;
-                poison(a.dx, lost.row[mine], a.n, all, a.dim, t, threads);
-                poison(a.dy, lost.row[mine], a.n, all, a.dim, t, threads);
-                poison(a.dgate, lost.row[mine], a.n, all, a.dim, t, threads);
-            }
-            poison({to, a.ld_partial * 4LL, 0}, 0, kSums, 1, a.dim, threadIdx.x, blockDim.x);
-        }
+        if (lost.any()) poison(a, lost);
     }
 }
 
