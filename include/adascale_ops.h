@@ -112,6 +112,7 @@ int64_t adascale_embed_grad_workspace(int64_t n_tokens, int64_t dim);
  * - Masked vocabulary entries may hold -inf or the type's lowest value.  NaN or +inf in a live row
  *   make that row's loss and gradient NaN, and `loss` with it.  NaN or +inf among the teacher's logits of valid
  *   entries makes q NaN: the row's loss, and the gradient of every entry that the list names.
+ * - Probabilities below 2^-126 count as 0, gradients below it may be 0.
  * - dlogits (type of logits) may be NULL: the loss alone.  It may be logits itself (same ld).
  * - teacher_logits and teacher_ids may be NULL when n_top = 0; labels and weight may be NULL.
  */

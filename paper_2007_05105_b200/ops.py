@@ -16,7 +16,7 @@ given for them - a slot of a gradient row, say - or to new ones; workspaces come
 caching allocator.  With another stream than the current one, new tensors belong to that stream, and
 ordering it against the producers of the inputs is the caller's, as everywhere in torch.  The last dimension of every
 matrix is contiguous; rows may have any stride.  There is no fallback and no autograd: gradients
-are calls of their own.  Wrong shapes or types raise ``ValueError``; what the library refuses
+are calls of their own, and results do not require one.  Wrong shapes or types raise ``ValueError``; what the library refuses
 raises ``AdaScaleError``.
 """
 from __future__ import annotations
@@ -151,6 +151,7 @@ def distill(logits, teacher_logits=None, teacher_ids=None, labels=None, T=1.0, a
     (``teacher_logits`` [n, k] at ``teacher_ids`` [n, k]; ids outside the vocabulary, -1 say, fill up short lists) and
     p_T that of ``logits`` over the whole vocabulary, both at temperature T.  Returns ``(loss, row_loss, dlogits)``:
     ``loss`` is the sum of ``row_loss``, ``dlogits`` its gradient in the type of ``logits`` (None without ``want_grad``).
+    (``loss`` and ``row_loss`` are parts of one allocation: a loss that is kept keeps both.)
     ``row_weight`` (float32) holds masks, means and upstream factors; rows of weight 0 are not read.
     ``dlogits`` may be given, also as ``logits`` itself.
     """
