@@ -3,11 +3,14 @@
  * (adascale.h) on one NVIDIA B200 (sm_100a).
  *
  * The step consumes S gradient rows of a model; these calls produce the parts of such a row, and
- * of the training step around it, that are neither a matrix product nor attention:
+ * of the training step around it, that a library's matrix products and attention do not:
  *
  *   adascale_embed, adascale_embed_grad            token table: scaled lookup, gradient by sorted tokens
  *   adascale_distill                               loss against a teacher's top logits, with its gradient
  *   adascale_residual_norm, ..._residual_norm_grad block boundary: norm, gate, residual scale, norm
+ *   adascale_position_softmax, ..._grad            attention weights with a relative position bias by buckets
+ *   adascale_expert_matmul, ..._grad               products with experts' weights over ragged groups of rows
+ *   adascale_clip_grads                            global norm of many gradients, clipping on the way into a row's slots
  *
  * Conventions (those of adascale.h, and)
  *   - Every call takes one struct of arguments (host pointer, read during the call) and a
@@ -45,6 +48,11 @@ typedef enum { ADASCALE_I32 = 0, ADASCALE_I64 = 1 } adascale_itype; /* token ids
 #define ADASCALE_EMBED_MAX_DIM 1073741824LL /* width of a token table */
 #define ADASCALE_DISTILL_MAX_K 1024        /* entries of a teacher's list */
 #define ADASCALE_NORM_MAX_DIM 16384        /* width of a block boundary */
+#define ADASCALE_POSITION_MAX_BUCKETS 128  /* buckets of relative positions */
+#define ADASCALE_POSITION_MAX_DISTANCE 16384 /* distance from which on all are in the last bucket */
+#define ADASCALE_EXPERT_MAX_EXPERTS 1024   /* experts of one product */
+#define ADASCALE_EXPERT_MAX_DIM 1048576    /* width of an expert's input or output */
+#define ADASCALE_CLIP_MAX_TENSORS 65536    /* gradients of one norm */
 
 /*
  * out[n, :] = scale * table[token[n], :].  A token outside 0 .. vocab-1 gives a row of zeros (and
@@ -201,6 +209,150 @@ typedef struct {
 } adascale_residual_norm_grad_args;
 adascale_status adascale_residual_norm_grad(const adascale_residual_norm_grad_args *args, void *cuda_stream);
 int64_t adascale_residual_norm_grad_workspace(int64_t n_rows, int64_t dim);
+
+/*
+ * Attention weights from scores, with a learned bias by relative position.  For batch b, head h, query i at position
+ * start[b] + i, key j at position j:
+ *
+ *   p[b,h,i,j] = softmax over the live keys j of  scale * s[b,h,i,j] + table[bucket(j - (start[b] + i)), h]
+ *
+ * Live are the keys with j < length[b] and, if causal, j <= start[b] + i.  Others get 0, whatever the scores hold there (they
+ * are not used); a query without live keys, or whose live keys all have -inf, gets zeros.  NaN or +inf at a live key makes
+ * its query's row NaN (at the live keys).  scale * s + bias is 32-bit arithmetic: the type's lowest value swallows the bias.
+ *
+ * Buckets: with m = n_buckets (half of them if bidirectional), e = m / 2 and n = |distance| (not bidirectional: the distance
+ * back, 0 for keys ahead), n < e has bucket n, and n >= e the bucket e + floor((m - e) log(n / e) / log(max_distance / e)),
+ * m - 1 at most, without rounding: a distance that lies on a border belongs to the bucket above it.  Bidirectional: keys ahead
+ * have m more.  n_buckets is even and at least 4 if bidirectional, at least 2 otherwise; max_distance > e.
+ *
+ * probs may be scores itself (same strides).  Strides are in elements and may be 0 for inputs; rows of probs do not overlap; the
+ * keys of a row are adjacent.  n_queries and n_keys are at most 2^29.  lengths and starts are clamped: to 0 .. n_keys and to
+ * +-2^30.  Weights below 2^-126 may be 0.
+ */
+typedef struct {
+    const void *scores;  /* [batch, heads, n_queries, n_keys] of dtype */
+    void *probs;         /* the same, of dtype */
+    const float *table;  /* [n_buckets, heads] */
+    const void *lengths; /* [batch] of length_type, or NULL (n_keys) */
+    const void *starts;  /* [batch] of start_type, or NULL (0) */
+    int64_t batch, heads, n_queries, n_keys;
+    int64_t scores_stride_b, scores_stride_h, scores_stride_q;
+    int64_t probs_stride_b, probs_stride_h, probs_stride_q;
+    int64_t ld_table;
+    int32_t dtype;
+    int32_t length_type, start_type; /* adascale_itype */
+    int32_t n_buckets, max_distance, bidirectional, causal;
+    float scale;
+} adascale_position_softmax_args;
+adascale_status adascale_position_softmax(const adascale_position_softmax_args *args, void *cuda_stream);
+
+/*
+ * Its gradient from the weights p of the forward call and dp arriving at them; lengths, starts and causal as there:
+ *
+ *   g = p (dp - sum over the live j of p dp),   dscores = scale * g
+ *   dtable[k, h] (+)= sum of g over all b, i and live j in bucket k, written in wgrad_dtype
+ *
+ * Keys that are not live get 0 and are not used.  Without `accumulate` dtable is written, with it the sums are added to what it
+ * holds (a table that several layers share).  dscores may be dprobs or probs itself (same strides).  dscores or dtable may be
+ * NULL.  workspace: at least adascale_position_softmax_grad_workspace(heads, n_buckets) bytes, 16-byte aligned, contents
+ * neither expected nor kept.
+ */
+typedef struct {
+    const void *probs, *dprobs; /* [batch, heads, n_queries, n_keys] of dtype */
+    void *dscores;              /* the same, or NULL */
+    void *dtable;               /* [n_buckets, heads] of wgrad_dtype, or NULL */
+    const void *lengths;        /* [batch] of length_type, or NULL */
+    const void *starts;         /* [batch] of start_type, or NULL */
+    void *workspace;
+    int64_t workspace_bytes;
+    int64_t batch, heads, n_queries, n_keys;
+    int64_t probs_stride_b, probs_stride_h, probs_stride_q;
+    int64_t dprobs_stride_b, dprobs_stride_h, dprobs_stride_q;
+    int64_t dscores_stride_b, dscores_stride_h, dscores_stride_q;
+    int64_t ld_dtable;
+    int32_t dtype, wgrad_dtype;
+    int32_t length_type, start_type; /* adascale_itype */
+    int32_t n_buckets, max_distance, bidirectional, causal;
+    int32_t accumulate;
+    float scale;
+} adascale_position_softmax_grad_args;
+adascale_status adascale_position_softmax_grad(const adascale_position_softmax_grad_args *args, void *cuda_stream);
+int64_t adascale_position_softmax_grad_workspace(int64_t heads, int64_t n_buckets);
+
+/*
+ * Products with experts' weights over ragged groups of rows: for the rows r of expert e, offsets[e] <= r < offsets[e + 1],
+ *
+ *   y[r, :] = w[e] x[r, :]
+ *
+ * x and w are bf16; sums are 32-bit (tensor cores), y is rounded once.  offsets has n_experts + 1 ascending numbers on the device;
+ * rows before the first or behind the last, up to n_rows, are neither used nor written.  Offsets outside 0 .. n_rows are
+ * clamped, and one below an earlier one counts as that.  An expert may have no rows.
+ * The rows of x and w start on 16-byte boundaries (ALIGNMENT otherwise): strides are multiples of 8 elements.  Widths may be odd.
+ */
+typedef struct {
+    const void *x;       /* [n_rows, in_dim] of bf16 */
+    const void *w;       /* [n_experts, out_dim, in_dim] of bf16 */
+    void *y;             /* [n_rows, out_dim] of y_dtype */
+    const void *offsets; /* [n_experts + 1] of offset_type */
+    int64_t n_rows, n_experts, in_dim, out_dim;
+    int64_t ld_x, ld_w, stride_w, ld_y; /* stride_w: from expert to expert */
+    int32_t offset_type;                /* adascale_itype */
+    int32_t y_dtype;
+} adascale_expert_matmul_args;
+adascale_status adascale_expert_matmul(const adascale_expert_matmul_args *args, void *cuda_stream);
+
+/*
+ * Its gradients from dy [n_rows, out_dim] of bf16:
+ *
+ *   dx[r, :] = w[e]^T dy[r, :]                          for the rows r of expert e
+ *   dw[e]  (+)= sum over the rows r of e of dy[r, :] x[r, :]^T     in dw_dtype
+ *
+ * Without `accumulate` all of dw is written, zeros for experts without rows; with it the sums are added to what dw holds and
+ * experts without rows are not touched.  w = NULL leaves dx out, x = NULL dw.  Rows of dy, x and w start on
+ * 16-byte boundaries.
+ */
+typedef struct {
+    const void *dy;      /* [n_rows, out_dim] of bf16 */
+    const void *x;       /* [n_rows, in_dim] of bf16, or NULL (no dw) */
+    const void *w;       /* [n_experts, out_dim, in_dim] of bf16, or NULL (no dx) */
+    void *dx;            /* [n_rows, in_dim] of dx_dtype */
+    void *dw;            /* [n_experts, out_dim, in_dim] of dw_dtype */
+    const void *offsets; /* [n_experts + 1] of offset_type */
+    int64_t n_rows, n_experts, in_dim, out_dim;
+    int64_t ld_dy, ld_x, ld_w, stride_w, ld_dx, ld_dw, stride_dw;
+    int32_t offset_type; /* adascale_itype */
+    int32_t dx_dtype, dw_dtype, accumulate;
+} adascale_expert_matmul_grad_args;
+adascale_status adascale_expert_matmul_grad(const adascale_expert_matmul_grad_args *args, void *cuda_stream);
+
+/*
+ * Global 2-norm of many gradients, and clipping by it:
+ *
+ *   norm = sqrt(sum over all tensors and elements of g^2)
+ *   out  = c g,   c = min(1, max_norm / (norm + eps))
+ *
+ * grads, out, numels, grad_dtypes and out_dtypes are HOST arrays of n_tensors entries, read during the call: device
+ * addresses, element counts (0 is allowed, its addresses are not looked at) and adascale_dtype of each tensor, whose elements are
+ * adjacent.  out = NULL: the norm alone.  out[k] may be grads[k] itself with the same type (if c = 1 nothing is written
+ * then); otherwise it overlaps neither another output nor a gradient.  No output may be given twice.
+ * Sums are 64-bit joins of 32-bit sums of a few terms; where squares leave the 32-bit range they are 64-bit throughout.  A NaN
+ * anywhere makes norm and all of out NaN; with an infinity and no NaN norm is inf, c 0, and out 0, NaN in the infinity's place.
+ * workspace: at least adascale_clip_grads_workspace(n_tensors) bytes, 16-byte aligned, contents neither expected nor kept.
+ */
+typedef struct {
+    const void *const *grads;
+    void *const *out;           /* or NULL */
+    const int64_t *numels;
+    const int32_t *grad_dtypes; /* adascale_dtype of each */
+    const int32_t *out_dtypes;  /* of each; NULL with out = NULL */
+    float *norm;                /* [1] */
+    void *workspace;
+    int64_t workspace_bytes;
+    int64_t n_tensors;
+    float max_norm, eps;        /* finite, >= 0; only with out */
+} adascale_clip_grads_args;
+adascale_status adascale_clip_grads(const adascale_clip_grads_args *args, void *cuda_stream);
+int64_t adascale_clip_grads_workspace(int64_t n_tensors);
 
 #ifdef __cplusplus
 }

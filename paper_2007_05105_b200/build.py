@@ -8,7 +8,8 @@ import sys
 import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-_SOURCE_NAMES = ("adascale.cu", "ops_embed.cu", "ops_distill.cu", "ops_norm.cu")
+_SOURCE_NAMES = ("adascale.cu", "ops_embed.cu", "ops_distill.cu", "ops_norm.cu", "ops_position.cu", "ops_expert.cu",
+                 "ops_clip.cu")
 SOURCES = [os.path.join(_HERE, "csrc", name) for name in _SOURCE_NAMES]
 HEADERS = [os.path.join(os.path.dirname(_HERE), "include", name) for name in ("adascale.h", "adascale_ops.h")] + \
           [os.path.join(_HERE, "csrc", name) for name in ("adascale_kernels.cuh", "ops_common.cuh")]

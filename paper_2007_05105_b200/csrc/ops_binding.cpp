@@ -500,8 +500,310 @@ PyObject *residual_norm_grad(PyObject *const *o)
                          wrap(dw_pre), wrap_or_none(db_pre));
 }
 
+// Strides of batch, head and query of a [batch, heads, queries, keys] tensor of the type and shape of `like`.
+struct Scores {
+    void *p = nullptr;
+    int64_t b = 0, h = 0, q = 0;
+};
+Scores scores_of(const at::Tensor &t, const at::Tensor &like, const char *what)
+{
+    if (t.device() != like.device()) refuse("%s is on %s, not on %s", what, t.device().str().c_str(), like.device().str().c_str());
+    if (t.dim() != 4 || t.sizes() != like.sizes()) refuse("%s: a [batch, heads, queries, keys] tensor, the same for all, is expected", what);
+    same_type(t, like.scalar_type(), what);
+    if (t.size(3) > 1 && t.stride(3) != 1) refuse("%s: the last dimension is not contiguous", what);
+    return {t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
+}
+const void *ids_of(const at::Tensor *t, int64_t n, at::Device device, const char *what, int32_t &type)
+{
+    if (!t) return nullptr;
+    type = id_code(t->scalar_type(), what);
+    return vector(*t, n, device, what);
+}
+int32_t flag32(PyObject *o, const char *what)
+{
+    const int64_t v = whole(o, what);
+    if (v < INT32_MIN || v > INT32_MAX) refuse("%s: %lld is out of range", what, (long long)v);
+    return (int32_t)v;
+}
+
+// scores, table, max_distance, bidirectional, scale, causal, lengths, starts, out
+PyObject *position_softmax(PyObject *const *o)
+{
+    const at::Tensor &scores = wanted(o[0], "scores"), &table = wanted(o[1], "table");
+    if (!scores.is_cuda()) refuse("scores: the operators take CUDA tensors");
+    const at::Device device = scores.device();
+    const c10::cuda::CUDAGuard guard(device);
+    const at::Tensor *given = tensor(o[8], "out");
+    adascale_position_softmax_args a = {};
+    a.dtype = float_code(scores.scalar_type(), "scores");
+    Scores m = scores_of(scores, scores, "scores");
+    a.scores = m.p;
+    a.scores_stride_b = m.b, a.scores_stride_h = m.h, a.scores_stride_q = m.q;
+    a.batch = scores.size(0), a.heads = scores.size(1), a.n_queries = scores.size(2), a.n_keys = scores.size(3);
+    if (table.scalar_type() != at::kFloat) refuse("table: %s is not float32", c10::toString(table.scalar_type()));
+    if (table.dim() != 2 || table.size(1) != a.heads) refuse("table: [buckets, %lld] is expected", (long long)a.heads);
+    if (table.size(0) > INT32_MAX) refuse("table: too many buckets");
+    const Matrix rows = matrix(table, table.size(0), a.heads, device, "table");
+    a.table = static_cast<const float *>(rows.p);
+    a.ld_table = rows.ld;
+    a.n_buckets = (int32_t)table.size(0);
+    a.max_distance = flag32(o[2], "max_distance");
+    a.bidirectional = truth(o[3]);
+    a.scale = (float)number(o[4], "scale");
+    a.causal = truth(o[5]);
+    a.lengths = ids_of(tensor(o[6], "lengths"), a.batch, device, "lengths", a.length_type);
+    a.starts = ids_of(tensor(o[7], "starts"), a.batch, device, "starts", a.start_type);
+    const at::Tensor probs = given_or_new(given, scores.sizes(), scores.scalar_type(), device, "out");
+    m = scores_of(probs, scores, "out");
+    a.probs = m.p;
+    a.probs_stride_b = m.b, a.probs_stride_h = m.h, a.probs_stride_q = m.q;
+    const adascale_status s = adascale_position_softmax(&a, stream_of(device));
+    if (s != ADASCALE_OK) return status_error(s);
+    written(given);
+    return wrap(probs);
+}
+
+// probs, dprobs, num_buckets, max_distance, bidirectional, scale, causal, lengths, starts, wgrad_dtype, accumulate, want_dscores,
+// want_dtable, dscores, dtable, workspace
+PyObject *position_softmax_grad(PyObject *const *o)
+{
+    const at::Tensor &probs = wanted(o[0], "probs"), &dprobs = wanted(o[1], "dprobs");
+    if (!probs.is_cuda()) refuse("probs: the operators take CUDA tensors");
+    const at::Device device = probs.device();
+    const c10::cuda::CUDAGuard guard(device);
+    const at::Tensor *given_s = tensor(o[13], "dscores"), *given_t = tensor(o[14], "dtable");
+    adascale_position_softmax_grad_args a = {};
+    a.dtype = float_code(probs.scalar_type(), "probs");
+    Scores m = scores_of(probs, probs, "probs");
+    a.probs = m.p;
+    a.probs_stride_b = m.b, a.probs_stride_h = m.h, a.probs_stride_q = m.q;
+    m = scores_of(dprobs, probs, "dprobs");
+    a.dprobs = m.p;
+    a.dprobs_stride_b = m.b, a.dprobs_stride_h = m.h, a.dprobs_stride_q = m.q;
+    a.batch = probs.size(0), a.heads = probs.size(1), a.n_queries = probs.size(2), a.n_keys = probs.size(3);
+    a.n_buckets = flag32(o[2], "num_buckets");
+    a.max_distance = flag32(o[3], "max_distance");
+    a.bidirectional = truth(o[4]);
+    a.scale = (float)number(o[5], "scale");
+    a.causal = truth(o[6]);
+    a.lengths = ids_of(tensor(o[7], "lengths"), a.batch, device, "lengths", a.length_type);
+    a.starts = ids_of(tensor(o[8], "starts"), a.batch, device, "starts", a.start_type);
+    a.accumulate = truth(o[10]);
+    at::Tensor dscores, dtable;
+    if (given_s || truth(o[11])) {
+        dscores = given_or_new(given_s, probs.sizes(), probs.scalar_type(), device, "dscores");
+        m = scores_of(dscores, probs, "dscores");
+        a.dscores = m.p;
+        a.dscores_stride_b = m.b, a.dscores_stride_h = m.h, a.dscores_stride_q = m.q;
+    }
+    std::optional<Room> room;
+    if (given_t || truth(o[12])) {
+        if (a.accumulate && !given_t) refuse("dtable: there is nothing to add to");
+        if (a.n_buckets < 1 || a.n_buckets > ADASCALE_POSITION_MAX_BUCKETS) refuse("num_buckets: %d is not within 2 .. %d", a.n_buckets, ADASCALE_POSITION_MAX_BUCKETS);
+        if (given_t && given_t->dim() != 2) refuse("dtable: [%d, %lld] is expected", a.n_buckets, (long long)a.heads);
+        dtable = given_t ? *given_t : make({a.n_buckets, a.heads}, type_of(o[9], at::kFloat), device);
+        a.wgrad_dtype = float_code(dtable.scalar_type(), "dtable");
+        const Matrix rows = matrix(dtable, a.n_buckets, a.heads, device, "dtable");
+        a.dtable = rows.p;
+        a.ld_dtable = rows.ld;
+        room.emplace(o[15], adascale_position_softmax_grad_workspace(a.heads, a.n_buckets), device);
+        a.workspace = room->p;
+        a.workspace_bytes = room->bytes;
+    }
+    const adascale_status s = adascale_position_softmax_grad(&a, stream_of(device));
+    if (s != ADASCALE_OK) return status_error(s);
+    written(given_s);
+    written(given_t);
+    return Py_BuildValue("(NN)", wrap_or_none(dscores), wrap_or_none(dtable));
+}
+
+// Experts' weights, or their gradient: address, row stride, expert stride.
+struct Weights {
+    void *p = nullptr;
+    int64_t ld = 0, stride = 0;
+};
+Weights weights_of(const at::Tensor &t, int64_t experts, int64_t out, int64_t in, at::Device device, const char *what)
+{
+    if (t.device() != device) refuse("%s is on %s, not on %s", what, t.device().str().c_str(), device.str().c_str());
+    if (t.dim() != 3 || t.size(0) != experts || t.size(1) != out || t.size(2) != in)
+        refuse("%s: [%lld, %lld, %lld] is expected", what, (long long)experts, (long long)out, (long long)in);
+    if (in > 1 && t.stride(2) != 1) refuse("%s: the last dimension is not contiguous", what);
+    return {t.data_ptr(), out > 1 ? t.stride(1) : (in + 7) / 8 * 8, experts > 1 ? t.stride(0) : out * ((in + 7) / 8 * 8)};
+}
+void want_bf16(const at::Tensor &t, const char *what) { same_type(t, at::kBFloat16, what); }
+
+// x, w, offsets, out, out_dtype
+PyObject *expert_matmul(PyObject *const *o)
+{
+    const at::Tensor &x = wanted(o[0], "x"), &w = wanted(o[1], "w"), &offsets = wanted(o[2], "offsets");
+    if (!x.is_cuda() || x.dim() != 2) refuse("x: a [rows, in] matrix on a CUDA device is expected");
+    if (w.dim() != 3) refuse("w: [experts, out, in] is expected");
+    const at::Device device = x.device();
+    const c10::cuda::CUDAGuard guard(device);
+    want_bf16(x, "x");
+    want_bf16(w, "w");
+    const at::Tensor *given = tensor(o[3], "out");
+    const at::ScalarType type = type_of(o[4], given ? given->scalar_type() : at::kBFloat16);
+    adascale_expert_matmul_args a = {};
+    a.n_rows = x.size(0), a.in_dim = x.size(1), a.n_experts = w.size(0), a.out_dim = w.size(1);
+    a.y_dtype = float_code(type, "out");
+    Matrix m = matrix(x, a.n_rows, a.in_dim, device, "x");
+    a.x = m.p;
+    a.ld_x = m.ld;
+    const Weights u = weights_of(w, a.n_experts, a.out_dim, a.in_dim, device, "w");
+    a.w = u.p;
+    a.ld_w = u.ld, a.stride_w = u.stride;
+    a.offsets = ids_of(&offsets, a.n_experts + 1, device, "offsets", a.offset_type);
+    const at::Tensor y = given_or_new(given, {a.n_rows, a.out_dim}, type, device, "out");
+    m = matrix(y, a.n_rows, a.out_dim, device, "out");
+    a.y = m.p;
+    a.ld_y = m.ld;
+    const adascale_status s = adascale_expert_matmul(&a, stream_of(device));
+    if (s != ADASCALE_OK) return status_error(s);
+    written(given);
+    return wrap(y);
+}
+
+// dy, offsets, x, w, dx_dtype, wgrad_dtype, accumulate, dx, dw
+PyObject *expert_matmul_grad(PyObject *const *o)
+{
+    const at::Tensor &dy = wanted(o[0], "dy"), &offsets = wanted(o[1], "offsets");
+    const at::Tensor *x = tensor(o[2], "x"), *w = tensor(o[3], "w"), *given_x = tensor(o[7], "dx"), *given_w = tensor(o[8], "dw");
+    if (!dy.is_cuda() || dy.dim() != 2) refuse("dy: a [rows, out] matrix on a CUDA device is expected");
+    if (!x && !w) refuse("x (for dw) or w (for dx) is needed");
+    if (offsets.numel() < 2) refuse("offsets: one more than the experts are expected");
+    const at::Device device = dy.device();
+    const c10::cuda::CUDAGuard guard(device);
+    want_bf16(dy, "dy");
+    adascale_expert_matmul_grad_args a = {};
+    a.n_rows = dy.size(0), a.out_dim = dy.size(1), a.n_experts = offsets.numel() - 1;
+    if (x && x->dim() != 2) refuse("x: a [rows, in] matrix is expected");
+    if (w && w->dim() != 3) refuse("w: [experts, out, in] is expected");
+    a.in_dim = x ? x->size(1) : w->size(2);
+    a.accumulate = truth(o[6]);
+    a.offsets = ids_of(&offsets, a.n_experts + 1, device, "offsets", a.offset_type);
+    Matrix m = matrix(dy, a.n_rows, a.out_dim, device, "dy");
+    a.dy = m.p;
+    a.ld_dy = m.ld;
+    at::Tensor dx, dw;
+    if (w) {
+        want_bf16(*w, "w");
+        const Weights u = weights_of(*w, a.n_experts, a.out_dim, a.in_dim, device, "w");
+        a.w = u.p;
+        a.ld_w = u.ld, a.stride_w = u.stride;
+        dx = given_or_new(given_x, {a.n_rows, a.in_dim}, type_of(o[4], given_x ? given_x->scalar_type() : at::kBFloat16), device, "dx");
+        a.dx_dtype = float_code(dx.scalar_type(), "dx");
+        m = matrix(dx, a.n_rows, a.in_dim, device, "dx");
+        a.dx = m.p;
+        a.ld_dx = m.ld;
+    }
+    if (x) {
+        want_bf16(*x, "x");
+        m = matrix(*x, a.n_rows, a.in_dim, device, "x");
+        a.x = m.p;
+        a.ld_x = m.ld;
+        if (a.accumulate && !given_w) refuse("dw: there is nothing to add to");
+        dw = given_or_new(given_w, {a.n_experts, a.out_dim, a.in_dim}, type_of(o[5], given_w ? given_w->scalar_type() : at::kFloat), device, "dw");
+        a.dw_dtype = float_code(dw.scalar_type(), "dw");
+        const Weights u = weights_of(dw, a.n_experts, a.out_dim, a.in_dim, device, "dw");
+        a.dw = u.p;
+        a.ld_dw = u.ld, a.stride_dw = u.stride;
+    }
+    const adascale_status s = adascale_expert_matmul_grad(&a, stream_of(device));
+    if (s != ADASCALE_OK) return status_error(s);
+    if (w) written(given_x);
+    if (x) written(given_w);
+    return Py_BuildValue("(NN)", wrap_or_none(dx), wrap_or_none(dw));
+}
+
+// Tensors of a list or tuple.
+class List {
+  public:
+    List(PyObject *o, const char *what) : what_(what), fast_(PySequence_Fast(o, ""))
+    {
+        if (fast_) return;
+        PyErr_Clear();
+        throw Refused{PyExc_TypeError, std::string(what) + " is not a list of tensors"};
+    }
+    ~List() { Py_XDECREF(fast_); }
+    List(const List &) = delete;
+    List &operator=(const List &) = delete;
+    Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(fast_); }
+    const at::Tensor &operator[](Py_ssize_t i) const { return wanted(PySequence_Fast_GET_ITEM(fast_, i), what_); }
+
+  private:
+    const char *what_;
+    PyObject *fast_;
+};
+
+// grads, max_norm (None: the norm alone), out, eps, workspace
+PyObject *clip_grads(PyObject *const *o)
+{
+    const List grads(o[0], "grads");
+    const bool clip = o[1] != Py_None;
+    std::optional<List> out;
+    if (o[2] != Py_None) out.emplace(o[2], "out");
+    const Py_ssize_t n = grads.size();
+    if (n == 0) refuse("grads: the list is empty");
+    if (out && out->size() != n) refuse("out: %zd tensors for %zd gradients", out->size(), n);
+    const at::Device device = grads[0].device();
+    if (!device.is_cuda()) refuse("grads: the operators take CUDA tensors");
+    const c10::cuda::CUDAGuard guard(device);
+    c10::SmallVector<const void *, 64> from;
+    c10::SmallVector<void *, 64> to;
+    c10::SmallVector<int64_t, 64> numels;
+    c10::SmallVector<int32_t, 64> from_types, to_types;
+    for (Py_ssize_t k = 0; k < n; ++k) {
+        const at::Tensor &g = grads[k];
+        if (g.device() != device) refuse("grads[%zd] is on %s, not on %s", k, g.device().str().c_str(), device.str().c_str());
+        if (!g.is_non_overlapping_and_dense()) refuse("grads[%zd]: its elements are not adjacent", k);
+        from.push_back(g.data_ptr());
+        numels.push_back(g.numel());
+        from_types.push_back(float_code(g.scalar_type(), "grads"));
+        if (!clip) continue;
+        if (!out) {
+            to.push_back(g.data_ptr());
+            to_types.push_back(from_types.back());
+            continue;
+        }
+        const at::Tensor &t = (*out)[k];
+        if (t.device() != device) refuse("out[%zd] is on %s, not on %s", k, t.device().str().c_str(), device.str().c_str());
+        if (t.sizes() != g.sizes()) refuse("out[%zd]: its shape is not the gradient's", k);
+        // the same order in memory (strides of dimensions of size 1 say nothing)
+        bool same = t.is_non_overlapping_and_dense();
+        if (g.numel() > 1)
+            for (int64_t d = 0; d < g.dim(); ++d) same &= g.size(d) == 1 || t.stride(d) == g.stride(d);
+        if (!same) refuse("out[%zd]: its elements are not in the gradient's order", k);
+        to.push_back(t.data_ptr());
+        to_types.push_back(float_code(t.scalar_type(), "out"));
+    }
+    adascale_clip_grads_args a = {};
+    a.n_tensors = n;
+    a.grads = from.data();
+    a.numels = numels.data();
+    a.grad_dtypes = from_types.data();
+    if (clip) {
+        a.out = to.data();
+        a.out_dtypes = to_types.data();
+        a.max_norm = (float)number(o[1], "max_norm");
+        a.eps = (float)number(o[3], "eps");
+    }
+    const at::Tensor norm = make({}, at::kFloat, device);
+    a.norm = static_cast<float *>(norm.data_ptr());
+    const Room room(o[4], adascale_clip_grads_workspace(n), device);
+    a.workspace = room.p;
+    a.workspace_bytes = room.bytes;
+    const adascale_status s = adascale_clip_grads(&a, stream_of(device));
+    if (s != ADASCALE_OK) return status_error(s);
+    if (clip)
+        for (Py_ssize_t k = 0; k < n; ++k) written(out ? &(*out)[k] : &grads[k]);
+    return wrap(norm);
+}
+
 #define ENTRY(name, count) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(&entry<name, count>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(embed, 5), ENTRY(embed_grad, 7), ENTRY(distill, 10), ENTRY(residual_norm, 13), ENTRY(residual_norm_grad, 21),
+                         ENTRY(position_softmax, 9), ENTRY(position_softmax_grad, 16), ENTRY(expert_matmul, 5), ENTRY(expert_matmul_grad, 9),
+                         ENTRY(clip_grads, 5),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,267 @@
+"""Products with experts' weights over ragged groups of rows, and their gradients, against 64-bit products.
+
+Tolerances: operands are bf16, so every product of two is exact in 32 bits.  The tensor cores add in 32 bits, each addition off
+by at most one unit in the last place (2u = 2^-23, as they may cut instead of round) of what is being added up, m summands by
+2 m u at most of the sum of the terms' magnitudes; errors of that many additions of either sign stay far below, so that bound is
+never near.  Storing adds u (float32) or 2^-8 (bfloat16) of the value, adding to what a gradient holds another u.
+"""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("needs a CUDA device", allow_module_level=True)
+
+from paper_2007_05105_b200 import ops  # noqa: E402
+from paper_2007_05105_b200.binding import AdaScaleError  # noqa: E402
+from test_gpu_ops import BF16, DEV, F32, U, check, gen, normal, rounding, strided  # noqa: E402
+
+
+def offsets_of(counts, first=0, ids=torch.int32):
+    return torch.tensor([first] + counts, device=DEV).cumsum(0).to(ids)
+
+
+def padded(t, pad):
+    """The same values with rows 8 * pad elements further apart."""
+    if not pad:
+        return t
+    wide = torch.full((*t.shape[:-1], (t.shape[-1] + 7) // 8 * 8 + 8 * pad), float("nan"), dtype=t.dtype, device=DEV)
+    wide[..., :t.shape[-1]] = t
+    return wide[..., :t.shape[-1]]
+
+
+def aligned(t):
+    """The same values in rows that start on 16-byte boundaries."""
+    return t if t.shape[-1] % 8 == 0 else padded(t, 1)
+
+
+def groups(offsets):
+    o = offsets.tolist()
+    return [(e, o[e], o[e + 1]) for e in range(len(o) - 1)]
+
+
+def forward_check(x, w, offsets, y, before, what):
+    want, mag = before.double(), torch.zeros(y.shape, dtype=torch.float64, device=DEV)
+    for e, lo, hi in groups(offsets):
+        want[lo:hi] = x[lo:hi].double() @ w[e].double().t()
+        mag[lo:hi] = x[lo:hi].double().abs() @ w[e].double().abs().t()
+    check(y, want, 2 * x.shape[1] * U * mag + rounding(y.dtype) * want.abs() * 1.01, what)
+
+
+SHAPES = [  # rows of each expert, rows before the first and behind the last, in, out
+    ([1], 0, 0, 8, 8),
+    ([5], 0, 0, 64, 128),
+    ([3, 0, 17, 1], 2, 5, 72, 40),
+    ([0, 0, 33, 0], 0, 0, 264, 136),
+    ([130, 7, 0, 255, 64], 0, 31, 136, 200),
+    ([257, 512, 1, 300], 9, 0, 512, 264),
+    ([700, 900], 0, 77, 1032, 520),
+    ([1] * 70 + [0] * 9 + [2] * 50, 0, 0, 128, 64),
+    ([40, 41], 0, 0, 13, 9),
+    ([600, 100], 0, 3, 77, 301),
+]
+
+
+@pytest.mark.parametrize("out_t", [BF16, F32])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_products(shape, out_t):
+    counts, first, tail, k, m = shape
+    n = first + sum(counts) + tail
+    g = gen(n + k)
+    x, w = aligned(normal(g, n, k, dtype=BF16)), aligned(normal(g, len(counts), m, k, dtype=BF16))
+    offsets = offsets_of(counts, first)
+    before = normal(g, n, m, dtype=out_t)
+    y, intact = strided(before, 3, 1)
+    assert ops.expert_matmul(x, w, offsets, out=y) is y
+    forward_check(x, w, offsets, y, before, "products")
+    intact()
+
+
+@pytest.mark.parametrize("dx_t,dw_t,accumulate", [(BF16, F32, False), (F32, BF16, False), (BF16, F32, True), (F32, BF16, True)])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_gradients(shape, dx_t, dw_t, accumulate):
+    counts, first, tail, k, m = shape
+    n = first + sum(counts) + tail
+    g = gen(n + k + 1)
+    x, w = aligned(normal(g, n, k, dtype=BF16)), aligned(normal(g, len(counts), m, k, dtype=BF16))
+    dy = aligned(normal(g, n, m, dtype=BF16))
+    x[:first], dy[:first] = float("nan"), float("inf")  # what no expert has is not used
+    x[n - tail:], dy[n - tail:] = float("nan"), float("nan")
+    offsets = offsets_of(counts, first, torch.int64)
+    dx0, dw0 = normal(g, n, k, dtype=dx_t), normal(g, len(counts), m, k, dtype=dw_t)
+    dx, dx_intact = strided(dx0, 1, 3)
+    flat, dw_intact = strided(dw0.view(1, -1), 0, 64)
+    dw = flat.view(len(counts), m, k)
+    got = ops.expert_matmul_grad(dy, offsets, x=x, w=w, dx=dx, dw=dw, accumulate=accumulate)
+    assert got.dx is dx and got.dw is dw
+    want, mag = dx0.double(), torch.zeros(n, k, dtype=torch.float64, device=DEV)
+    for e, lo, hi in groups(offsets):
+        want[lo:hi] = dy[lo:hi].double() @ w[e].double()
+        mag[lo:hi] = dy[lo:hi].double().abs() @ w[e].double().abs()
+        part = dy[lo:hi].double().t() @ x[lo:hi].double()
+        terms = dy[lo:hi].double().abs().t() @ x[lo:hi].double().abs()
+        whole = part + dw0[e].double() if accumulate else part
+        check(dw[e], whole, 2 * max(hi - lo, 1) * U * terms + U * whole.abs() + rounding(dw_t) * whole.abs() * 1.01, "dw of %d" % e)
+    check(dx, want, 2 * m * U * mag + rounding(dx_t) * want.abs() * 1.01, "dx")
+    dx_intact()
+    dw_intact()
+
+
+def test_against_differences():
+    """The gradients of a weighted sum of results against that sum's own differences: exact steps, so that only the sum's
+    rounding is between them."""
+    counts, k, m = [3, 0, 20], 24, 16
+    g = gen(5)
+    n = sum(counts)
+    whole = lambda *s: torch.randint(-4, 5, s, device=DEV, generator=g).to(BF16)  # noqa: E731
+    x, w, dy, offsets = whole(n, k), whole(3, m, k), whole(n, m), offsets_of(counts)
+    loss = lambda x, w: float((ops.expert_matmul(x, w, offsets, out_dtype=F32).double() * dy.double()).sum())  # noqa: E731
+    got = ops.expert_matmul_grad(dy, offsets, x=x, w=w, dx_dtype=F32)
+    for at in [(0, 0), (2, 23), (3, 7), (22, 11)]:  # whole numbers below 2^24: no rounding at all
+        x2 = x.clone()
+        x2[at] += 1
+        assert loss(x2, w) - loss(x, w) == float(got.dx[at])
+    for at in [(0, 0, 0), (1, 3, 3), (2, 15, 23)]:
+        w2 = w.clone()
+        w2[at] += 1
+        assert loss(x, w2) - loss(x, w) == float(got.dw[at])
+
+
+@pytest.mark.parametrize("rows", [1, 2, 16, 31, 32, 33, 64, 127, 128, 129, 255, 256, 257, 400])
+def test_every_width_of_a_tile(rows):
+    g = gen(rows)
+    x, w, dy = normal(g, rows + 3, 192, dtype=BF16), normal(g, 2, 130, 192, dtype=BF16), normal(g, rows + 3, 130, dtype=BF16)
+    dy = aligned(dy)
+    offsets = offsets_of([rows, 2])
+    before = torch.full((rows + 3, 130), 7.0, device=DEV)
+    y = ops.expert_matmul(x, w, offsets, out=before.clone())
+    forward_check(x, w, offsets, y, before, "width")
+    got = ops.expert_matmul_grad(dy, offsets, x=x, w=w)
+    for e, lo, hi in groups(offsets):
+        part = dy[lo:hi].double().t() @ x[lo:hi].double()
+        check(got.dw[e], part, 2 * rows * U * (dy[lo:hi].double().abs().t() @ x[lo:hi].double().abs()) + U * part.abs(), "dw")
+
+
+def test_nan_stays_in_its_expert():
+    """A NaN of one expert's rows is in nobody else's results, also where both are in one tile."""
+    g = gen(2)
+    x, w, dy = normal(g, 100, 64, dtype=BF16), normal(g, 3, 64, 64, dtype=BF16), normal(g, 100, 64, dtype=BF16)
+    offsets = offsets_of([30, 37, 33])
+    x[40], dy[50], w[1, 3, 3] = float("nan"), float("inf"), float("nan")
+    y = ops.expert_matmul(x, w, offsets)
+    got = ops.expert_matmul_grad(dy, offsets, x=x, w=w)
+    for e, lo, hi in groups(offsets):
+        bad = e == 1
+        assert bool(torch.isnan(y[lo:hi]).any()) == bad and bool(torch.isnan(got.dx[lo:hi]).any()) == bad
+        assert bool(torch.isnan(got.dw[e]).any()) == bad
+    assert not torch.isnan(y[30:67, :3]).any(dim=1)[:10].any()  # in its expert: only the row, and the output it meets
+
+
+def test_offsets_out_of_order_or_range():
+    """Clamped to the rows, and never below an earlier one."""
+    g = gen(3)
+    x, w = normal(g, 50, 32, dtype=BF16), normal(g, 5, 24, 32, dtype=BF16)
+    for ids in (torch.int32, torch.int64):
+        given = torch.tensor([-7, 20, 10, 30, 1 << 30, 45], dtype=ids, device=DEV)
+        meant = torch.tensor([0, 20, 20, 30, 50, 50], device=DEV)
+        before = normal(g, 50, 24)
+        y = ops.expert_matmul(x, w, given, out=before.clone())
+        forward_check(x, w, meant, y, before, "offsets")
+    wide = torch.tensor([0, 1 << 40, -(1 << 40), 3, 4, 5], device=DEV)
+    y = ops.expert_matmul(x, w, wide, out_dtype=F32)
+    forward_check(x, w, torch.tensor([0, 50, 50, 50, 50, 50], device=DEV), y, y * 0, "offsets")
+
+
+def test_no_rows():
+    w = normal(gen(0), 3, 16, 8, dtype=BF16)
+    x, offsets = torch.empty(0, 8, dtype=BF16, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    assert ops.expert_matmul(x, w, offsets).shape == (0, 16)
+    dw = torch.full((3, 16, 8), 5.0, device=DEV)
+    got = ops.expert_matmul_grad(x.new_empty(0, 16), offsets, x=x, w=w, dw=dw, accumulate=True)
+    assert got.dx.shape == (0, 8) and bool((dw == 5.0).all())
+    ops.expert_matmul_grad(x.new_empty(0, 16), offsets, x=x, dw=dw)
+    assert not dw.any()
+    x = normal(gen(0), 9, 8, dtype=BF16)  # rows, but nobody's
+    dw.fill_(5.0)
+    ops.expert_matmul_grad(normal(gen(0), 9, 16, dtype=BF16), offsets, x=x, dw=dw)
+    assert not dw.any()
+
+
+def test_strides_and_parts():
+    """Rows and experts with room between them, slices of wider matrices, and either gradient alone; the same bits."""
+    g = gen(11)
+    x, w, dy = normal(g, 333, 136, dtype=BF16), normal(g, 4, 72, 136, dtype=BF16), normal(g, 333, 72, dtype=BF16)
+    offsets = offsets_of([100, 200, 0, 33])
+    y = ops.expert_matmul(x, w, offsets)
+    assert torch.equal(ops.expert_matmul(padded(x, 2), padded(w, 3), offsets), y)
+    room = torch.zeros(4, 100, 136, dtype=BF16, device=DEV)
+    room[:, :72] = w
+    assert torch.equal(ops.expert_matmul(x, room[:, :72], offsets), y)
+    assert torch.equal(ops.expert_matmul(x, w, offsets, out_dtype=F32).to(BF16), y)
+    both = ops.expert_matmul_grad(dy, offsets, x=x, w=w)
+    only_dx, only_dw = ops.expert_matmul_grad(padded(dy, 1), offsets, w=padded(w, 1)), ops.expert_matmul_grad(dy, offsets, x=padded(x, 1))
+    assert only_dx.dw is None and only_dw.dx is None
+    assert torch.equal(only_dx.dx, both.dx) and torch.equal(only_dw.dw, both.dw)
+    assert both.dx.dtype == BF16 and both.dw.dtype == F32
+    slot = torch.zeros(1 + 4 * 72 * 136, dtype=BF16, device=DEV)
+    ops.expert_matmul_grad(dy, offsets, x=x, dw=slot[1:].view(4, 72, 136))
+    assert torch.equal(slot[1:].view(4, 72, 136), both.dw.to(BF16)) and float(slot[0]) == 0.0
+    again = ops.expert_matmul_grad(dy, offsets, x=x, w=w)
+    assert torch.equal(again.dx, both.dx) and torch.equal(again.dw, both.dw)
+
+
+def test_results_far_behind_the_first():
+    """More than 2^31 elements of results."""
+    n, m = 70000, 32768
+    x, w = torch.ones(n, 8, dtype=BF16, device=DEV), torch.ones(1, m, 8, dtype=BF16, device=DEV)
+    x[-1] = 2.0
+    y = ops.expert_matmul(x, w, offsets_of([n]))
+    assert bool((y[-1] == 16.0).all()) and bool((y[-2] == 8.0).all()) and bool((y[0] == 8.0).all())
+    assert bool((y[:, -1] == y[:, 0]).all())
+
+
+def test_captured_and_on_a_stream():
+    g = gen(8)
+    x, w, dy = normal(g, 300, 256, dtype=BF16), normal(g, 4, 128, 256, dtype=BF16), normal(g, 300, 128, dtype=BF16)
+    offsets = offsets_of([100, 0, 150, 50])
+    want, wgrad = ops.expert_matmul(x, w, offsets), ops.expert_matmul_grad(dy, offsets, x=x, w=w)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    y = ops.expert_matmul(x, w, offsets, stream=stream)
+    stream.synchronize()
+    assert torch.equal(y, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = ops.expert_matmul(x, w, offsets)
+        got = ops.expert_matmul_grad(dy, offsets, x=x, w=w)
+    for counts in ([100, 0, 150, 50], [7, 100, 20, 173]):  # the rows may be divided anew between replays
+        offsets.copy_(offsets_of(counts))
+        graph.replay()
+        assert torch.equal(y, ops.expert_matmul(x, w, offsets))
+        again = ops.expert_matmul_grad(dy, offsets, x=x, w=w)
+        assert torch.equal(got.dx, again.dx) and torch.equal(got.dw, again.dw)
+
+
+def test_refusals():
+    x, w, dy = (torch.zeros(*s, dtype=BF16, device=DEV) for s in ((10, 16), (2, 24, 16), (10, 24)))
+    offsets = offsets_of([5, 5])
+    for bad in [lambda: ops.expert_matmul(x.float(), w, offsets), lambda: ops.expert_matmul(x, w.float(), offsets),
+                lambda: ops.expert_matmul(x, w[:, :, :8], offsets), lambda: ops.expert_matmul(x, w, offsets[:2]),
+                lambda: ops.expert_matmul(x, w, offsets.float()), lambda: ops.expert_matmul(x, w, offsets.cpu()),
+                lambda: ops.expert_matmul(x.cpu(), w, offsets), lambda: ops.expert_matmul(x, w.transpose(1, 2), offsets),
+                lambda: ops.expert_matmul(x, w, offsets, out=torch.zeros(10, 23, device=DEV)),
+                lambda: ops.expert_matmul(x, w, offsets, out_dtype=torch.float16), lambda: ops.expert_matmul(x[0], w, offsets),
+                lambda: ops.expert_matmul(x.t(), w, offsets), lambda: ops.expert_matmul_grad(dy, offsets),
+                lambda: ops.expert_matmul_grad(dy, offsets, x=x[:9]), lambda: ops.expert_matmul_grad(dy, offsets, x=x, accumulate=True),
+                lambda: ops.expert_matmul_grad(dy, offsets, w=w, dx=torch.zeros(10, 8, device=DEV)),
+                lambda: ops.expert_matmul_grad(dy, offsets, x=x, w=w[:, :, :8])]:
+        with pytest.raises(ValueError):
+            bad()
+    off = torch.zeros(10, 20, dtype=BF16, device=DEV)[:, 1:17]  # rows off their boundaries
+    for bad in [lambda: ops.expert_matmul(off, w, offsets), lambda: ops.expert_matmul(x[:, :13].contiguous(), w[:, :, :13], offsets),
+                lambda: ops.expert_matmul_grad(dy, offsets, x=off)]:
+        with pytest.raises(AdaScaleError):
+            bad()
+    with pytest.raises(AdaScaleError):
+        ops.expert_matmul(x, w[:1].expand(1025, 24, 16), offsets_of([0] * 1025))
