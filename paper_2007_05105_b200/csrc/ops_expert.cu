@@ -2,8 +2,8 @@
 //
 //   y_r = W_e x_r       dx_r = W_e^T dy_r       dW_e (+)= sum over e's rows of dy_r x_r^T
 //
-// One kernel of three forms.  Each computes tiles D[128 x n] = A[128 x k] B[n x k]^T with A's rows on the 128 lanes of tensor
-// memory and n, a multiple of 16 up to NT, its columns:
+// One kernel of three forms.  Each computes tiles D[lanes x columns] = A[lanes x k] B[columns x k]^T with A's rows on the
+// lanes of tensor memory:
 //
 //            lanes (A)        columns (B)      summed over
 //   Y        W_e's rows       e's rows of x    in_dim
@@ -15,9 +15,16 @@
 // expert's rows, their products are not stored.  In the weights' gradient the rows are summed over: what the last
 // 64 of them bring of the next expert is set to zero in shared memory.
 //
-// A block a SM walks over the tiles: one warp issues the copies (tensor maps, 128-byte swizzle) into a ring of stages of 64
-// summands, one the matrix instructions, four bring finished tiles from tensor memory, where two take turns, to memory.
+// A block a SM, or a pair of them, walks over the tiles: one warp issues the copies (tensor maps, 128-byte swizzle) into a ring of
+// stages of 64 summands, one the matrix instructions, four bring finished tiles from tensor memory, where two take turns,
+// through shared memory to whole lines of memory.  In a pair both have 128 lanes and half of the columns' operand each, and the
+// first one's instructions work on both: 256 x 256 results for 32 KB a stage and SM where a block alone takes 48 KB for half as
+// many, and 48 KB are what the L2 cache does not deliver in the time that they are worked on.
 // Every block works out the tiles from the offsets by itself: no host, no kernel before.
+//
+// The tensor cores cut, not round, when they add to the 32-bit sums: over m summands a float32 result loses 1.1e-9 m of itself
+// (4.4e-6 at 4096, measured; bf16 results do not show it).  For float32 results no sum is longer than kPart: the parts are
+// added up, rounded, by the warps that read them, in tensor memory.
 #include "ops_common.cuh"
 
 #include <cuda.h>
@@ -27,16 +34,16 @@
 namespace {
 
 constexpr int kMaxExperts = ADASCALE_EXPERT_MAX_EXPERTS;
-constexpr int kM = 128;          // lanes of a tile
+constexpr int kLanes = 128;      // of a block
 constexpr int kK = 64;           // summands of a stage: 128 bytes, the swizzle's width
-constexpr int kTokenBox = 32;    // rows of one copy of tokens
-constexpr int kThreads = 192;    // copies, matrix instructions, four warps for results
-constexpr int kRingMax = 200 * 1024;
+constexpr int kPart = 12 * kK;   // summands of one sum in tensor memory, for float32 results
+constexpr int kThreads = 256;    // warps: copies, matrix instructions, ends of groups, one idle, four for results
+constexpr int kDynamicMax = 216 * 1024;
 
 enum Form { Y, DX, DW };
 
 struct ExpertArgs {
-    CUtensorMap a, b;
+    CUtensorMap a, b, c;  // operands; results
     const void *offsets;
     void *out;
     long long n_rows;
@@ -44,31 +51,56 @@ struct ExpertArgs {
     int n_experts, wide_offsets;
     int lanes, columns, summed;    // extents; the one that is e's rows is 0
     int accumulate, out_aligned;
+    int in_parts;                  // sums are cut at kPart
 };
 
-// ---- tensor memory and matrix instructions -------------------------------------------------
+// ---- tensor memory and matrix instructions: of a block, or of a pair -----------------------
 
-__device__ __forceinline__ void tmem_alloc(unsigned *where, unsigned columns)
+template <bool PAIR> __device__ __forceinline__ void tmem_alloc(unsigned *where, unsigned columns)
 {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if constexpr (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
 }
-__device__ __forceinline__ void tmem_free(unsigned base, unsigned columns)
+template <bool PAIR> __device__ __forceinline__ void tmem_free(unsigned base, unsigned columns)
 {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns));
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns));
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns));
 }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// All matrix instructions that this thread has issued arrive at the barrier when they are done.
-__device__ __forceinline__ void mma_commit(u64 *bar)
+// All matrix instructions that this thread has issued arrive at the barrier (in a pair: of both blocks) when they are done.
+template <bool PAIR> __device__ __forceinline__ void mma_commit(u64 *bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+                     "h"((unsigned short)3)
+                     : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void mma(unsigned d, u64 a, u64 b, unsigned what, bool add)
+template <bool PAIR> __device__ __forceinline__ void mma(unsigned d, u64 a, u64 b, unsigned what, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
-                 "r"(what), "r"((unsigned)add)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                     "l"(b), "r"(what), "r"((unsigned)add)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                     "l"(b), "r"(what), "r"((unsigned)add)
+                     : "memory");
+}
+// One thread of the warp.  What it alone does stands inside one branch on this, waits and all: with a branch on the thread's
+// number a matrix instruction goes out every 128 cycles at best, be it of 64 columns or 256.
+__device__ __forceinline__ bool elected()
+{
+    unsigned is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is;
 }
 // 32 columns of this warp's 32 lanes
 __device__ __forceinline__ void tmem_load(unsigned at, float (&x)[32])
@@ -86,12 +118,31 @@ __device__ __forceinline__ void tmem_load(unsigned at, float (&x)[32])
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
 }
-// A copy by a tensor map; the innermost coordinate is a multiple of 8 elements (16 bytes).
-__device__ __forceinline__ void tensor_load(void *dst, const CUtensorMap *map, int x, int y, int z, u64 *bar)
+__device__ __forceinline__ void tmem_store(unsigned at, const float (&x)[32])
 {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
-                 "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+                 "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "f"(x[8]), "f"(x[9]), "f"(x[10]),
+                 "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]), "f"(x[16]), "f"(x[17]), "f"(x[18]), "f"(x[19]), "f"(x[20]),
+                 "f"(x[21]), "f"(x[22]), "f"(x[23]), "f"(x[24]), "f"(x[25]), "f"(x[26]), "f"(x[27]), "f"(x[28]), "f"(x[29]), "f"(x[30]),
+                 "f"(x[31])
                  : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// A copy by a tensor map into this block's shared memory; the innermost coordinate is a multiple of 8 elements (16 bytes).  In a pair
+// the barrier may be the other block's.
+template <bool PAIR> __device__ __forceinline__ void tensor_load(void *dst, const CUtensorMap *map, int x, int y, int z, unsigned bar)
+{
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+                         smem_u32(dst)),
+                     "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+                     "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+                     : "memory");
 }
 
 // Shared memory operand, rows of 128 swizzled bytes, eight of them a group of 1024.
@@ -104,6 +155,30 @@ __device__ __forceinline__ u64 operand(unsigned addr, unsigned next)
     return (u64)((addr & 0x3ffff) >> 4) | (u64)((next & 0x3ffff) >> 4) << 16 | (u64)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
+// ---- pairs of blocks -----------------------------------------------------------------------
+
+__device__ __forceinline__ unsigned pair_rank()
+{
+    unsigned r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void pair_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The first block's barrier of the same place.
+__device__ __forceinline__ unsigned at_first(u64 *bar)
+{
+    unsigned there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"(smem_u32(bar)));
+    return there;
+}
+__device__ __forceinline__ void arrive_at_first(u64 *bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_first(bar)) : "memory");
+}
+
 // ---- tiles ---------------------------------------------------------------------------------
 
 // Of each expert: its rows, and the number of tiles before it.
@@ -112,16 +187,10 @@ struct Experts {
     int *tiles;  // [n + 1]
 };
 
-// Tiles of one expert: across the lanes, and across the columns.
-template <Form F, int NT> __device__ __forceinline__ int column_tiles(const ExpertArgs &a, int rows)
-{
-    return F == DW ? (a.columns + NT - 1) / NT : (rows + NT - 1) / NT;
-}
-
 // By one warp: offsets, ascending and within the rows, and running sums of the tiles.
-template <Form F, int NT> __device__ __forceinline__ void find_tiles(const ExpertArgs &a, const Experts &x)
+template <Form F, int NT, int LANES> __device__ __forceinline__ void find_tiles(const ExpertArgs &a, const Experts &x)
 {
-    const int lane = threadIdx.x % 32, lane_tiles = (a.lanes + kM - 1) / kM;
+    const int lane = threadIdx.x % 32, lane_tiles = (a.lanes + LANES - 1) / LANES;
     int floor = 0;
     for (int i = lane; i - lane <= a.n_experts; i += 32) {
         long long o = i <= a.n_experts ? load_id(a.offsets, a.wide_offsets, i) : 0;
@@ -141,7 +210,7 @@ template <Form F, int NT> __device__ __forceinline__ void find_tiles(const Exper
         int v = 0;
         if (i < a.n_experts) {
             const int rows = x.begin[i + 1] - x.begin[i];
-            v = rows || (F == DW && !a.accumulate) ? lane_tiles * column_tiles<F, NT>(a, rows) : 0;
+            v = rows || (F == DW && !a.accumulate) ? lane_tiles * (((F == DW ? a.columns : rows) + NT - 1) / NT) : 0;
         }
 #pragma unroll
         for (int k = 1; k < 32; k *= 2) {
@@ -157,225 +226,385 @@ template <Form F, int NT> __device__ __forceinline__ void find_tiles(const Exper
 
 struct Tile {
     int expert;
-    int lane;           // first lane
+    int lane;           // this block's first lane
     int column, width;  // first column (Y, DX: a row of the tokens), how many
     int row, summands;  // DW: first row; how many summands there are
 };
-// The tile that comes after `t.expert`'s first tiles; tiles ascend from call to call.
-template <Form F, int NT> __device__ __forceinline__ void find_tile(const ExpertArgs &a, const Experts &x, int tile, Tile &t)
+// Tiles ascend from call to call.
+template <Form F, int NT, int LANES> __device__ __forceinline__ void find_tile(const ExpertArgs &a, const Experts &x, int tile, int rank, Tile &t)
 {
+    constexpr int kStep = LANES > kLanes ? 32 : 16;  // of n, the width that an instruction can have
     while (tile >= x.tiles[t.expert + 1]) ++t.expert;
     const int begin = x.begin[t.expert], rows = x.begin[t.expert + 1] - begin, k = tile - x.tiles[t.expert];
-    const int across = column_tiles<F, NT>(a, rows), col = k % across;
-    t.lane = k / across * kM;
+    const int across = ((F == DW ? a.columns : rows) + NT - 1) / NT, col = k % across;
+    t.lane = k / across * LANES + rank * kLanes;
     if (F == DW) {
         t.column = col * NT;
         t.width = min(NT, a.columns - t.column);
         t.row = begin;
         t.summands = rows;
-    } else {  // of equal width, in steps of 16
-        const int each = ((rows + across - 1) / across + 15) / 16 * 16;
+    } else {  // of equal width
+        const int each = ((rows + across - 1) / across + kStep - 1) / kStep * kStep;
         t.column = begin + col * each;
-        t.width = min(each, rows - col * each);
+        t.width = min(each, rows - col * each);  // not less than 1: across - 1 of them are fewer than the rows
         t.row = 0;
         t.summands = a.summed;
     }
 }
 
-// A wait of a whole warp, with one answer for all of it.
-__device__ __forceinline__ bool wait_all(u64 *bar, unsigned parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
+// Waits of this kernel have a limit (kWaitNs) like all others, and one that runs out sets a flag that ends every other: the
+// block then runs to its end without copies, and what it would have stored is NaN.
+template <bool CLUSTER> __device__ __noinline__ void wait_long(u64 *bar, unsigned parity, volatile int *gave_up)
+{
+    u64 t0 = 0;
+    for (unsigned spin = 0; spin < 1u << 22; ++spin) {
+        if (mbar_poll<CLUSTER>(smem_u32(bar), parity) || *gave_up) return;
+        if ((spin & 63u) == 63u) {
+            u64 now;
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > kWaitNs) break;
+        }
+    }
+    *gave_up = 1;
+}
+template <bool CLUSTER = false> __device__ __forceinline__ void wait_for(u64 *bar, unsigned parity, volatile int *gave_up)
+{
+    if (!mbar_poll<CLUSTER>(smem_u32(bar), parity)) wait_long<CLUSTER>(bar, parity, gave_up);
+}
+
+// ---- results -------------------------------------------------------------------------------
+// A warp stores its 32 lanes by itself, 32 columns a time, by way of its two rooms of 32 x 32 results in shared memory and a copy
+// by tensor map, which leaves out what lies outside the matrix.
+
+// What was put into shared memory by all lanes goes out: lane 0 has the copies, at most one of them while the other room is filled.
+template <typename Issue> __device__ __forceinline__ void copy_out(Issue issue)
+{
+    copy_fence();
+    if (threadIdx.x % 32 == 0) bulk_wait_read<0>();  // of the other room: who has passed the next line may fill it
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) {
+        issue();
+        bulk_commit();
+    }
+}
+__device__ __forceinline__ void tensor_store(const CUtensorMap *map, int x, int y, int z, const void *src)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
+__device__ __forceinline__ void tensor_add(const CUtensorMap *map, int x, int y, int z, const void *src)
+{
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y),
+                 "r"(z)
+                 : "memory");
+}
+
+// Y, DX: of n columns (tokens) the lanes from lane0 on, adjacent elements of a token's row.  A row of `room` is a token's.
+template <typename O> __device__ __forceinline__ void store_tokens(const ExpertArgs &a, const float (&v)[32], O *room, int lane0, int token, int n)
+{
+    constexpr int V = 16 / sizeof(O), kPieces = 32 / V, kAtOnce = 32 / kPieces;
+    const int me = threadIdx.x % 32;
+    if (lane0 >= a.lanes) return;
+    O *out = static_cast<O *>(a.out) + (long long)token * a.ld_out + lane0;
+    if (!a.out_aligned) {
+        if (lane0 + me < a.lanes)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < n) put(out + i * a.ld_out + me, v[i]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) put(room + i * 32 + me, v[i]);
+    if (n == 32) {
+        copy_out([&] { tensor_store(&a.c, lane0, token, 0, room); });
+        return;
+    }
+    copy_out([] {});  // the last tokens of a group: what follows them is not ours
+    const int piece = me % kPieces, left = a.lanes - lane0 - piece * V;
+    for (int k = me / kPieces; k < n; k += kAtOnce) {
+        const O *q = room + k * 32 + piece * V;
+        O *p = out + k * a.ld_out + piece * V;
+        if (left >= V) {
+            *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(q);
+        } else {
+            for (int e = 0; e < left; ++e) p[e] = q[e];
+        }
+    }
+    __syncwarp();
+}
+
+// DW: n columns of the warp's lanes, each lane a row of dw.  Rows of `room` are 128 bytes (float32) or 64, with their 16-byte pieces in
+// the order of the tensor map's swizzle, which keeps banks apart.
+template <typename O> __device__ __forceinline__ void store_rows(const ExpertArgs &a, float (&v)[32], O *room, int expert, int lane0, int column, int n)
+{
+    constexpr int V = 16 / sizeof(O), kPieces = 32 / V;
+    const int me = threadIdx.x % 32;
+    if (lane0 >= a.lanes) return;
+    // a float32 gradient that is copied is added to on the way; others are read, added to in 32 bits and rounded once
+    const bool add_here = a.accumulate && (sizeof(O) == 2 || !a.out_aligned);
+    O *p = static_cast<O *>(a.out) + expert * a.stride_out + (lane0 + me) * a.ld_out + column;
+    if (add_here && lane0 + me < a.lanes) {
+        if (a.out_aligned && n == 32) {
+            float old[32];
+            load_vec<32>(p, old);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] += old[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < n) v[i] += to_f32(p[i]);
+        }
+    }
+    if (!a.out_aligned) {
+        if (lane0 + me < a.lanes)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < n) put(p + i, v[i]);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+        float x[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] = v[j * V + e];
+        store_vec<V>(room + me * 32 + (j ^ (kPieces == 8 ? me & 7 : me >> 1 & 3)) * V, x);
+    }
+    copy_out([&] {
+        if (sizeof(O) == 4 && a.accumulate) tensor_add(&a.c, column, lane0, expert, room);
+        else tensor_store(&a.c, column, lane0, expert, room);
+    });
+}
 
 // ---- the kernel ----------------------------------------------------------------------------
 
-template <int NT> constexpr int kStageBytes = (kM + NT) * kK * 2;
-template <int NT> constexpr int kStages = kRingMax / kStageBytes<NT>;
-template <int NT> constexpr int kSmemBytes = 1024 + kStages<NT> * kStageBytes<NT>;  // the ring starts on a boundary of 1024
+template <int NT, bool PAIR> constexpr int kStageBytes = (kLanes + (PAIR ? NT / 2 : NT)) * kK * 2;
+template <typename O> constexpr int kStaging = 2 * 32 * kLanes * (int)sizeof(O);
+template <int NT, bool PAIR, typename O> constexpr int kStages = (kDynamicMax - kStaging<O>) / kStageBytes<NT, PAIR>;
+// staging and ring, which start on a boundary of 1024
+template <int NT, bool PAIR, typename O> constexpr int kSmemBytes = 1024 + kStaging<O> + kStages<NT, PAIR, O> * kStageBytes<NT, PAIR>;
+template <int NT> constexpr int kTokenBox = NT < 64 ? NT : 64;  // rows of one copy of tokens
 
-template <Form F, int NT, typename O> __global__ void __launch_bounds__(kThreads) k_expert(const __grid_constant__ ExpertArgs a)
+template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds__(kThreads) k_expert(const __grid_constant__ ExpertArgs a)
 {
-    constexpr int S = kStages<NT>;
-    constexpr unsigned kColumns = NT <= 16 ? 32 : 2 * NT;
+    constexpr int S = kStages<NT, PAIR, O>, LANES = PAIR ? 2 * kLanes : kLanes, kA = kLanes * kK * 2, kBox = kTokenBox<NT>;
+    constexpr unsigned kColumns = 2 * NT;
     extern __shared__ unsigned char raw[];
-    __shared__ u64 full[S], empty[S], done[2], taken[2];
+    __shared__ u64 full[S], there[S], empty[S], done[2], taken[2], arrived, ended;
     __shared__ unsigned tmem_base;
+    __shared__ volatile int gave_up;
     __shared__ int begins[kMaxExperts + 1], tile_sums[kMaxExperts + 1];
-    unsigned char *ring = raw + (1024 - smem_u32(raw) % 1024) % 1024;
+    unsigned char *staging = raw + (1024 - smem_u32(raw) % 1024) % 1024, *ring = staging + kStaging<O>;
     const Experts x = {begins, tile_sums};
-    const int warp = threadIdx.x / 32;
+    const int warp = threadIdx.x / 32, rank = PAIR ? (int)pair_rank() : 0;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S; ++i) {
+            // the copies of a stage are there: of both blocks, at the first one's barrier; but the last 64 rows of a group of DW, which
+            // have to be ended first, arrive at each block's own, and are worked on when `there` says that the second block has ended its
             mbar_init(&full[i], 1);
+            mbar_init(&there[i], 1);
             mbar_init(&empty[i], 1);
         }
+        gave_up = 0;
+        mbar_init(&arrived, 1);
+        mbar_init(&ended, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&done[i], 1);
-            mbar_init(&taken[i], 128);
+            mbar_init(&taken[i], PAIR ? 8 : 4);
         }
         mbar_publish();
     }
-    if (warp == 1) tmem_alloc(&tmem_base, kColumns);
+    if (warp == 1) tmem_alloc<PAIR>(&tmem_base, kColumns);
     griddep_wait();
-    if (warp == 0) find_tiles<F, NT>(a, x);
+    if (warp == 0) find_tiles<F, NT, LANES>(a, x);
     tmem_fence_before();
     __syncthreads();
+    if constexpr (PAIR) pair_sync();
     tmem_fence_after();
     const unsigned tmem = tmem_base;
-    const int n_tiles = x.tiles[a.n_experts];
+    const int n_tiles = x.tiles[a.n_experts], first_tile = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
+    const int part = a.in_parts ? kPart : 0x7fffffc0;  // more than there are rows
     // operands whose summands lie across the rows in memory
     constexpr bool kAcrossA = F != Y, kAcrossB = F == DW;
 
     if (warp == 0) {
-        if (threadIdx.x == 0) {
+        if (elected()) {
             Tile t = {};
             int stage = 0, issued = 0;
             unsigned phase = 1;  // the first pass over the ring waits for nobody
-            bool ok = true;
-            for (int tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
-                find_tile<F, NT>(a, x, tile, t);
+            for (int tile = first_tile; tile < n_tiles; tile += step) {
+                find_tile<F, NT, LANES>(a, x, tile, rank, t);
+                // this block's columns: all of them, or its half
+                const int half = PAIR ? (t.width + 31) / 32 * 16 : t.width, column = t.column + rank * half;
+                const int boxes = F == DW ? (half + 63) / 64 : (half + kBox - 1) / kBox;
                 for (int k = 0; k < t.summands; k += kK) {
-                    if (!mbar_wait(&empty[stage], phase)) {
-                        ok = false;
-                        break;
-                    }
-                    unsigned char *as = ring + stage * kStageBytes<NT>, *bs = as + kM * kK * 2;
-                    u64 *bar = &full[stage];
+                    wait_for(&empty[stage], phase, &gave_up);
+                    if (gave_up) break;
+                    unsigned char *as = ring + stage * kStageBytes<NT, PAIR>, *bs = as + kA;
+                    const int bytes = kA + boxes * (F == DW ? 64 : kBox) * kK * 2;
+                    // in a pair the first block's barrier takes both blocks' bytes; the ends of groups go to each one's own
+                    const bool own = !PAIR || (F == DW && t.summands - k < kK);
+                    const unsigned bar = own ? smem_u32(&full[stage]) : at_first(&full[stage]);
+                    if (own || rank == 0) mbar_expect_tx(&full[stage], own ? bytes : 2 * bytes);
                     if constexpr (F == DW) {
-                        const int boxes = (t.width + 63) / 64;
-                        mbar_expect_tx(bar, (2 + boxes) * 8192);
-                        for (int i = 0; i < 2; ++i) tensor_load(as + i * 8192, &a.a, t.lane + 64 * i, t.row + k, 0, bar);
-                        for (int i = 0; i < boxes; ++i) tensor_load(bs + i * 8192, &a.b, t.column + 64 * i, t.row + k, 0, bar);
+                        for (int i = 0; i < 2; ++i) tensor_load<PAIR>(as + i * 8192, &a.a, t.lane + 64 * i, t.row + k, 0, bar);
+                        for (int i = 0; i < boxes; ++i) tensor_load<PAIR>(bs + i * 8192, &a.b, column + 64 * i, t.row + k, 0, bar);
                     } else {
-                        const int boxes = (t.width + kTokenBox - 1) / kTokenBox;
-                        mbar_expect_tx(bar, kM * kK * 2 + boxes * kTokenBox * kK * 2);
                         if constexpr (F == Y) {
-                            tensor_load(as, &a.a, k, t.lane, t.expert, bar);
+                            tensor_load<PAIR>(as, &a.a, k, t.lane, t.expert, bar);
                         } else {
-                            for (int i = 0; i < 2; ++i) tensor_load(as + i * 8192, &a.a, t.lane + 64 * i, k, t.expert, bar);
+                            for (int i = 0; i < 2; ++i) tensor_load<PAIR>(as + i * 8192, &a.a, t.lane + 64 * i, k, t.expert, bar);
                         }
-                        for (int i = 0; i < boxes; ++i) tensor_load(bs + i * kTokenBox * kK * 2, &a.b, k, t.column + i * kTokenBox, 0, bar);
+                        for (int i = 0; i < boxes; ++i) tensor_load<PAIR>(bs + i * kBox * kK * 2, &a.b, k, column + i * kBox, 0, bar);
                     }
                     ++issued;
                     if (++stage == S) stage = 0, phase ^= 1;
                 }
             }
-            // copies in flight end before the block does
+            // copies in flight end before the block does: their stages have been worked on
             for (int i = 0; i < min(issued, S); ++i) {
                 const int n = issued - 1 - i;
-                mbar_wait(&full[n % S], (n / S) & 1);
+                wait_for(&empty[n % S], (n / S) & 1, &gave_up);
             }
         }
-    } else if (warp == 1) {
-        Tile t = {};
-        int stage = 0, turn = 0;
-        unsigned phase = 0, free_phase[2] = {1, 1};
-        bool ok = true;
-        for (int tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
-            find_tile<F, NT>(a, x, tile, t);
-            if (t.summands == 0) continue;
-            ok = wait_all(&taken[turn], free_phase[turn]);
-            free_phase[turn] ^= 1;
-            tmem_fence_after();
-            const unsigned d = tmem + turn * NT;
-            const unsigned what = 1u << 4 | 1u << 7 | 1u << 10 | (kAcrossA ? 1u << 15 : 0u) | (kAcrossB ? 1u << 16 : 0u) |
-                                  (unsigned)((t.width + 15) / 16 * 2) << 17 | (unsigned)(kM / 16) << 24;
-            for (int k = 0; k < t.summands && ok; k += kK) {
-                ok = wait_all(&full[stage], phase);
-                if (!ok) break;
-                tmem_fence_after();
-                unsigned char *as = ring + stage * kStageBytes<NT>, *bs = as + kM * kK * 2;
-                const int left = t.summands - k;
-                if (F == DW && left < kK) {  // rows of the next expert, or of nobody
-                    const int boxes = 2 + (t.width + 63) / 64, step_end = (left + 15) / 16 * 16;
-                    for (int box = 0; box < boxes; ++box)
-                        for (int i = threadIdx.x % 32; i < (step_end - left) * 8; i += 32)
-                            reinterpret_cast<uint4 *>(as + box * 8192 + left * 128)[i] = make_uint4(0, 0, 0, 0);
-                    copy_fence();
-                    __syncwarp();
-                }
-                if (threadIdx.x % 32 == 0) {
-                    const u64 da = operand(smem_u32(as), kAcrossA ? 8192 : 16), db = operand(smem_u32(bs), kAcrossB ? 8192 : 16);
-#pragma unroll
-                    for (int i = 0; i < kK / 16; ++i) {
-                        if (16 * i >= left) break;
-                        mma(d, da + (u64)(i * (kAcrossA ? 2048 : 32) >> 4), db + (u64)(i * (kAcrossB ? 2048 : 32) >> 4), what, k + i > 0);
-                    }
-                    mma_commit(&empty[stage]);
-                }
-                __syncwarp();
-                if (++stage == S) stage = 0, phase ^= 1;
-            }
-            if (ok && threadIdx.x % 32 == 0) mma_commit(&done[turn]);
-            __syncwarp();
-            turn ^= 1;
-        }
-    } else {
-        const int lane = threadIdx.x % 32, quarter = warp % 4;  // a warp reads the quarter of the lanes that its number names
-        Tile t = {};
-        int turn = 0;
-        unsigned phase[2] = {0, 0};
-        bool ok = true;
-        O *out = static_cast<O *>(a.out);
-        for (int tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
-            find_tile<F, NT>(a, x, tile, t);
-            const bool any = t.summands > 0;
-            if (any && ok) {
-                ok = wait_all(&done[turn], phase[turn]);
-                tmem_fence_after();
-            }
-            if (any) phase[turn] ^= 1;
-            const int row = t.lane + quarter * 32 + lane;
-            const unsigned at = tmem + turn * NT + ((unsigned)(quarter * 32) << 16);
-            for (int c = 0; c < t.width; c += 32) {
-                float v[32];
-                __syncwarp();
-                if (any && ok) {
-                    tmem_load(at + c, v);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = any ? NAN : 0.f;  // NaN: a wait was given up
-                }
-                const int n = row < a.lanes ? min(32, t.width - c) : 0;
-                if constexpr (F == DW) {
-                    O *p = out + t.expert * a.stride_out + row * a.ld_out + t.column + c;
-                    if (a.out_aligned && n == 32) {
-                        constexpr int V = 16 / sizeof(O);
-#pragma unroll
-                        for (int i = 0; i < 32; i += V) {
-                            float part[V];
-#pragma unroll
-                            for (int k = 0; k < V; ++k) part[k] = v[i + k];
-                            if (a.accumulate) {
-                                float old[V];
-                                load_vec<V>(p + i, old);
-#pragma unroll
-                                for (int k = 0; k < V; ++k) part[k] += old[k];
+    } else if (warp == 1 && rank == 0) {
+        if (elected()) {
+            Tile t = {};
+            int stage = 0, turn = 0;
+            unsigned phase = 0, free_phase = 1, end_phase = 0, there_phase = 0;
+            for (int tile = first_tile; tile < n_tiles; tile += step) {
+                find_tile<F, NT, LANES>(a, x, tile, rank, t);
+                const unsigned n = PAIR ? (t.width + 31) / 32 * 32 : (t.width + 15) / 16 * 16;
+                const unsigned what =
+                    1u << 4 | 1u << 7 | 1u << 10 | (kAcrossA ? 1u << 15 : 0u) | (kAcrossB ? 1u << 16 : 0u) | n / 8 << 17 | (unsigned)(LANES / 16) << 24;
+                for (int begin = 0; begin < t.summands; begin += part) {
+                    wait_for<PAIR>(&taken[turn], free_phase, &gave_up);
+                    tmem_fence_after();
+                    const unsigned d = tmem + turn * NT;
+                    const int end = min(t.summands, begin + part);
+                    for (int k = begin; k < end; k += kK) {
+                        wait_for(&full[stage], phase, &gave_up);
+                        if (F == DW && t.summands - k < kK) {  // it is there: warp 2 may end it
+                            mbar_arrive(&arrived);
+                            wait_for(&ended, end_phase, &gave_up);
+                            end_phase ^= 1;
+                            if constexpr (PAIR) {
+                                wait_for<true>(&there[stage], there_phase >> stage & 1, &gave_up);
+                                there_phase ^= 1u << stage;
                             }
-                            store_vec<V>(p + i, part);
                         }
+                        tmem_fence_after();
+                        const unsigned as = smem_u32(ring + stage * kStageBytes<NT, PAIR>);
+                        const u64 da = operand(as, kAcrossA ? 8192 : 16), db = operand(as + kA, kAcrossB ? 8192 : 16);
+#pragma unroll
+                        for (int i = 0; i < kK / 16; ++i)  // summands behind the last are zeros
+                            mma<PAIR>(d, da + (u64)(i * (kAcrossA ? 2048 : 32) >> 4), db + (u64)(i * (kAcrossB ? 2048 : 32) >> 4), what, k + i > begin);
+                        mma_commit<PAIR>(&empty[stage]);
+                        if (++stage == S) stage = 0, phase ^= 1;
+                    }
+                    mma_commit<PAIR>(&done[turn]);
+                    if (a.in_parts) {
+                        free_phase ^= 1;
+                    } else {
+                        free_phase ^= turn;
+                        turn ^= 1;
+                    }
+                }
+            }
+        }
+    } else if (F == DW && warp == 2) {  // rows of the next expert, or of nobody, behind the last of e's: zeros
+        Tile t = {};
+        int blocks = 0;
+        unsigned phase = 0;  // rank 1: of every stage
+        for (int tile = first_tile; tile < n_tiles; tile += step) {
+            find_tile<F, NT, LANES>(a, x, tile, rank, t);
+            blocks += (t.summands + kK - 1) / kK;
+            const int left = t.summands % kK;
+            if (left == 0) continue;
+            const int stage = (blocks - 1) % S;
+            if (rank == 0) {
+                wait_for(&arrived, phase, &gave_up);
+                phase ^= 1;
+            } else {
+                wait_for(&full[stage], phase >> stage & 1, &gave_up);
+                phase ^= 1u << stage;
+            }
+            __syncwarp();
+            unsigned char *as = ring + stage * kStageBytes<NT, PAIR>;
+            const int half = PAIR ? (t.width + 31) / 32 * 16 : t.width, boxes = 2 + (half + 63) / 64;
+            for (int box = 0; box < boxes; ++box)
+                for (int i = threadIdx.x % 32; i < (kK - left) * 8; i += 32)
+                    reinterpret_cast<uint4 *>(as + box * 8192 + left * 128)[i] = make_uint4(0, 0, 0, 0);
+            copy_fence();
+            __syncwarp();
+            if (threadIdx.x % 32 == 0) {
+                if (rank == 0) mbar_arrive(&ended);
+                else arrive_at_first(&there[stage]);
+            }
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp - 4;  // a warp reads the quarter of the lanes that its number names
+        O *room = reinterpret_cast<O *>(staging) + quarter * 2 * 32 * 32;
+        const unsigned mine = (unsigned)(quarter * 32) << 16;
+        Tile t = {};
+        int turn = 0, chunks = 0;
+        unsigned phase = 0;
+        for (int tile = first_tile; tile < n_tiles; tile += step) {
+            find_tile<F, NT, LANES>(a, x, tile, rank, t);
+            for (int begin = 0; begin < t.summands || begin == 0; begin += part) {
+                const bool any = t.summands > 0, last = begin + part >= t.summands;
+                if (any) {
+                    wait_for(&done[turn], phase, &gave_up);
+                    __syncwarp();
+                    tmem_fence_after();
+                }
+                const bool lost = __any_sync(0xffffffffu, gave_up);
+                for (int c = 0; c < t.width; c += 32) {
+                    float v[32];
+                    if (any && !lost) {
+                        tmem_load(tmem + turn * NT + mine + c, v);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (i < n) put(p + i, a.accumulate ? v[i] + to_f32(p[i]) : v[i]);
+                        for (int i = 0; i < 32; ++i) v[i] = any ? NAN : 0.f;
                     }
-                } else {
-                    O *p = out + (t.column + c) * a.ld_out + row;
+                    if (begin > 0) {
+                        float sum[32];
+                        tmem_load(tmem + NT + mine + c, sum);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (i < n) put(p + i * a.ld_out, v[i]);
+                        for (int i = 0; i < 32; ++i) v[i] += sum[i];
+                    }
+                    if (!last) {
+                        tmem_store(tmem + NT + mine + c, v);
+                        continue;
+                    }
+                    const int n = min(32, t.width - c);
+                    O *mine_now = room + chunks++ % 2 * 32 * 32;
+                    if constexpr (F == DW) store_rows<O>(a, v, mine_now, t.expert, t.lane + quarter * 32, t.column + c, n);
+                    else store_tokens<O>(a, v, mine_now, t.lane + quarter * 32, t.column + c, n);
+                }
+                if (!any) continue;
+                tmem_fence_before();
+                __syncwarp();
+                if (threadIdx.x % 32 == 0) {
+                    if constexpr (PAIR) arrive_at_first(&taken[turn]);
+                    else mbar_arrive(&taken[turn]);
+                }
+                if (a.in_parts) {
+                    phase ^= 1;
+                } else {
+                    phase ^= turn;
+                    turn ^= 1;
                 }
             }
-            if (any) {
-                tmem_fence_before();
-                mbar_arrive(&taken[turn]);
-                turn ^= 1;
-            }
         }
+        if (threadIdx.x % 32 == 0) bulk_wait_all();
     }
     tmem_fence_before();
     __syncthreads();
+    if constexpr (PAIR) pair_sync();  // neither ends while the other may arrive at its barriers
     tmem_fence_after();
-    if (warp == 1) tmem_free(tmem, kColumns);
+    if (warp == 1) tmem_free<PAIR>(tmem, kColumns);
 }
 
 // ---- host side -----------------------------------------------------------------------------
@@ -398,44 +627,72 @@ EncodeTiled encode_tiled()
     known.store(f, std::memory_order_relaxed);
     return f;
 }
-// [n, rows, cols] of bf16 with `ld` and `stride` elements between rows and matrices; boxes of 64 columns and `box` rows.
-bool make_map(CUtensorMap *map, const void *p, long long n, long long rows, long long cols, long long stride, long long ld, int box)
+// [n, rows, cols] with `ld` and `stride` elements between rows and matrices.
+struct Extents {
+    long long n, rows, cols, stride, ld;
+};
+bool make_map(CUtensorMap *map, const void *p, Extents x, int dtype, int box_cols, int box_rows, CUtensorMapSwizzle swizzle)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
-    const long long wide = (cols + 7) / 8 * 8;  // a stride that is never used still has to be one
-    if (rows <= 1) ld = std::max(ld, wide) / 8 * 8;
-    if (n <= 1) stride = ld * rows;
-    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)n}, strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)stride * 2};
-    const cuuint32_t boxes[3] = {64, (cuuint32_t)box, 1}, steps[3] = {1, 1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    // strides that are never used still have to be some
+    if (x.rows <= 1) x.ld = (x.cols + 7) / 8 * 8;
+    if (x.n <= 1) x.stride = x.ld * x.rows;
+    const cuuint64_t b = (cuuint64_t)elem_bytes(dtype), dims[3] = {(cuuint64_t)x.cols, (cuuint64_t)x.rows, (cuuint64_t)x.n};
+    const cuuint64_t strides[2] = {(cuuint64_t)x.ld * b, (cuuint64_t)x.stride * b};
+    const cuuint32_t boxes[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, steps[3] = {1, 1, 1};
+    return encode(map, dtype == ADASCALE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void *>(p), dims, strides,
+                  boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// An operand: 64 columns and `box` rows a copy.
+bool operand_map(CUtensorMap *map, const void *p, const Extents &x, int box)
+{
+    return make_map(map, p, x, ADASCALE_BF16, 64, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// Results, 32 x 32 a copy, where their rows allow it.
+bool result_map(ExpertArgs &e, const Extents &x, int dtype, CUtensorMapSwizzle swizzle)
+{
+    const int b = elem_bytes(dtype);
+    e.out_aligned = on(e.out, 16) && (x.rows <= 1 || x.ld * b % 16 == 0) && (x.n <= 1 || x.stride * b % 16 == 0);
+    return !e.out_aligned || make_map(&e.c, e.out, x, dtype, 32, 32, swizzle);
 }
 
-template <Form F, int NT, typename O> cudaError_t run_tiles(const ExpertArgs &a, long long tiles, cudaStream_t s)
+template <Form F, int NT, bool PAIR, typename O> cudaError_t run_tiles(const ExpertArgs &a, long long tiles, cudaStream_t s)
 {
     static OncePerDevice known;
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_expert<F, NT, O>), known);
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_expert<F, NT, PAIR, O>), known);
     if (e != cudaSuccess) return e;
     const int sms = sm_count();
-    if (sms <= 0) return cudaErrorUnknown;
-    return launch(k_expert<F, NT, O>, std::min<long long>(tiles, sms), kThreads, kSmemBytes<NT>, s, a);
+    if (sms < 2) return cudaErrorUnknown;
+    const long long blocks = PAIR ? 2 * std::min<long long>(tiles, sms / 2) : std::min<long long>(tiles, sms);
+    return launch(k_expert<F, NT, PAIR, O>, blocks, kThreads, kSmemBytes<NT, PAIR, O>, s, a, PAIR ? 2 : 1);
 }
-template <Form F, int NT> cudaError_t run_type(const ExpertArgs &a, int dtype, cudaStream_t s)
+template <Form F, int NT, bool PAIR = false> cudaError_t run_type(ExpertArgs &a, int dtype, cudaStream_t s)
 {
-    const long long lane_tiles = ceil_div(a.lanes, kM);
+    const long long lane_tiles = ceil_div(a.lanes, PAIR ? 2 * kLanes : kLanes);
+    const long long summands = F == DW ? a.n_rows : a.summed;
+    a.in_parts = dtype == ADASCALE_F32 && summands > kPart;
     // at most this many tiles: each expert may have one that is not full
     const long long tiles = F == DW ? a.n_experts * lane_tiles * ceil_div(a.columns, NT)
                                     : lane_tiles * (a.n_rows / NT + std::min<long long>(a.n_experts, a.n_rows));
-    return dtype == ADASCALE_BF16 ? run_tiles<F, NT, bf16>(a, tiles, s) : run_tiles<F, NT, float>(a, tiles, s);
+    return dtype == ADASCALE_BF16 ? run_tiles<F, NT, PAIR, bf16>(a, tiles, s) : run_tiles<F, NT, PAIR, float>(a, tiles, s);
+}
+// Pairs of blocks where there are lanes for both.
+template <Form F> cudaError_t run_wide(ExpertArgs &a, int dtype, cudaStream_t s)
+{
+    return a.lanes > kLanes ? run_type<F, 256, true>(a, dtype, s) : run_type<F, 256>(a, dtype, s);
 }
 // Tiles of tokens are as wide as the rows of an expert on average, as far as the host knows.
-template <Form F> cudaError_t run_tokens(const ExpertArgs &a, int dtype, cudaStream_t s)
+template <Form F> cudaError_t run_tokens(ExpertArgs &a, int dtype, cudaStream_t s, int n)
 {
-    const long long mean = ceil_div(a.n_rows, a.n_experts);
-    if (mean <= 32) return run_type<F, 32>(a, dtype, s);
-    if (mean <= 128) return run_type<F, 128>(a, dtype, s);
-    return run_type<F, 256>(a, dtype, s);
+    if (n == 32) return run_type<F, 32>(a, dtype, s);
+    if (n == 128) return run_type<F, 128>(a, dtype, s);
+    return run_wide<F>(a, dtype, s);
+}
+int token_tile(long long n_rows, long long n_experts)
+{
+    const long long mean = ceil_div(n_rows, n_experts);
+    return mean <= 32 ? 32 : mean <= 128 ? 128 : 256;
 }
 
 bool rows16(const void *p, long long ld, long long rows, long long stride, long long n)
@@ -448,7 +705,7 @@ template <typename A> adascale_status check_sizes(const A &a)
     if (a.n_rows < 0 || a.n_experts < 1 || a.in_dim < 1 || a.out_dim < 1 || !is_itype(a.offset_type) || !a.offsets) return ADASCALE_ERR_INVALID_ARG;
     if (a.n_rows > kMaxRows - 512 || a.n_experts > kMaxExperts || a.in_dim > ADASCALE_EXPERT_MAX_DIM || a.out_dim > ADASCALE_EXPERT_MAX_DIM) return ADASCALE_ERR_TOO_LARGE;
     // tiles are counted in 32 bits
-    const long long in = ceil_div(a.in_dim, kM), out = ceil_div(a.out_dim, kM);
+    const long long in = ceil_div(a.in_dim, kLanes), out = ceil_div(a.out_dim, kLanes);
     if ((a.n_rows / 32 + a.n_experts) > (1LL << 30) / std::max(in, out) || in * out > (1LL << 30) / a.n_experts) return ADASCALE_ERR_TOO_LARGE;
     return ADASCALE_OK;
 }
@@ -486,10 +743,12 @@ extern "C" adascale_status adascale_expert_matmul(const adascale_expert_matmul_a
     e.ld_out = a.ld_y;
     e.lanes = (int)a.out_dim;
     e.summed = (int)a.in_dim;
-    if (!make_map(&e.a, a.w, a.n_experts, a.out_dim, a.in_dim, a.stride_w, a.ld_w, kM) ||
-        !make_map(&e.b, a.x, 1, a.n_rows, a.in_dim, 0, a.ld_x, kTokenBox))
+    const int n = token_tile(a.n_rows, a.n_experts);
+    if (!operand_map(&e.a, a.w, {a.n_experts, a.out_dim, a.in_dim, a.stride_w, a.ld_w}, kLanes) ||
+        !operand_map(&e.b, a.x, {1, a.n_rows, a.in_dim, 0, a.ld_x}, std::min(n, 64)) ||
+        !result_map(e, {1, a.n_rows, a.out_dim, 0, a.ld_y}, a.y_dtype, CU_TENSOR_MAP_SWIZZLE_NONE))
         return ADASCALE_ERR_CUDA;
-    OPS_CU(run_tokens<Y>(e, a.y_dtype, static_cast<cudaStream_t>(cuda_stream)));
+    OPS_CU(run_tokens<Y>(e, a.y_dtype, static_cast<cudaStream_t>(cuda_stream), n));
     return ADASCALE_OK;
 }
 
@@ -517,10 +776,12 @@ extern "C" adascale_status adascale_expert_matmul_grad(const adascale_expert_mat
         e.ld_out = a.ld_dx;
         e.lanes = (int)a.in_dim;
         e.summed = (int)a.out_dim;
-        if (!make_map(&e.a, a.w, a.n_experts, a.out_dim, a.in_dim, a.stride_w, a.ld_w, kK) ||
-            !make_map(&e.b, a.dy, 1, a.n_rows, a.out_dim, 0, a.ld_dy, kTokenBox))
+        const int n = token_tile(a.n_rows, a.n_experts);
+        if (!operand_map(&e.a, a.w, {a.n_experts, a.out_dim, a.in_dim, a.stride_w, a.ld_w}, kK) ||
+            !operand_map(&e.b, a.dy, {1, a.n_rows, a.out_dim, 0, a.ld_dy}, std::min(n, 64)) ||
+            !result_map(e, {1, a.n_rows, a.in_dim, 0, a.ld_dx}, a.dx_dtype, CU_TENSOR_MAP_SWIZZLE_NONE))
             return ADASCALE_ERR_CUDA;
-        OPS_CU(run_tokens<DX>(e, a.dx_dtype, s));
+        OPS_CU(run_tokens<DX>(e, a.dx_dtype, s, n));
     }
     if (want_dw) {
         ExpertArgs e = make_args(a);
@@ -530,12 +791,12 @@ extern "C" adascale_status adascale_expert_matmul_grad(const adascale_expert_mat
         e.lanes = (int)a.out_dim;
         e.columns = (int)a.in_dim;
         e.accumulate = a.accumulate != 0;
-        const int v = 16 / elem_bytes(a.dw_dtype);
-        e.out_aligned = on(a.dw, 16) && a.ld_dw % v == 0 && a.stride_dw % v == 0;
-        // without rows no copy is made
-        if (rows && (!make_map(&e.a, a.dy, 1, a.n_rows, a.out_dim, 0, a.ld_dy, kK) || !make_map(&e.b, a.x, 1, a.n_rows, a.in_dim, 0, a.ld_x, kK)))
+        // without rows no operand is copied
+        if ((rows && (!operand_map(&e.a, a.dy, {1, a.n_rows, a.out_dim, 0, a.ld_dy}, kK) || !operand_map(&e.b, a.x, {1, a.n_rows, a.in_dim, 0, a.ld_x}, kK))) ||
+            !result_map(e, {a.n_experts, a.out_dim, a.in_dim, a.stride_dw, a.ld_dw}, a.dw_dtype,
+                        a.dw_dtype == ADASCALE_F32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
             return ADASCALE_ERR_CUDA;
-        OPS_CU(run_type<DW, 256>(e, a.dw_dtype, s));
+        OPS_CU(run_wide<DW>(e, a.dw_dtype, s));
     }
     return ADASCALE_OK;
 }
