@@ -4,16 +4,22 @@
 //   g = p (dp - sum p dp),   ds = scale g,   dtable[k, h] = sum of g over bucket k
 //
 // One pass over the data: a group of threads (8 lanes, a warp, or a block, by the length of a row) holds a row in registers
-// between the maximum, the sum and the result.  Bound by memory.  The bias is never in memory: a block works on one head, keeps
-// that head's table column and the bucket of every distance up to max_distance in shared memory, and asks for the buckets of the
-// first and the last of the 4 or 8 adjacent keys that a thread holds; where they are equal - everywhere but near the
-// diagonal - all of them are, since buckets are monotone on either side.  Keys that are not live are not read.
+// between the maximum, the sum and the result.  Bound by memory.  Keys that are not live are not read, but for those that share 16
+// bytes with the last live one.
+//
+// The bias is never in memory: a block works on one head and keeps that head's bias by distance in shared memory, up to
+// max_distance, where it stops changing; beyond, a register has it.  A thread's 4 or 8 adjacent keys want as many adjacent
+// entries, which begin anywhere: four copies, each shifted by one entry, let 16-byte reads fetch them (single reads: four lanes a
+// bank).  Above kCopiesMax the copies would not fit, and the bucket of each distance is looked up.
 //
 // The gradient of the table is summed without atomics: every lane has a column of its own in shared memory (bank = lane), one
-// entry a bucket; keys further than max_distance, most of them, are summed in two registers.  Blocks leave their sums, a
+// entry a bucket; keys further than max_distance, most of them, are summed in two registers.  A thread's adjacent keys are in one
+// bucket if the first and the last of them are, since buckets are monotone on either side.  Blocks leave their sums, a
 // second kernel adds them up in order.
 //
-// Rows may start anywhere: accesses are cut at 16-byte boundaries of memory, the ragged ends of a row go element by element.
+// While a row is worked on, the group's next one is on its way into shared memory, each thread's part to a place of its own.
+//
+// Rows may start anywhere (then without that): accesses are cut at 16-byte boundaries of memory, the ragged ends of a row go element by element.
 #include "ops_common.cuh"
 
 #include <algorithm>
@@ -24,6 +30,7 @@ namespace {
 constexpr int kBordersMax = ADASCALE_POSITION_MAX_BUCKETS / 2;
 constexpr long long kMaxLen = 1LL << 29, kMaxStart = 1LL << 30;  // distances stay 32-bit numbers
 constexpr int kBlocksMax = 2048;   // of all heads, roughly; the gradient's partial sums are that many times the buckets
+constexpr int kCopiesMax = 1024;   // max_distance up to which the bias is kept by distance (33 KB)
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Buckets of a side: n < exact by itself, then one more for every border that is not above n.
@@ -63,84 +70,160 @@ __device__ __forceinline__ int bucket_of(const Buckets &b, int d)
     return k + (b.both && d > 0 ? b.m : 0);
 }
 
-// Shared memory: the head's table column, the buckets by distance, the lanes' sums.
-struct Tables {
-    float *bias;
-    unsigned char *bucket;  // of distance d at d + max_distance
-    int max_distance;
-    __device__ __forceinline__ int at(int d) const
-    {
-        d = d < -max_distance ? -max_distance : d > max_distance ? max_distance : d;
-        return bucket[d + max_distance];
-    }
-};
-__host__ __device__ inline int bucket_bytes(int max_distance) { return (2 * max_distance + 1 + 15) / 16 * 16; }
+// ---- rows ----------------------------------------------------------------------------------
 
-__device__ __forceinline__ Tables make_tables(const PositionArgs &a, int head, unsigned char *room, bool bias)
-{
-    Tables t;
-    t.max_distance = a.buckets.max_distance;
-    t.bucket = room;
-    t.bias = reinterpret_cast<float *>(room + bucket_bytes(t.max_distance));
-    for (int i = threadIdx.x; i <= 2 * t.max_distance; i += blockDim.x) t.bucket[i] = (unsigned char)bucket_of(a.buckets, i - t.max_distance);
-    if (bias)
-        for (int i = threadIdx.x; i < a.buckets.n; i += blockDim.x) t.bias[i] = a.table[i * a.ld_table + head];
-    return t;
-}
-
-// A row: its address in each matrix, the position of its query, and how many keys are live.
+// A row's batch and query; the position of its query, and how many keys are live.
 struct Row {
-    long long b;
-    int i, pos, live;
+    int b, i, pos, live;
+    int n;         // keys of the row: 0 behind the last
+    long long at;  // where it begins in the first matrix
 };
-__device__ __forceinline__ Row row_of(const PositionArgs &a, long long r, long long end)
+__device__ __forceinline__ void look_up(const PositionArgs &a, Row &w)
 {
-    Row w = {0, 0, 0, 0};
-    if (r >= end) return w;
-    w.b = (unsigned)r / (unsigned)a.n_queries;
-    w.i = (int)(r - w.b * a.n_queries);
-    long long start = a.starts ? load_id(a.starts, a.wide_starts, w.b) : 0;
-    start = start < -kMaxStart ? -kMaxStart : start > kMaxStart ? kMaxStart : start;
-    w.pos = (int)start + w.i;
-    long long live = a.n_keys;
+    w.pos = w.i;
+    if (a.starts) {
+        const long long start = load_id(a.starts, a.wide_starts, w.b);
+        w.pos += (int)(start < -kMaxStart ? -kMaxStart : start > kMaxStart ? kMaxStart : start);
+    }
+    w.live = a.n_keys;
     if (a.lengths) {
         const long long n = load_id(a.lengths, a.wide_lengths, w.b);
-        live = n < 0 ? 0 : n < live ? n : live;
+        w.live = n < 0 ? 0 : n < w.live ? (int)n : w.live;
     }
-    if (a.causal && w.pos < live) live = w.pos < 0 ? 0 : (long long)w.pos + 1 < live ? w.pos + 1 : live;
-    w.live = (int)live;
-    return w;
+    if (a.causal) w.live = min(w.live, max(w.pos + 1, 0));
 }
-template <typename T> __device__ __forceinline__ T *row_at(const void *base, const Strides &at, const Row &w, int head)
-{
-    return static_cast<T *>(const_cast<void *>(base)) + w.b * at.b + head * at.h + w.i * at.q;
-}
+__device__ __forceinline__ long long offset_of(const Strides &at, const Row &w, int head) { return w.b * at.b + head * at.h + w.i * at.q; }
+
+// Walks over every chunks * kGroups-th row of all: neighbours, which have as many live keys, go to different blocks.
+template <int kGroups> struct Walk {
+    unsigned r, step;
+    int step_b, step_i;
+    long long step_at, wrap_at;  // of the offset in the first matrix
+    Row w;
+    __device__ __forceinline__ Walk(const PositionArgs &a, int head, int chunk, int group)
+    {
+        const unsigned n = (unsigned)a.n_queries;
+        step = (unsigned)(a.chunks * kGroups);
+        r = (unsigned)(chunk * kGroups + group);
+        step_b = (int)(step / n);
+        step_i = (int)(step % n);
+        w.b = (int)(r / n);
+        w.i = (int)(r % n);
+        w.at = offset_of(a.s_at, w, head);
+        step_at = step_b * a.s_at.b + step_i * a.s_at.q;
+        wrap_at = a.s_at.b - n * a.s_at.q;
+    }
+    // The row where it stands.
+    __device__ __forceinline__ Row here(const PositionArgs &a) const
+    {
+        Row x = w;
+        x.n = x.pos = x.live = 0;
+        if (r < (unsigned)a.rows) {
+            x.n = a.n_keys;
+            look_up(a, x);
+        }
+        return x;
+    }
+    __device__ __forceinline__ void next(const PositionArgs &a)
+    {
+        r += step;  // below 2^31 + 2^17
+        w.b += step_b;
+        w.i += step_i;
+        w.at += step_at;
+        if (w.i >= a.n_queries) {
+            w.i -= a.n_queries;
+            ++w.b;
+            w.at += wrap_at;
+        }
+    }
+};
+
+// Whether the next row is requested while one is worked on: bf16 rows have twice the arithmetic a byte, and the warps that fit do not cover
+// the wait for memory (gradient of 8 x 16 x 1024 x 1024, causal: 126 us without, 114 with; float32 of 32 x 8 x 512 x 512: 127 and 150).
+template <typename T, bool LONG, bool EVEN> constexpr bool kRowsAhead = sizeof(T) == 2 && EVEN && !LONG;
+
 // Elements by which an address lies behind a 16-byte boundary.
 template <typename T> __device__ __forceinline__ int off16(const T *p) { return (int)((uintptr_t)p % 16 / sizeof(T)); }
 
-// Elements c .. c + V - 1 of a row of which [0, end) may be read; others are 0.
-template <typename T, int V> __device__ __forceinline__ void load_cols(const T *row, int c, int end, bool aligned, float (&x)[V])
+// 16 bytes: elements c .. c + V - 1 of a row of n; those outside are 0.  EVEN: rows begin on and end at 16-byte boundaries, and all
+// matrices have the same strides.
+template <bool EVEN, typename T> __device__ __forceinline__ uint4 load_raw(const T *row, int c, int n, bool aligned)
 {
-    if (aligned && c >= 0 && c + V <= end) {
-        load_vec<V>(row + c, x);
-    } else {
+    constexpr int V = 16 / sizeof(T);
+    if (EVEN || (aligned && c >= 0 && c + V <= n)) return *reinterpret_cast<const uint4 *>(row + c);
+    union {
+        uint4 raw;
+        T x[V];
+    } u;
+    u.raw = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[e] = c + e >= 0 && c + e < end ? to_f32(row[c + e]) : 0.f;
+    for (int e = 0; e < V; ++e)
+        if (c + e >= 0 && c + e < n) u.x[e] = row[c + e];
+    return u.raw;
+}
+// Zeros for the elements outside [0, live).
+template <bool EVEN, typename T> __device__ __forceinline__ void keep_live(uint4 &raw, int c, int live)
+{
+    constexpr int V = 16 / sizeof(T);
+    if ((EVEN || c >= 0) && c + V <= live) return;
+    unsigned *x = reinterpret_cast<unsigned *>(&raw);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            if (c + i < 0 || c + i >= live) x[i] = 0u;
+        } else {
+            if (c + 2 * i < 0 || c + 2 * i >= live) x[i] &= 0xffff0000u;
+            if (c + 2 * i + 1 < 0 || c + 2 * i + 1 >= live) x[i] &= 0xffffu;
+        }
     }
 }
-template <typename T, int V> __device__ __forceinline__ void store_cols(T *row, int c, int end, bool aligned, const float (&x)[V])
+// Its elements, two and two.
+__device__ __forceinline__ void spread(const uint4 &r, f2 (&x)[2], float)
 {
-    if (aligned && c >= 0 && c + V <= end) {
-        store_vec<V>(row + c, x);
+    x[0] = pack2(__uint_as_float(r.x), __uint_as_float(r.y));
+    x[1] = pack2(__uint_as_float(r.z), __uint_as_float(r.w));
+}
+__device__ __forceinline__ void spread(const uint4 &r, f2 (&x)[4], bf16)
+{
+    x[0] = pack2(bf_lo(r.x), bf_hi(r.x));
+    x[1] = pack2(bf_lo(r.y), bf_hi(r.y));
+    x[2] = pack2(bf_lo(r.z), bf_hi(r.z));
+    x[3] = pack2(bf_lo(r.w), bf_hi(r.w));
+}
+template <int P> __device__ __forceinline__ void flat(const f2 (&x)[P], float (&y)[2 * P])
+{
+#pragma unroll
+    for (int i = 0; i < P; ++i) unpack2(x[i], y[2 * i], y[2 * i + 1]);
+}
+// Elements outside [0, live) become `other`.
+template <bool EVEN, int P> __device__ __forceinline__ void keep_live(f2 (&x)[P], int c, int live, float other)
+{
+    if ((EVEN || c >= 0) && c + 2 * P <= live) return;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        float lo, hi;
+        unpack2(x[i], lo, hi);
+        lo = (EVEN || c + 2 * i >= 0) && c + 2 * i < live ? lo : other;
+        hi = (EVEN || c + 2 * i + 1 >= 0) && c + 2 * i + 1 < live ? hi : other;
+        x[i] = pack2(lo, hi);
+    }
+}
+template <bool EVEN, typename T, int P> __device__ __forceinline__ void store_cols(T *row, int c, int n, bool aligned, const f2 (&x)[P])
+{
+    float y[2 * P];
+    flat(x, y);
+    if (EVEN || (aligned && c >= 0 && c + 2 * P <= n)) {
+        store_vec_streaming<2 * P>(row + c, y);
     } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (c + e >= 0 && c + e < end) put(row + c + e, x[e]);
+        for (int e = 0; e < 2 * P; ++e)
+            if (c + e >= 0 && c + e < n) put(row + c + e, y[e]);
     }
 }
 
-// Sum or maximum over the GS threads of a group, the same in each of them.
-template <int GS, bool MAX> __device__ __forceinline__ float group_join(float v, float *scratch)
+// Sum or maximum over the GS threads of a group, the same in each of them.  `scratch` is another one for each of two joins that
+// follow each other, so that one barrier a join is enough.
+template <int GS, bool MAX> __device__ __forceinline__ float group_join(float v, float (*scratch)[32])
 {
     constexpr int kLanes = GS < 32 ? GS : 32;
 #pragma unroll
@@ -148,13 +231,14 @@ template <int GS, bool MAX> __device__ __forceinline__ float group_join(float v,
         const float w = __shfl_xor_sync(0xffffffffu, v, o);
         v = MAX ? fmaxf(v, w) : v + w;
     }
-    if constexpr (GS > 32) {  // the group is the block; scratch is used in turn, so that one barrier a join is enough
-        if (threadIdx.x % 32 == 0) scratch[threadIdx.x / 32] = v;
-        __syncthreads();
-        v = scratch[threadIdx.x % 32 < GS / 32 ? threadIdx.x % 32 : 0];
-        if (!MAX && threadIdx.x % 32 >= GS / 32) v = 0.f;
+    if constexpr (GS > 32) {
+        constexpr int kWarps = GS / 32;
+        float *mine = *scratch + threadIdx.x / GS * kWarps;
+        if (threadIdx.x % 32 == 0) mine[threadIdx.x % GS / 32] = v;
+        asm volatile("bar.sync %0, %1;" ::"r"((int)threadIdx.x / GS + 1), "n"(GS) : "memory");
+        v = mine[threadIdx.x % kWarps];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
+        for (int o = kWarps / 2; o > 0; o >>= 1) {
             const float w = __shfl_xor_sync(0xffffffffu, v, o);
             v = MAX ? fmaxf(v, w) : v + w;
         }
@@ -162,216 +246,502 @@ template <int GS, bool MAX> __device__ __forceinline__ float group_join(float v,
     return v;
 }
 
-// scale s + bias of V adjacent keys; -inf where not live
-template <int V> __device__ __forceinline__ void logits(const Tables &t, const Row &w, int c, float scale, float (&x)[V])
+// ---- weights -------------------------------------------------------------------------------
+
+// The head's bias.  By distance: entry d of copy k at [k][d + reach + k], reach being max_distance and the 8 keys of an access more,
+// in rows of `pitch`.  Otherwise: the buckets of all distances, and the bias of each bucket behind them.
+struct Bias {
+    const float *by_distance;
+    const unsigned char *bucket;
+    int max_distance, reach, pitch;
+    float behind, ahead;  // of distances beyond it
+};
+__host__ __device__ inline int bias_reach(int max_distance) { return max_distance + 8; }
+__host__ __device__ inline int bias_pitch(int max_distance) { return (2 * bias_reach(max_distance) + 1 + 8 + 3) / 4 * 4; }
+__host__ __device__ inline int bucket_bytes(int max_distance) { return (2 * max_distance + 1 + 15) / 16 * 16; }
+__host__ __device__ inline size_t bias_bytes(int max_distance, int n_buckets)
 {
-    const int d = c - w.pos, first = t.at(d), last = t.at(d + V - 1);
-    if (first == last) {
-        const float bias = t.bias[first];
+    return max_distance <= kCopiesMax ? 16 * (size_t)bias_pitch(max_distance) : bucket_bytes(max_distance) + 16 * (size_t)((n_buckets + 3) / 4);
+}
+
+__device__ __forceinline__ Bias make_bias(const PositionArgs &a, int head, unsigned char *room)
+{
+    Bias t;
+    const int m = a.buckets.max_distance;
+    t.max_distance = m;
+    t.reach = bias_reach(m);
+    t.pitch = bias_pitch(m);
+    const auto value = [&](int d) {
+        d = d < -m ? -m : d > m ? m : d;
+        return a.table[bucket_of(a.buckets, d) * a.ld_table + head];
+    };
+    t.behind = value(-m);
+    t.ahead = value(m);
+    float *f = reinterpret_cast<float *>(room);
+    if (m <= kCopiesMax) {
+        for (int i = threadIdx.x; i < t.pitch; i += blockDim.x) {
+            const float v = value(i - t.reach);
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[e] = fmaf(scale, x[e], bias);
+            for (int k = 0; k < 4; ++k)
+                if (i + k < t.pitch) f[k * t.pitch + i + k] = v;
+        }
+        t.by_distance = f;
+        t.bucket = nullptr;
+    } else {
+        for (int i = threadIdx.x; i <= 2 * m; i += blockDim.x) room[i] = (unsigned char)bucket_of(a.buckets, i - m);
+        f = reinterpret_cast<float *>(room + bucket_bytes(m));
+        for (int i = threadIdx.x; i < a.buckets.n; i += blockDim.x) f[i] = a.table[i * a.ld_table + head];
+        t.by_distance = f;
+        t.bucket = room;
+    }
+    return t;
+}
+// Of V adjacent keys, the first at distance d.
+template <int P> __device__ __forceinline__ void bias_of(const Bias &t, int d, f2 (&bias)[P])
+{
+    const int m = t.max_distance;
+    if (d >= m || d + 2 * P - 1 <= -m) {
+        const float v = d >= m ? t.ahead : t.behind;
+#pragma unroll
+        for (int i = 0; i < P; ++i) bias[i] = pack2(v, v);
+    } else if (!t.bucket) {
+        const int at = d + t.reach, k = -at & 3;  // of the copy in which this entry begins 16 bytes
+        const ulonglong2 *p = reinterpret_cast<const ulonglong2 *>(t.by_distance + k * t.pitch + at + k);
+#pragma unroll
+        for (int i = 0; i < P / 2; ++i) {
+            const ulonglong2 q = p[i];
+            bias[2 * i] = q.x;
+            bias[2 * i + 1] = q.y;
+        }
     } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[e] = fmaf(scale, x[e], t.bias[t.at(d + e)]);
-    }
-    if (c < 0 || c + V > w.live) {
+        for (int i = 0; i < P; ++i) {
+            float v[2];
 #pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (c + e < 0 || c + e >= w.live) x[e] = -INFINITY;
+            for (int k = 0; k < 2; ++k) {
+                const int e = d + 2 * i + k, near = e < -m ? -m : e > m ? m : e;
+                v[k] = t.by_distance[t.bucket[near + m]];
+            }
+            bias[i] = pack2(v[0], v[1]);
+        }
     }
 }
 
-// 2^((x - top) log2 e): the difference is taken first, so that large logits lose nothing
-__device__ __forceinline__ float exp_of(float x, float top)
+__device__ __forceinline__ float exp2_of(float x)
 {
     float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"((x - top) * kLog2e));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// 2^((x - top) log2 e).  The factor is not in the logits: the type's lowest value would be infinite with it, and a row of
+// nothing else has weights all the same.
+__device__ __forceinline__ float exp_of(float x, float top) { return exp2_of((x - top) * kLog2e); }
+template <int P> __device__ __forceinline__ void exp_of(f2 (&x)[P], float top)
+{
+    const f2 less = pack2(-top, -top), log2e = pack2(kLog2e, kLog2e);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        float lo, hi;
+        unpack2(mul2(add2(x[i], less), log2e), lo, hi);
+        x[i] = pack2(exp2_of(lo), exp2_of(hi));
+    }
+}
+// off by one unit in the last place at most
+__device__ __forceinline__ float reciprocal(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+template <int P> __device__ __forceinline__ float sum_of(const f2 (&x)[P])
+{
+    f2 s = x[0];
+#pragma unroll
+    for (int i = 1; i < P; ++i) s = add2(s, x[i]);
+    float lo, hi;
+    unpack2(s, lo, hi);
+    return lo + hi;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+template <int P> __device__ __forceinline__ float max_of(const f2 (&x)[P], float m)
+{
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        float lo, hi;
+        unpack2(x[i], lo, hi);
+        m = max3(m, lo, hi);
+    }
+    return m;
+}
+
+// Logits of V adjacent keys; -inf where not live.
+template <bool EVEN, typename T, int P>
+__device__ __forceinline__ void logits(const Bias &t, const Row &w, const uint4 &raw, int c, float scale, f2 (&x)[P])
+{
+    f2 bias[P];
+    spread(raw, x, T());
+    bias_of(t, c - w.pos, bias);
+#pragma unroll
+    for (int i = 0; i < P; ++i) x[i] = fma2(pack2(scale, scale), x[i], bias[i]);
+    keep_live<EVEN>(x, c, w.live, -INFINITY);
+}
+
+// Blocks of an SM: registers for E elements a thread, without spilling, decide.
+template <int GS, int E> constexpr int kSoftmaxBlocks = GS > 256 ? 1 : E > 16 ? 3 : 4;
 
 // GS threads a row, E elements a thread; LONG: rows of any length, read twice.
-template <typename T, int GS, int E, bool LONG>
-__global__ void __launch_bounds__(GS > 256 ? GS : 256) k_softmax(const PositionArgs a)
+template <typename T, int GS, int E, bool LONG, bool EVEN>
+__global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<GS, E>) k_softmax(const __grid_constant__ PositionArgs a)
 {
-    constexpr int V = 16 / sizeof(T), NV = E / V, kThreads = GS > 256 ? GS : 256, kGroups = kThreads / GS;
+    constexpr int V = 16 / sizeof(T), P = V / 2, NV = E / V, kThreads = GS > 256 ? GS : 256, kGroups = kThreads / GS;
     extern __shared__ __align__(16) unsigned char room[];
-    __shared__ float scratch[3][32];
+    __shared__ float scratch[2][32];
     griddep_wait();
     griddep_launch();
     const int head = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-    const Tables t = make_tables(a, head, room, true);
+    const Bias t = make_bias(a, head, room);
     __syncthreads();
-    const long long begin = a.rows * chunk / a.chunks, end = a.rows * (chunk + 1) / a.chunks;
-    const int group = threadIdx.x / GS, lane = threadIdx.x % GS;
-    for (long long r = begin; r < end; r += kGroups) {
-        const Row w = row_of(a, r + group, end);
-        const int n = r + group < end ? a.n_keys : 0;
-        const T *s = row_at<T>(a.s, a.s_at, w, head);
-        T *p = row_at<T>(a.out, a.out_at, w, head);
-        const int off = off16(s);
+    const int lane = threadIdx.x % GS;
+    constexpr bool kAhead = kRowsAhead<T, LONG, EVEN>;
+    uint4 *mine = reinterpret_cast<uint4 *>(room + bias_bytes(a.buckets.max_distance, a.buckets.n)) + threadIdx.x;
+    const auto request = [&](const Row &w) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if ((v * GS + lane) * V < w.live) copy_async(mine + v * kThreads, static_cast<const T *>(a.s) + w.at + (v * GS + lane) * V);
+        copy_commit();
+    };
+    // where the thread's v-th access begins, in a row on a 16-byte boundary
+    const auto at = [&](int v) { return (v * GS + lane) * V; };
+    Walk<kGroups> walk(a, head, chunk, threadIdx.x / GS);
+    Row w = walk.here(a), next;
+    if constexpr (kAhead) request(w);
+    // the groups of a block take as many rounds
+    for (unsigned r = chunk * kGroups; r < (unsigned)a.rows; r += walk.step, w = next) {
+        walk.next(a);
+        next = walk.here(a);
+        const int n = w.n;
+        const T *s = static_cast<const T *>(a.s) + w.at;
+        T *p = static_cast<T *>(a.out) + (EVEN ? w.at : offset_of(a.out_at, w, head));
+        const int off = EVEN ? 0 : off16(s);
         const bool aligned = off16(p) == off;
         if constexpr (!LONG) {
-            float x[NV][V], top = -INFINITY, sum = 0.f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) load_cols<T, V>(s, (v * GS + lane) * V - off, w.live, true, x[v]);
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                logits<V>(t, w, (v * GS + lane) * V - off, a.scale, x[v]);
-#pragma unroll
-                for (int e = 0; e < V; ++e) top = fmaxf(top, x[v][e]);
-            }
-            top = group_join<GS, true>(top, scratch[0]);
-            if (top == -INFINITY) top = 0.f;  // nothing is live, all is -inf, or the rest is NaN
+            f2 x[NV][P];
+            uint4 raw[NV];
+            float top = -INFINITY, sum = 0.f;
+            if constexpr (kAhead) copy_wait<0>();
 #pragma unroll
             for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum += x[v][e] = exp_of(x[v][e], top);
-            sum = group_join<GS, false>(sum, scratch[1]);
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                if (at(v) - off < w.live) raw[v] = kAhead ? mine[v * kThreads] : load_raw<EVEN>(s, at(v) - off, n, true);
+            // the group's accesses that end before `plain` are live and far behind: most of them, with nothing to look up
+            const int plain = EVEN ? min(w.live, w.pos - t.max_distance + 1) : 0;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int c = (v * GS + lane) * V - off;
-                if (c >= n) break;
+                const int c = at(v) - off;
+                if ((v + 1) * GS * V <= plain) {
+                    const f2 factor = pack2(a.scale, a.scale), bias = pack2(t.behind, t.behind);
+                    spread(raw[v], x[v], T());
 #pragma unroll
-                for (int e = 0; e < V; ++e) x[v][e] = c + e < w.live ? x[v][e] * inv : 0.f;  // not NaN where not live
-                store_cols<T, V>(p, c, n, aligned, x[v]);
+                    for (int i = 0; i < P; ++i) x[v][i] = fma2(factor, x[v][i], bias);
+                    top = max_of(x[v], top);
+                } else if (c < w.live) {
+                    logits<EVEN, T, P>(t, w, raw[v], c, a.scale, x[v]);
+                    top = max_of(x[v], top);
+                } else if (v * GS * V - off < w.live) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) x[v][i] = pack2(-INFINITY, -INFINITY);
+                }
             }
-            if constexpr (GS > 32) __syncthreads();  // scratch is free for the next row
+            top = group_join<GS, true>(top, scratch);
+            if constexpr (kAhead) request(next);  // its place has been read
+            if (top == -INFINITY) top = 0.f;  // nothing is live, all is -inf, or the rest is NaN
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                if (v * GS * V - off < w.live) {
+                    exp_of(x[v], top);
+                    sum += sum_of(x[v]);
+                }
+            }
+            sum = group_join<GS, false>(sum, scratch + 1);
+            const float inv = sum == 0.f ? 0.f : reciprocal(sum);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = at(v) - off;
+                if (v * GS * V - off < w.live) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) x[v][i] = mul2(x[v][i], pack2(inv, inv));
+                    if (inv != inv) keep_live<EVEN>(x[v], c, w.live, 0.f);  // NaN, but not where nothing is live
+                } else {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) x[v][i] = 0ull;
+                }
+                if (c < n) store_cols<EVEN, T, P>(p, c, n, aligned, x[v]);
+            }
         } else {
             float top = -INFINITY, sum = 0.f;
             for (int c = lane * V - off; c < w.live; c += GS * V) {
-                float x[V], best = top;
-                load_cols<T, V>(s, c, w.live, true, x);
-                logits<V>(t, w, c, a.scale, x);
-#pragma unroll
-                for (int e = 0; e < V; ++e) best = fmaxf(best, x[e]);
-                const float base = best == -INFINITY ? 0.f : best;
-                sum *= exp_of(top == -INFINITY ? base : top, base);
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum += exp_of(x[e], base);
+                f2 x[P];
+                logits<EVEN, T, P>(t, w, load_raw<EVEN>(s, c, n, true), c, a.scale, x);
+                const float best = max_of(x, top), base = best == -INFINITY ? 0.f : best;
+                exp_of(x, base);
+                sum = sum * exp_of(top == -INFINITY ? base : top, base) + sum_of(x);
                 top = best;
             }
-            float all = group_join<GS, true>(top, scratch[0]);
+            float all = group_join<GS, true>(top, scratch);
             if (all == -INFINITY) all = 0.f;
-            sum = group_join<GS, false>(sum * exp_of(top == -INFINITY ? all : top, all), scratch[1]);
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            sum = group_join<GS, false>(sum * exp_of(top == -INFINITY ? all : top, all), scratch + 1);
+            const float inv = sum == 0.f ? 0.f : reciprocal(sum);
             for (int c = lane * V - off; c < n; c += GS * V) {
-                float x[V];
-                load_cols<T, V>(s, c, w.live, true, x);
-                logits<V>(t, w, c, a.scale, x);
+                f2 x[P] = {};
+                if (c < w.live) {
+                    logits<EVEN, T, P>(t, w, load_raw<EVEN>(s, c, n, true), c, a.scale, x);
+                    exp_of(x, all);
 #pragma unroll
-                for (int e = 0; e < V; ++e) x[e] = c + e < w.live ? exp_of(x[e], all) * inv : 0.f;
-                store_cols<T, V>(p, c, n, aligned, x);
+                    for (int i = 0; i < P; ++i) x[i] = mul2(x[i], pack2(inv, inv));
+                    if (inv != inv) keep_live<EVEN>(x, c, w.live, 0.f);
+                }
+                store_cols<EVEN, T, P>(p, c, n, aligned, x);
             }
-            __syncthreads();
         }
     }
 }
 
 // ---- gradient ------------------------------------------------------------------------------
 
-// Adds V adjacent values to the lane's sums by bucket.
-template <int V> __device__ __forceinline__ void add_buckets(const Tables &t, float *lane_sums, int d, const float (&g)[V], float &behind, float &ahead)
+// Near the diagonal adjacent keys are in different buckets: those are summed by distance, in registers.  A warp puts its values at the
+// keys from 64 before the query to 72 behind it, in whole accesses, into shared memory, and lane l takes the distances
+// l - 72, l - 40, ... from there.  (One by one into the sums by bucket: 9 instructions a key, 100 of 640 a row of 1024.)
+constexpr int kNear = 64, kNearKeys = 2 * kNear + 16, kNearTakes = 5;
+struct Near {
+    float *room;  // [kNearKeys] of this warp
+    float sum[kNearTakes];
+    __device__ __forceinline__ static int distance(int k) { return (int)threadIdx.x % 32 - kNear - 8 + 32 * k; }
+    // The first key: as many elements behind a boundary of 8 as the rows begin before one.
+    __device__ __forceinline__ static int first(const Row &w, int off) { return ((w.pos - kNear + off) & ~7) - off; }
+};
+
+// Shared memory before the rows that are on their way: the buckets by distance, the sums.
+__host__ __device__ inline size_t grad_bytes(int max_distance, int n_buckets)
 {
-    if (d + V - 1 <= -t.max_distance || d >= t.max_distance) {
-        float all = 0.f;
-#pragma unroll
-        for (int e = 0; e < V; ++e) all += g[e];
-        if (d < 0) behind += all;
-        else ahead += all;
-        return;
-    }
-    const int first = t.at(d), last = t.at(d + V - 1);
-    if (first == last) {
-        float all = 0.f;
-#pragma unroll
-        for (int e = 0; e < V; ++e) all += g[e];
-        lane_sums[first * 32] += all;
+    return bucket_bytes(max_distance) + (n_buckets ? 8 * (128 * (size_t)n_buckets + 4 * kNearKeys) : 0);
+}
+
+// Adds V adjacent values, the first at distance d, to the lane's sums by bucket.
+template <int P>
+__device__ __forceinline__ void add_buckets(const unsigned char *bucket, int m, float *lane_sums, int d, const f2 (&g)[P], float &behind, float &ahead)
+{
+    if (d + 2 * P - 1 <= -m) {
+        behind += sum_of(g);
+    } else if (d >= m) {
+        ahead += sum_of(g);
     } else {
+        const auto at = [&](int e) {
+            e = e < -m ? -m : e > m ? m : e;
+            return (int)bucket[e + m];
+        };
+        const int first = at(d), last = at(d + 2 * P - 1);
+        if (first == last) {
+            lane_sums[first * 32] += sum_of(g);
+        } else {
+            float y[2 * P];
+            flat(g, y);
 #pragma unroll
-        for (int e = 0; e < V; ++e) lane_sums[t.at(d + e) * 32] += g[e];
+            for (int e = 0; e < 2 * P; ++e) lane_sums[at(d + e) * 32] += y[e];
+        }
     }
 }
 
-template <typename T, int GS, int E, bool LONG> __global__ void __launch_bounds__(256) k_softmax_grad(const PositionArgs a)
+// Two raw rows a thread: E elements of 2 or 4 bytes each.
+template <typename T, int E> constexpr int kGradBlocks = E * (int)sizeof(T) > 64 ? 2 : E * (int)sizeof(T) == 64 ? 3 : 4;
+
+template <typename T, int GS, int E, bool LONG, bool EVEN>
+__global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const __grid_constant__ PositionArgs a)
 {
-    constexpr int V = 16 / sizeof(T), NV = E / V, kGroups = 256 / GS;
+    constexpr int V = 16 / sizeof(T), P = V / 2, NV = E / V, kGroups = 256 / GS;
     extern __shared__ __align__(16) unsigned char room[];
-    __shared__ float scratch[32];
+    __shared__ float scratch[2][32];
+    int turn = 0;
     griddep_wait();
     if (a.partials) griddep_launch();  // the successor is another kernel of this call
-    const int head = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-    const Tables t = make_tables(a, head, room, false);
-    float *sums = t.bias;  // [warp][bucket][lane]
+    const int head = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, m = a.buckets.max_distance;
+    float *sums = reinterpret_cast<float *>(room + bucket_bytes(m));  // [warp][bucket][lane]
     const int n_buckets = a.buckets.n;
-    if (a.partials)
-        for (int i = threadIdx.x; i < 8 * n_buckets * 32; i += 256) sums[i] = 0.f;
+    if (a.partials) {
+        for (int i = threadIdx.x; i <= 2 * m; i += 256) room[i] = (unsigned char)bucket_of(a.buckets, i - m);
+        for (int i = threadIdx.x; i < 8 * n_buckets * 8; i += 256) reinterpret_cast<float4 *>(sums)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
     __syncthreads();
     float *lane_sums = sums + (threadIdx.x / 32) * n_buckets * 32 + threadIdx.x % 32;
     float behind = 0.f, ahead = 0.f;
-    const long long begin = a.rows * chunk / a.chunks, end = a.rows * (chunk + 1) / a.chunks;
-    const int group = threadIdx.x / GS, lane = threadIdx.x % GS;
-    for (long long r = begin; r < end; r += kGroups) {
-        const Row w = row_of(a, r + group, end);
-        const int n = r + group < end ? a.n_keys : 0;
-        const T *p = row_at<T>(a.s, a.s_at, w, head), *dp = row_at<T>(a.dp, a.dp_at, w, head);
-        T *ds = row_at<T>(a.out, a.out_at, w, head);
-        const int off = off16(p);
+    f2 behind2 = 0ull;
+    const int far_from = m > kNear + 8 ? m : kNear + 8;  // keys so far behind are in the last bucket and none of those by distance
+    constexpr bool kByDistance = GS >= 32;
+    constexpr unsigned kWarps = GS < 32 ? 1 : GS / 32;
+    Near near;
+    near.room = sums + 8 * n_buckets * 32 + threadIdx.x / 32 * kNearKeys;
+#pragma unroll
+    for (int k = 0; k < kNearTakes; ++k) near.sum[k] = 0.f;
+    const int lane = threadIdx.x % GS;
+    const f2 scale = pack2(a.scale, a.scale);
+    const auto at = [&](int v) { return (v * GS + lane) * V; };
+    constexpr bool kAhead = kRowsAhead<T, LONG, EVEN>;
+    uint4 *mine = reinterpret_cast<uint4 *>(room + grad_bytes(m, a.partials ? n_buckets : 0)) + threadIdx.x;
+    const auto request = [&](const Row &w) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * GS + lane) * V;
+            if (c < w.live) {
+                copy_async(mine + 2 * v * 256, static_cast<const T *>(a.s) + w.at + c);
+                copy_async(mine + (2 * v + 1) * 256, static_cast<const T *>(a.dp) + w.at + c);
+            }
+        }
+        copy_commit();
+    };
+    Walk<kGroups> walk(a, head, chunk, threadIdx.x / GS);
+    Row w = walk.here(a), next;
+    if constexpr (kAhead) request(w);
+    for (unsigned r = chunk * kGroups; r < (unsigned)a.rows; r += walk.step, w = next) {
+        walk.next(a);
+        next = walk.here(a);
+        const int n = w.n;
+        const T *p = static_cast<const T *>(a.s) + w.at, *dp = static_cast<const T *>(a.dp) + (EVEN ? w.at : offset_of(a.dp_at, w, head));
+        T *ds = static_cast<T *>(a.out) + (EVEN ? w.at : offset_of(a.out_at, w, head));
+        const int off = EVEN ? 0 : off16(p);
         const bool aligned = off16(dp) == off, out_aligned = off16(ds) == off;
+        const int near_first = Near::first(w, off);
+        // of V adjacent keys, with zeros where nothing is live: g, its sums, ds
+        const auto finish = [&](const uint4 &p_raw, const uint4 &dp_raw, int c, float dot) {
+            f2 g[P], y[P];
+            if (c < w.live) {
+                const f2 less = pack2(-dot, -dot);
+                spread(p_raw, g, T());
+                spread(dp_raw, y, T());
+#pragma unroll
+                for (int i = 0; i < P; ++i) g[i] = mul2(g[i], add2(y[i], less));
+                if (!isfinite(dot)) keep_live<EVEN>(g, c, w.live, 0.f);
+                if (a.partials) {
+                    if (kByDistance && (unsigned)(c - near_first) < (unsigned)kNearKeys) {
+                        float x[V];
+                        flat(g, x);
+                        store_vec<V>(near.room + (c - near_first), x);
+                    } else {
+                        add_buckets<P>(room, m, lane_sums, c - w.pos, g, behind, ahead);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < P; ++i) y[i] = mul2(g[i], scale);
+            } else {
+#pragma unroll
+                for (int i = 0; i < P; ++i) y[i] = 0ull;
+            }
+            if (a.out) store_cols<EVEN, T, P>(ds, c, n, out_aligned, y);
+        };
+        const auto products = [&](const uint4 &p_raw, const uint4 &dp_raw, f2 sum) {
+            f2 x[P], y[P];
+            spread(p_raw, x, T());
+            spread(dp_raw, y, T());
+#pragma unroll
+            for (int i = 0; i < P; ++i) sum = fma2(x[i], y[i], sum);
+            return sum;
+        };
+        // zeros where nothing is live
+        const auto fetch = [&](int c, uint4 &p_raw, uint4 &dp_raw) {
+            p_raw = load_raw<EVEN>(p, c, n, true);
+            dp_raw = load_raw<EVEN>(dp, c, n, aligned);
+            keep_live<EVEN, T>(p_raw, c, w.live);
+            keep_live<EVEN, T>(dp_raw, c, w.live);
+        };
+        f2 sum = 0ull;
+        float dot, odd;
         if constexpr (!LONG) {
-            float x[NV][V], y[NV][V], dot = 0.f;
+            uint4 x[NV], y[NV];
+            if constexpr (kAhead) copy_wait<0>();
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                load_cols<T, V>(p, (v * GS + lane) * V - off, w.live, true, x[v]);
-                load_cols<T, V>(dp, (v * GS + lane) * V - off, w.live, aligned, y[v]);
+                const int c = at(v) - off;
+                if (c < w.live) {
+                    x[v] = kAhead ? mine[2 * v * 256] : load_raw<EVEN>(p, c, n, true);
+                    y[v] = kAhead ? mine[(2 * v + 1) * 256] : load_raw<EVEN>(dp, c, n, aligned);
+                }
             }
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int e = 0; e < V; ++e) dot = fmaf(x[v][e], y[v][e], dot);
-            dot = group_join<GS, false>(dot, scratch);
+            for (int v = 0; v < NV; ++v) {
+                const int c = at(v) - off;
+                if (c < w.live) {
+                    if (!EVEN || (v + 1) * GS * V > w.live) {
+                        keep_live<EVEN, T>(x[v], c, w.live);
+                        keep_live<EVEN, T>(y[v], c, w.live);
+                    }
+                    sum = products(x[v], y[v], sum);
+                }
+            }
+            unpack2(sum, dot, odd);
+            dot = group_join<GS, false>(dot + odd, scratch + (turn ^= 1));
+            if constexpr (kAhead) request(next);  // its place has been read
+            // the group's accesses that end before `plain` are live and in the last bucket
+            const int plain = EVEN && isfinite(dot) ? min(w.live, w.pos - far_from) : 0;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int c = (v * GS + lane) * V - off;
-                if (c >= n) break;
+                if ((v + 1) * GS * V <= plain) {
+                    f2 g[P], d[P];
+                    const f2 less = pack2(-dot, -dot);
+                    spread(x[v], g, T());
+                    spread(y[v], d, T());
 #pragma unroll
-                for (int e = 0; e < V; ++e) x[v][e] = c + e >= 0 && c + e < w.live ? x[v][e] * (y[v][e] - dot) : 0.f;
-                if (a.partials && c < w.live) add_buckets<V>(t, lane_sums, c - w.pos, x[v], behind, ahead);
-                if (a.out) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) x[v][e] *= a.scale;
-                    store_cols<T, V>(ds, c, n, out_aligned, x[v]);
+                    for (int i = 0; i < P; ++i) {
+                        g[i] = mul2(g[i], add2(d[i], less));
+                        behind2 = add2(behind2, g[i]);
+                        d[i] = mul2(g[i], scale);
+                    }
+                    if (a.out) store_cols<EVEN, T, P>(ds, at(v), n, true, d);
+                } else if (at(v) - off < n) {
+                    finish(x[v], y[v], at(v) - off, dot);
                 }
             }
         } else {
-            float dot = 0.f;
+            uint4 x, y;
             for (int c = lane * V - off; c < w.live; c += GS * V) {
-                float x[V], y[V];
-                load_cols<T, V>(p, c, w.live, true, x);
-                load_cols<T, V>(dp, c, w.live, aligned, y);
-#pragma unroll
-                for (int e = 0; e < V; ++e) dot = fmaf(x[e], y[e], dot);
+                fetch(c, x, y);
+                sum = products(x, y, sum);
             }
-            dot = group_join<GS, false>(dot, scratch);
+            unpack2(sum, dot, odd);
+            dot = group_join<GS, false>(dot + odd, scratch + (turn ^= 1));
             for (int c = lane * V - off; c < n; c += GS * V) {
-                float x[V], y[V];
-                load_cols<T, V>(p, c, w.live, true, x);
-                load_cols<T, V>(dp, c, w.live, aligned, y);
-#pragma unroll
-                for (int e = 0; e < V; ++e) x[e] = c + e >= 0 && c + e < w.live ? x[e] * (y[e] - dot) : 0.f;
-                if (a.partials && c < w.live) add_buckets<V>(t, lane_sums, c - w.pos, x, behind, ahead);
-                if (a.out) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) x[e] *= a.scale;
-                    store_cols<T, V>(ds, c, n, out_aligned, x);
-                }
+                if (c < w.live) fetch(c, x, y);
+                finish(x, y, c, dot);
             }
         }
-        if constexpr (GS > 32) __syncthreads();  // scratch is free for the next row
+        if (kByDistance && a.partials) {
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < kNearTakes; ++k) {
+                if (a.causal && k > 2) break;  // distances from 24 on
+                const int j = w.pos + Near::distance(k);
+                // live, and one of this warp's
+                if (j >= 0 && j < w.live && (GS == 32 || (unsigned)(j + off) / (32 * V) % kWarps == threadIdx.x % GS / 32) &&
+                    (unsigned)(j - near_first) < (unsigned)kNearKeys)
+                    near.sum[k] += near.room[j - near_first];
+            }
+            __syncwarp();
+        }
     }
     if (!a.partials) return;
-    lane_sums[t.at(-t.max_distance) * 32] += behind;
-    lane_sums[t.at(t.max_distance) * 32] += ahead;
+    if constexpr (kByDistance) {
+#pragma unroll
+        for (int k = 0; k < kNearTakes; ++k) {
+            int d = Near::distance(k);
+            d = d < -m ? -m : d > m ? m : d;
+            lane_sums[room[d + m] * 32] += near.sum[k];
+        }
+    }
+    float lo, hi;
+    unpack2(behind2, lo, hi);
+    lane_sums[room[0] * 32] += behind + (lo + hi);
+    lane_sums[room[2 * m] * 32] += ahead;
     __syncthreads();
     // a warp adds up a bucket: lane by lane over the warps, then over the lanes
     for (int k = threadIdx.x / 32; k < n_buckets; k += 8) {
@@ -489,67 +859,78 @@ template <typename A> bool writable(const A &a, long long b, long long h, long l
     return true;
 }
 
-// Head by head, in chunks of rows: enough blocks to fill the device several times over, fewer where there are few rows.
-int chunks_of(long long rows, long long heads, int groups, int sms, int blocks_per_sm)
+// Blocks of a head: as many as the device holds at once, fewer where there are few rows.
+int chunks_of(long long rows, long long heads, int groups, int sms, int blocks, size_t smem)
 {
-    const long long want = ceil_div((long long)sms * blocks_per_sm, heads), most = std::max<long long>(1, kBlocksMax / heads);
+    const long long held = std::max<long long>(1, std::min<long long>(blocks, (227 << 10) / (long long)(smem + 2048)));  // beside static and reserved memory
+    const long long want = std::max<long long>(1, sms * held / heads), most = std::max<long long>(1, kBlocksMax / heads);
     return (int)std::max<long long>(1, std::min(std::min(want, most), ceil_div(rows, groups)));
 }
 
-template <typename T, int GS, int E, bool LONG> cudaError_t run_softmax(PositionArgs &a, int heads, int sms, cudaStream_t s)
+template <typename T, int GS, int E, bool LONG, bool EVEN> cudaError_t run_softmax(PositionArgs &a, int heads, int sms, cudaStream_t s)
 {
     static OncePerDevice known;
     constexpr int kThreads = GS > 256 ? GS : 256;
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_softmax<T, GS, E, LONG>), known);
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_softmax<T, GS, E, LONG, EVEN>), known);
     if (e != cudaSuccess) return e;
-    a.chunks = chunks_of(a.rows, heads, kThreads / GS, sms, 2048 / kThreads);
-    const size_t smem = bucket_bytes(a.buckets.max_distance) + 4 * (size_t)a.buckets.n;
-    return launch(k_softmax<T, GS, E, LONG>, (long long)heads * a.chunks, kThreads, smem, s, a);
+    const size_t smem = bias_bytes(a.buckets.max_distance, a.buckets.n) + (kRowsAhead<T, LONG, EVEN> ? kThreads * E * sizeof(T) : 0);
+    a.chunks = chunks_of(a.rows, heads, kThreads / GS, sms, kSoftmaxBlocks<GS, E>, smem);
+    return launch(k_softmax<T, GS, E, LONG, EVEN>, (long long)heads * a.chunks, kThreads, smem, s, a);
+}
+// Whether all rows of a matrix begin on 16-byte boundaries.
+template <typename T> bool on16(const void *p, const Strides &at)
+{
+    constexpr long long V = 16 / (long long)sizeof(T);
+    return !p || (on(p, 16) && at.b % V == 0 && at.h % V == 0 && at.q % V == 0);
 }
 // The elements that a row's group has to hold: with rows off 16-byte boundaries up to V - 1 before it too.
 template <typename T> long long held(const PositionArgs &a)
 {
-    constexpr long long V = 16 / (long long)sizeof(T);
-    const bool aligned = on(a.s, 16) && a.s_at.b % V == 0 && a.s_at.h % V == 0 && a.s_at.q % V == 0;
-    return a.n_keys + (aligned ? 0 : V - 1);
+    return a.n_keys + (on16<T>(a.s, a.s_at) ? 0 : 16 / (long long)sizeof(T) - 1);
+}
+template <typename T> bool all_even(const PositionArgs &a)
+{
+    const auto same = [&](const void *p, const Strides &at) { return !p || (on(p, 16) && at.b == a.s_at.b && at.h == a.s_at.h && at.q == a.s_at.q); };
+    return a.n_keys % (16 / (int)sizeof(T)) == 0 && on16<T>(a.s, a.s_at) && same(a.dp, a.dp_at) && same(a.out, a.out_at);
 }
 // The narrowest group whose registers hold a row.
-template <typename T> cudaError_t pick_softmax(PositionArgs &a, int heads, int sms, cudaStream_t s)
+template <typename T, bool EVEN> cudaError_t pick_softmax(PositionArgs &a, int heads, int sms, cudaStream_t s)
 {
     const long long n = held<T>(a);
-    if (n <= 8 * 8) return run_softmax<T, 8, 8, false>(a, heads, sms, s);
-    if (n <= 8 * 16) return run_softmax<T, 8, 16, false>(a, heads, sms, s);
-    if (n <= 32 * 8) return run_softmax<T, 32, 8, false>(a, heads, sms, s);
-    if (n <= 32 * 16) return run_softmax<T, 32, 16, false>(a, heads, sms, s);
-    if (n <= 32 * 32) return run_softmax<T, 32, 32, false>(a, heads, sms, s);
-    if (n <= 256 * 8) return run_softmax<T, 256, 8, false>(a, heads, sms, s);
-    if (n <= 256 * 16) return run_softmax<T, 256, 16, false>(a, heads, sms, s);
-    if (n <= 256 * 32) return run_softmax<T, 256, 32, false>(a, heads, sms, s);
-    if (n <= 1024 * 32) return run_softmax<T, 1024, 32, false>(a, heads, sms, s);
-    return run_softmax<T, 1024, 8, true>(a, heads, sms, s);
+    if (n <= 8 * 8) return run_softmax<T, 8, 8, false, EVEN>(a, heads, sms, s);
+    if (n <= 8 * 16) return run_softmax<T, 8, 16, false, EVEN>(a, heads, sms, s);
+    if (n <= 32 * 8) return run_softmax<T, 32, 8, false, EVEN>(a, heads, sms, s);
+    if (n <= 32 * 16) return run_softmax<T, 32, 16, false, EVEN>(a, heads, sms, s);
+    if (n <= 32 * 32) return run_softmax<T, 32, 32, false, EVEN>(a, heads, sms, s);
+    if (n <= 64 * 32) return run_softmax<T, 64, 32, false, EVEN>(a, heads, sms, s);
+    if (n <= 128 * 32) return run_softmax<T, 128, 32, false, EVEN>(a, heads, sms, s);
+    if (n <= 256 * 32) return run_softmax<T, 256, 32, false, EVEN>(a, heads, sms, s);
+    if (n <= 1024 * 16) return run_softmax<T, 1024, 16, false, EVEN>(a, heads, sms, s);
+    return run_softmax<T, 1024, 8, true, EVEN>(a, heads, sms, s);
 }
 
-template <typename T, int GS, int E, bool LONG> cudaError_t run_grad(PositionArgs &a, int heads, int sms, cudaStream_t s)
+template <typename T, int GS, int E, bool LONG, bool EVEN> cudaError_t run_grad(PositionArgs &a, int heads, int sms, cudaStream_t s)
 {
     static OncePerDevice known;
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_softmax_grad<T, GS, E, LONG>), known);
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_softmax_grad<T, GS, E, LONG, EVEN>), known);
     if (e != cudaSuccess) return e;
-    a.chunks = chunks_of(a.rows, heads, 256 / GS, sms, 8);
-    const size_t smem = bucket_bytes(a.buckets.max_distance) + (a.partials ? 8 * 128 * (size_t)a.buckets.n : 0);
-    return launch(k_softmax_grad<T, GS, E, LONG>, (long long)heads * a.chunks, 256, smem, s, a);
+    const size_t smem = grad_bytes(a.buckets.max_distance, a.partials ? a.buckets.n : 0) + (kRowsAhead<T, LONG, EVEN> ? 256 * 2 * E * sizeof(T) : 0);
+    a.chunks = chunks_of(a.rows, heads, 256 / GS, sms, kGradBlocks<T, E>, smem);
+    return launch(k_softmax_grad<T, GS, E, LONG, EVEN>, (long long)heads * a.chunks, 256, smem, s, a);
 }
-template <typename T> cudaError_t pick_grad(PositionArgs &a, int heads, int sms, cudaStream_t s)
+template <typename T, bool EVEN> cudaError_t pick_grad(PositionArgs &a, int heads, int sms, cudaStream_t s)
 {
     const long long n = held<T>(a);
-    if (n <= 8 * 8) return run_grad<T, 8, 8, false>(a, heads, sms, s);
-    if (n <= 8 * 16) return run_grad<T, 8, 16, false>(a, heads, sms, s);
-    if (n <= 32 * 8) return run_grad<T, 32, 8, false>(a, heads, sms, s);
-    if (n <= 32 * 16) return run_grad<T, 32, 16, false>(a, heads, sms, s);
-    if (n <= 32 * 32) return run_grad<T, 32, 32, false>(a, heads, sms, s);
-    if (n <= 256 * 8) return run_grad<T, 256, 8, false>(a, heads, sms, s);
-    if (n <= 256 * 16) return run_grad<T, 256, 16, false>(a, heads, sms, s);
-    if (n <= 256 * 32) return run_grad<T, 256, 32, false>(a, heads, sms, s);
-    return run_grad<T, 256, 8, true>(a, heads, sms, s);
+    if (n <= 8 * 8) return run_grad<T, 8, 8, false, EVEN>(a, heads, sms, s);
+    if (n <= 8 * 16) return run_grad<T, 8, 16, false, EVEN>(a, heads, sms, s);
+    if (n <= 32 * 8) return run_grad<T, 32, 8, false, EVEN>(a, heads, sms, s);
+    if (n <= 32 * 16) return run_grad<T, 32, 16, false, EVEN>(a, heads, sms, s);
+    if (n <= 32 * 24) return run_grad<T, 32, 24, false, EVEN>(a, heads, sms, s);
+    if (n <= 32 * 32) return run_grad<T, 32, 32, false, EVEN>(a, heads, sms, s);
+    if (n <= 64 * 32) return run_grad<T, 64, 32, false, EVEN>(a, heads, sms, s);
+    if (n <= 128 * 32) return run_grad<T, 128, 32, false, EVEN>(a, heads, sms, s);
+    if (n <= 256 * 32) return run_grad<T, 256, 32, false, EVEN>(a, heads, sms, s);
+    return run_grad<T, 256, 8, true, EVEN>(a, heads, sms, s);
 }
 
 template <typename A> void fill_common(PositionArgs &p, const A &a)
@@ -596,8 +977,8 @@ extern "C" adascale_status adascale_position_softmax(const adascale_position_sof
     p.s_at = {a.scores_stride_b, a.scores_stride_h, a.scores_stride_q};
     p.out_at = {a.probs_stride_b, a.probs_stride_h, a.probs_stride_q};
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    if (a.dtype == ADASCALE_BF16) OPS_CU(pick_softmax<bf16>(p, (int)a.heads, sms, s));
-    else OPS_CU(pick_softmax<float>(p, (int)a.heads, sms, s));
+    if (a.dtype == ADASCALE_BF16) OPS_CU(all_even<bf16>(p) ? pick_softmax<bf16, true>(p, (int)a.heads, sms, s) : pick_softmax<bf16, false>(p, (int)a.heads, sms, s));
+    else OPS_CU(all_even<float>(p) ? pick_softmax<float, true>(p, (int)a.heads, sms, s) : pick_softmax<float, false>(p, (int)a.heads, sms, s));
     return ADASCALE_OK;
 }
 
@@ -645,8 +1026,8 @@ extern "C" adascale_status adascale_position_softmax_grad(const adascale_positio
     p.out_at = {a.dscores_stride_b, a.dscores_stride_h, a.dscores_stride_q};
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     if (!nothing) {
-        if (a.dtype == ADASCALE_BF16) OPS_CU(pick_grad<bf16>(p, (int)a.heads, sms, s));
-        else OPS_CU(pick_grad<float>(p, (int)a.heads, sms, s));
+        if (a.dtype == ADASCALE_BF16) OPS_CU(all_even<bf16>(p) ? pick_grad<bf16, true>(p, (int)a.heads, sms, s) : pick_grad<bf16, false>(p, (int)a.heads, sms, s));
+        else OPS_CU(all_even<float>(p) ? pick_grad<float, true>(p, (int)a.heads, sms, s) : pick_grad<float, false>(p, (int)a.heads, sms, s));
     }
     if (!a.dtable) return ADASCALE_OK;
     JoinArgs j = {p.partials, a.dtable, a.ld_dtable, (int)a.heads, a.n_buckets, nothing ? 0 : p.chunks, a.accumulate != 0};
