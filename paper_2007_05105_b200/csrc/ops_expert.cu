@@ -16,7 +16,7 @@
 // 64 of them bring of the next expert is set to zero in shared memory.
 //
 // A block a SM, or a pair of them, walks over the tiles: one warp issues the copies (tensor maps, 128-byte swizzle) into a ring of
-// stages of 64 summands, one the matrix instructions, four bring finished tiles from tensor memory, where two take turns,
+// stages of 64 summands, one the matrix instructions, eight bring finished tiles from tensor memory, where two take turns,
 // through shared memory to whole lines of memory.  In a pair both have 128 lanes and half of the columns' operand each, and the
 // first one's instructions work on both: 256 x 256 results for 32 KB a stage and SM where a block alone takes 48 KB for half as
 // many, and 48 KB are what the L2 cache does not deliver in the time that they are worked on.
@@ -37,7 +37,8 @@ constexpr int kMaxExperts = ADASCALE_EXPERT_MAX_EXPERTS;
 constexpr int kLanes = 128;      // of a block
 constexpr int kK = 64;           // summands of a stage: 128 bytes, the swizzle's width
 constexpr int kPart = 12 * kK;   // summands of one sum in tensor memory, for float32 results
-constexpr int kThreads = 256;    // warps: copies, matrix instructions, ends of groups, one idle, four for results
+constexpr int kResultWarps = 8;
+constexpr int kThreads = 128 + 32 * kResultWarps;  // warps: copies, matrix instructions, ends of groups, one idle; results
 constexpr int kDynamicMax = 216 * 1024;
 
 enum Form { Y, DX, DW };
@@ -52,6 +53,10 @@ struct ExpertArgs {
     int lanes, columns, summed;    // extents; the one that is e's rows is 0
     int accumulate, out_aligned;
     int in_parts;                  // sums are cut at kPart
+    // Two kernels of one call that do not need each other: the first (leads) lets the second (follows) start as soon as all of its blocks
+    // have passed their wait for what was before it - which is then done for the second too - so that the second's blocks take the SMs
+    // that the first one's leave.  The second waits for the first before it ends, so that who waits for it has waited for both.
+    int leads, follows;
 };
 
 // ---- tensor memory and matrix instructions: of a block, or of a pair -----------------------
@@ -102,10 +107,9 @@ __device__ __forceinline__ bool elected()
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
     return is;
 }
-// 32 columns of this warp's 32 lanes
-__device__ __forceinline__ void tmem_load(unsigned at, float (&x)[32])
+// 32 columns of this warp's 32 lanes; they are there after tmem_loaded, which all uses of x come behind.
+__device__ __forceinline__ void tmem_load(unsigned at, unsigned (&r)[32])
 {
-    unsigned r[32];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
                  "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
@@ -114,10 +118,14 @@ __device__ __forceinline__ void tmem_load(unsigned at, float (&x)[32])
                    "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
                    "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
                  : "r"(at));
+}
+__device__ __forceinline__ void tmem_loaded(unsigned (&r)[32])
+{
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));  // not read before
 }
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_store(unsigned at, const float (&x)[32])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
@@ -128,8 +136,8 @@ __device__ __forceinline__ void tmem_store(unsigned at, const float (&x)[32])
                  "f"(x[21]), "f"(x[22]), "f"(x[23]), "f"(x[24]), "f"(x[25]), "f"(x[26]), "f"(x[27]), "f"(x[28]), "f"(x[29]), "f"(x[30]),
                  "f"(x[31])
                  : "memory");
-    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // A copy by a tensor map into this block's shared memory; the innermost coordinate is a multiple of 8 elements (16 bytes).  In a pair
 // the barrier may be the other block's.
 template <bool PAIR> __device__ __forceinline__ void tensor_load(void *dst, const CUtensorMap *map, int x, int y, int z, unsigned bar)
@@ -274,14 +282,19 @@ template <bool CLUSTER = false> __device__ __forceinline__ void wait_for(u64 *ba
 }
 
 // ---- results -------------------------------------------------------------------------------
-// A warp stores its 32 lanes by itself, 32 columns a time, by way of its two rooms of 32 x 32 results in shared memory and a copy
-// by tensor map, which leaves out what lies outside the matrix.
+// Two warps share 32 lanes and take every other 32 columns of them, each by way of its room of 32 x 32 results in shared memory and a
+// copy by tensor map, which leaves out what lies outside the matrix.
 
-// What was put into shared memory by all lanes goes out: lane 0 has the copies, at most one of them while the other room is filled.
+// Until the last copy out of the warp's room has read it; lane 0 has the copies.
+__device__ __forceinline__ void room_wait()
+{
+    if (threadIdx.x % 32 == 0) bulk_wait_read<0>();
+    __syncwarp();
+}
+// What was put into it by all lanes goes out.
 template <typename Issue> __device__ __forceinline__ void copy_out(Issue issue)
 {
     copy_fence();
-    if (threadIdx.x % 32 == 0) bulk_wait_read<0>();  // of the other room: who has passed the next line may fill it
     __syncwarp();
     if (threadIdx.x % 32 == 0) {
         issue();
@@ -314,13 +327,14 @@ template <typename O> __device__ __forceinline__ void store_tokens(const ExpertA
                 if (i < n) put(out + i * a.ld_out + me, v[i]);
         return;
     }
+    room_wait();
 #pragma unroll
     for (int i = 0; i < 32; ++i) put(room + i * 32 + me, v[i]);
     if (n == 32) {
         copy_out([&] { tensor_store(&a.c, lane0, token, 0, room); });
         return;
     }
-    copy_out([] {});  // the last tokens of a group: what follows them is not ours
+    __syncwarp();  // the last tokens of a group: what follows them is not ours
     const int piece = me % kPieces, left = a.lanes - lane0 - piece * V;
     for (int k = me / kPieces; k < n; k += kAtOnce) {
         const O *q = room + k * 32 + piece * V;
@@ -363,6 +377,7 @@ template <typename O> __device__ __forceinline__ void store_rows(const ExpertArg
                 if (i < n) put(p + i, v[i]);
         return;
     }
+    room_wait();
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
         float x[V];
@@ -379,7 +394,7 @@ template <typename O> __device__ __forceinline__ void store_rows(const ExpertArg
 // ---- the kernel ----------------------------------------------------------------------------
 
 template <int NT, bool PAIR> constexpr int kStageBytes = (kLanes + (PAIR ? NT / 2 : NT)) * kK * 2;
-template <typename O> constexpr int kStaging = 2 * 32 * kLanes * (int)sizeof(O);
+template <typename O> constexpr int kStaging = kResultWarps * 32 * 32 * (int)sizeof(O);
 template <int NT, bool PAIR, typename O> constexpr int kStages = (kDynamicMax - kStaging<O>) / kStageBytes<NT, PAIR>;
 // staging and ring, which start on a boundary of 1024
 template <int NT, bool PAIR, typename O> constexpr int kSmemBytes = 1024 + kStaging<O> + kStages<NT, PAIR, O> * kStageBytes<NT, PAIR>;
@@ -411,12 +426,18 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
         mbar_init(&ended, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&done[i], 1);
-            mbar_init(&taken[i], PAIR ? 8 : 4);
+            mbar_init(&taken[i], PAIR ? 2 * kResultWarps : kResultWarps);
         }
         mbar_publish();
     }
     if (warp == 1) tmem_alloc<PAIR>(&tmem_base, kColumns);
-    griddep_wait();
+    if (warp == 3 && elected()) {
+        prefetch_map(&a.a);
+        prefetch_map(&a.b);
+        prefetch_map(&a.c);
+    }
+    if (!a.follows) griddep_wait();
+    if (a.leads) griddep_launch();
     if (warp == 0) find_tiles<F, NT, LANES>(a, x);
     tmem_fence_before();
     __syncthreads();
@@ -544,11 +565,11 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
             }
         }
     } else if (warp >= 4) {
-        const int quarter = warp - 4;  // a warp reads the quarter of the lanes that its number names
-        O *room = reinterpret_cast<O *>(staging) + quarter * 2 * 32 * 32;
+        const int quarter = warp % 4;  // a warp reads the quarter of the lanes that its number names
+        O *room = reinterpret_cast<O *>(staging) + (warp - 4) * 32 * 32;
         const unsigned mine = (unsigned)(quarter * 32) << 16;
         Tile t = {};
-        int turn = 0, chunks = 0;
+        int turn = 0;
         unsigned phase = 0;
         for (int tile = first_tile; tile < n_tiles; tile += step) {
             find_tile<F, NT, LANES>(a, x, tile, rank, t);
@@ -560,29 +581,33 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                     tmem_fence_after();
                 }
                 const bool lost = __any_sync(0xffffffffu, gave_up);
-                for (int c = 0; c < t.width; c += 32) {
+                for (int c = (warp - 4) / 4 * 32; c < t.width; c += kResultWarps / 4 * 32) {
                     float v[32];
                     if (any && !lost) {
-                        tmem_load(tmem + turn * NT + mine + c, v);
+                        unsigned now[32], before[32];
+                        tmem_load(tmem + turn * NT + mine + c, now);
+                        if (begin > 0) tmem_load(tmem + NT + mine + c, before);
+                        tmem_loaded(now);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(now[i]);
+                        if (begin > 0) {
+                            tmem_loaded(before);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(before[i]);
+                        }
                     } else {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = any ? NAN : 0.f;
-                    }
-                    if (begin > 0) {
-                        float sum[32];
-                        tmem_load(tmem + NT + mine + c, sum);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] += sum[i];
                     }
                     if (!last) {
                         tmem_store(tmem + NT + mine + c, v);
                         continue;
                     }
                     const int n = min(32, t.width - c);
-                    O *mine_now = room + chunks++ % 2 * 32 * 32;
-                    if constexpr (F == DW) store_rows<O>(a, v, mine_now, t.expert, t.lane + quarter * 32, t.column + c, n);
-                    else store_tokens<O>(a, v, mine_now, t.lane + quarter * 32, t.column + c, n);
+                    if constexpr (F == DW) store_rows<O>(a, v, room, t.expert, t.lane + quarter * 32, t.column + c, n);
+                    else store_tokens<O>(a, v, room, t.lane + quarter * 32, t.column + c, n);
                 }
+                if (!last) tmem_stored();
                 if (!any) continue;
                 tmem_fence_before();
                 __syncwarp();
@@ -605,6 +630,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
     if constexpr (PAIR) pair_sync();  // neither ends while the other may arrive at its barriers
     tmem_fence_after();
     if (warp == 1) tmem_free<PAIR>(tmem, kColumns);
+    if (a.follows) griddep_wait();
 }
 
 // ---- host side -----------------------------------------------------------------------------
@@ -743,6 +769,7 @@ extern "C" adascale_status adascale_expert_matmul(const adascale_expert_matmul_a
     e.ld_out = a.ld_y;
     e.lanes = (int)a.out_dim;
     e.summed = (int)a.in_dim;
+    e.leads = 1;  // this is no gradient: whatever comes next may start
     const int n = token_tile(a.n_rows, a.n_experts);
     if (!operand_map(&e.a, a.w, {a.n_experts, a.out_dim, a.in_dim, a.stride_w, a.ld_w}, kLanes) ||
         !operand_map(&e.b, a.x, {1, a.n_rows, a.in_dim, 0, a.ld_x}, std::min(n, 64)) ||
@@ -776,6 +803,7 @@ extern "C" adascale_status adascale_expert_matmul_grad(const adascale_expert_mat
         e.ld_out = a.ld_dx;
         e.lanes = (int)a.in_dim;
         e.summed = (int)a.out_dim;
+        e.leads = want_dw;
         const int n = token_tile(a.n_rows, a.n_experts);
         if (!operand_map(&e.a, a.w, {a.n_experts, a.out_dim, a.in_dim, a.stride_w, a.ld_w}, kK) ||
             !operand_map(&e.b, a.dy, {1, a.n_rows, a.out_dim, 0, a.ld_dy}, std::min(n, 64)) ||
@@ -791,6 +819,7 @@ extern "C" adascale_status adascale_expert_matmul_grad(const adascale_expert_mat
         e.lanes = (int)a.out_dim;
         e.columns = (int)a.in_dim;
         e.accumulate = a.accumulate != 0;
+        e.follows = want_dx;
         // without rows no operand is copied
         if ((rows && (!operand_map(&e.a, a.dy, {1, a.n_rows, a.out_dim, 0, a.ld_dy}, kK) || !operand_map(&e.b, a.x, {1, a.n_rows, a.in_dim, 0, a.ld_x}, kK))) ||
             !result_map(e, {a.n_experts, a.out_dim, a.in_dim, a.stride_dw, a.ld_dw}, a.dw_dtype,
