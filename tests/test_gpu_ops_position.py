@@ -342,3 +342,33 @@ def test_refusals():
                 lambda: ops.position_softmax_grad(s, s, 32, workspace=torch.zeros(16, dtype=torch.uint8, device=DEV))]:
         with pytest.raises(AdaScaleError):
             bad()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape,distance", [((1, 2, 40, 1500), 1000), ((2, 1, 30, 5000), 3000), ((1, 1, 3, 20000), 16384), ((1, 2, 30, 700), 1025)])
+def test_far_distances(shape, distance, dtype):
+    """Maximum distances on either side of what is kept by distance, with buckets that change within a thread's keys."""
+    for mode in [(True, False, False, True), (False, True, True, True)]:
+        case, tensor, table = make(shape, dtype, distance, *mode, buckets=128, distance=distance)
+        scores, dprobs = tensor(8.0), tensor(1.0)
+        probs = ops.position_softmax(scores, table, **how(case))
+        check_forward(probs, scores, table, case, "weights")
+        got = ops.position_softmax_grad(probs, dprobs, 128, **how(case))
+        check_gradient(got, probs, dprobs, case, None, "gradient")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_of_every_length(dtype):
+    """One and the same row cut at every length, so that each part of an access is once the last live one; whole rows, and lengths."""
+    g = gen(12)
+    scores, dprobs, table = normal(g, 1, 2, 3, 140, dtype=dtype, std=8.0), normal(g, 1, 2, 3, 140, dtype=dtype), normal(g, 16, 2)
+    for n in list(range(1, 40)) + [63, 64, 65, 71, 100, 127, 128, 129, 139, 140]:
+        case = dict(buckets=16, distance=50, both=True, causal=False, scale=0.125, lengths=None, starts=torch.tensor([60], device=DEV))
+        s, d = scores[..., :n].contiguous(), dprobs[..., :n].contiguous()
+        probs = ops.position_softmax(s, table, **how(case))
+        check_forward(probs, s, table, case, "cut at %d" % n)
+        check_gradient(ops.position_softmax_grad(probs, d, 16, **how(case)), probs, d, case, None, "cut at %d" % n)
+        case["lengths"] = torch.tensor([n], device=DEV)
+        whole = ops.position_softmax(scores, table, **how(case))
+        check_forward(whole, scores, table, case, "length %d" % n)
+        check_gradient(ops.position_softmax_grad(whole, dprobs, 16, **how(case)), whole, dprobs, case, None, "length %d" % n)
