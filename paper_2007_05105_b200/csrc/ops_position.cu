@@ -513,9 +513,10 @@ __global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<GS, E>) k_
 // ---- gradient ------------------------------------------------------------------------------
 
 // Near the diagonal adjacent keys are in different buckets: those are summed by distance, in registers.  A warp puts its values at the
-// keys from 64 before the query to 72 behind it, in whole accesses, into shared memory, and lane l takes the distances
-// l - 72, l - 40, ... from there.  (One by one into the sums by bucket: 9 instructions a key, 100 of 640 a row of 1024.)
-constexpr int kNear = 64, kNearKeys = 2 * kNear + 16, kNearTakes = 5;
+// keys from 128 before the query to 136 behind it, in whole accesses, into shared memory, and lane l takes the distances
+// l - 136, l - 104, ... from there.  (One by one into the sums by bucket: 9 instructions a key, for 8 keys wherever one lane's keys are
+// in different buckets.)
+constexpr int kNear = 128, kNearKeys = 2 * kNear + 16, kNearTakes = 9;
 struct Near {
     float *room;  // [kNearKeys] of this warp
     float sum[kNearTakes];
@@ -555,8 +556,9 @@ __device__ __forceinline__ void add_buckets(const unsigned char *bucket, int m, 
     }
 }
 
-// Two raw rows a thread: E elements of 2 or 4 bytes each.
-template <typename T, int E> constexpr int kGradBlocks = E * (int)sizeof(T) > 64 ? 2 : E * (int)sizeof(T) == 64 ? 3 : 4;
+// Blocks of an SM, as registers for two rows of E elements a thread allow without spilling (bf16, 1024 keys: 118 us with two blocks or
+// three, 127 with three and 80 bytes spilled).
+template <typename T, int E> constexpr int kGradBlocks = sizeof(T) == 2 ? (E <= 8 ? 4 : E <= 24 ? 3 : 2) : (E <= 8 ? 4 : E <= 16 ? 3 : 2);
 
 template <typename T, int GS, int E, bool LONG, bool EVEN>
 __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const __grid_constant__ PositionArgs a)
@@ -698,6 +700,9 @@ __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const _
                         d[i] = mul2(g[i], scale);
                     }
                     if (a.out) store_cols<EVEN, T, P>(ds, at(v), n, true, d);
+                } else if (v * GS * V - off >= w.live) {
+                    const f2 zero[P] = {};
+                    if (a.out && at(v) - off < n) store_cols<EVEN, T, P>(ds, at(v) - off, n, out_aligned, zero);
                 } else if (at(v) - off < n) {
                     finish(x[v], y[v], at(v) - off, dot);
                 }
@@ -719,7 +724,7 @@ __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const _
             __syncwarp();
 #pragma unroll
             for (int k = 0; k < kNearTakes; ++k) {
-                if (a.causal && k > 2) break;  // distances from 24 on
+                if (a.causal && k > 4) break;  // distances from 24 on
                 const int j = w.pos + Near::distance(k);
                 // live, and one of this warp's
                 if (j >= 0 && j < w.live && (GS == 32 || (unsigned)(j + off) / (32 * V) % kWarps == threadIdx.x % GS / 32) &&
