@@ -703,10 +703,14 @@ template <Form F, int NT, bool PAIR = false> cudaError_t run_type(ExpertArgs &a,
                                     : lane_tiles * (a.n_rows / NT + std::min<long long>(a.n_experts, a.n_rows));
     return dtype == ADASCALE_BF16 ? run_tiles<F, NT, PAIR, bf16>(a, tiles, s) : run_tiles<F, NT, PAIR, float>(a, tiles, s);
 }
-// Pairs of blocks where there are lanes for both.
+// Pairs of blocks where there are lanes for both and the summands (of an expert on average) are many: with few of them the time goes into
+// bringing results out, and half as many, twice as large tiles leave more SMs without one.  Pair against blocks alone, us:
+// 1024 x 4096 over 8 experts, weights' gradient of 256 rows each 33.4 and 28.2, of 512 rows 41.8 and 42.8, product of 256 rows
+// each (1024 summands) 26.4 and 29.1; 512 x 512 over 64 experts, 256 rows each (512 summands) 24.5 and 21.8.
 template <Form F> cudaError_t run_wide(ExpertArgs &a, int dtype, cudaStream_t s)
 {
-    return a.lanes > kLanes ? run_type<F, 256, true>(a, dtype, s) : run_type<F, 256>(a, dtype, s);
+    const long long summands = F == DW ? a.n_rows / a.n_experts : a.summed;
+    return a.lanes > kLanes && summands > 512 ? run_type<F, 256, true>(a, dtype, s) : run_type<F, 256>(a, dtype, s);
 }
 // Tiles of tokens are as wide as the rows of an expert on average, as far as the host knows.
 template <Form F> cudaError_t run_tokens(ExpertArgs &a, int dtype, cudaStream_t s, int n)

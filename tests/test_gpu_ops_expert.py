@@ -265,3 +265,45 @@ def test_refusals():
             bad()
     with pytest.raises(AdaScaleError):
         ops.expert_matmul(x, w[:1].expand(1025, 24, 16), offsets_of([0] * 1025))
+
+
+@pytest.mark.parametrize("out_t", [BF16, F32])
+@pytest.mark.parametrize("rows", [1, 15, 17, 31, 32, 33, 63, 64, 65, 100, 160, 255, 256, 257, 300, 449])
+def test_every_width_of_a_tile_of_two_blocks(rows, out_t):
+    """Enough summands for pairs of blocks, beside a large expert; NaN before the first row and behind the last."""
+    k, m, counts = 576, 530, [rows, 1100]
+    g = gen(rows)
+    n = sum(counts) + 9
+    x, w, dy = normal(g, n, k, dtype=BF16), normal(g, 2, m, k, dtype=BF16), aligned(normal(g, n, m, dtype=BF16))
+    for t in (x, dy):
+        t[:4], t[-5:] = float("nan"), float("nan")
+    offsets = offsets_of(counts, 4)
+    before = torch.full((n, m), 7.0, device=DEV, dtype=out_t)
+    y = ops.expert_matmul(x, w, offsets, out=before.clone())
+    forward_check(x, w, offsets, y, before, "product")
+    before = torch.full((n, k), 7.0, device=DEV, dtype=out_t)
+    dw0 = normal(g, 2, m, k, dtype=out_t)
+    got = ops.expert_matmul_grad(dy, offsets, x=x, w=w, dx=before.clone(), dw=dw0.clone(), accumulate=True)
+    want, mag = before.double(), torch.zeros(n, k, dtype=torch.float64, device=DEV)
+    for e, lo, hi in groups(offsets):
+        want[lo:hi], mag[lo:hi] = dy[lo:hi].double() @ w[e].double(), dy[lo:hi].double().abs() @ w[e].double().abs()
+        whole = dw0[e].double() + dy[lo:hi].double().t() @ x[lo:hi].double()
+        terms = dy[lo:hi].double().abs().t() @ x[lo:hi].double().abs()
+        check(got.dw[e], whole, 2 * (hi - lo) * U * terms + U * whole.abs() + rounding(out_t) * whole.abs() * 1.01, "dw")
+    check(got.dx, want, 2 * m * U * mag + rounding(out_t) * want.abs() * 1.01, "dx")
+
+
+def test_long_sums_in_32_bits():
+    """Sums of 20000 terms of one sign, which instructions that cut lose 2e-5 of: a float32 result is formed in parts of 768 terms, each cut 48
+    times (16 terms an instruction) by less than 2^-23 of what it holds, and 27 rounded additions of parts by 2^-24 each."""
+    g = gen(9)
+    n = 20000
+    x, dy = normal(g, n, 64, dtype=BF16).abs(), normal(g, n, 320, dtype=BF16).abs()
+    got = ops.expert_matmul_grad(dy, offsets_of([n]), x=x)
+    want = dy.double().t() @ x.double()
+    check(got.dw[0], want, (48 * 2.0 ** -23 + 27 * U) * want, "dw")
+    w = normal(g, 1, 200, 12000, dtype=BF16).abs()
+    x = normal(g, 300, 12000, dtype=BF16).abs()
+    y = ops.expert_matmul(x, w, offsets_of([300]), out_dtype=F32)
+    want = x.double() @ w[0].double().t()
+    check(y, want, (48 * 2.0 ** -23 + 16 * U) * want, "y")
