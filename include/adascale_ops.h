@@ -331,7 +331,8 @@ adascale_status adascale_expert_matmul_grad(const adascale_expert_matmul_grad_ar
  *   norm = sqrt(sum over all tensors and elements of g^2)
  *   out  = c g,   c = min(1, max_norm / (norm + eps))
  *
- * grads, out, numels, grad_dtypes and out_dtypes are HOST arrays of n_tensors entries, read during the call: device
+ * grads, out, numels, grad_dtypes and out_dtypes are HOST arrays of n_tensors entries, read during the call (which uses host memory
+ * of their size until it returns): device
  * addresses, element counts (0 is allowed, its addresses are not looked at) and adascale_dtype of each tensor, whose elements are
  * adjacent.  out = NULL: the norm alone.  out[k] may be grads[k] itself with the same type (if c = 1 nothing is written
  * then); otherwise it overlaps neither another output nor a gradient.  No output may be given twice.

@@ -189,6 +189,27 @@ __device__ __forceinline__ void arrive_at_first(u64 *bar)
 
 // ---- tiles ---------------------------------------------------------------------------------
 
+// What other kernels may have written is read past the L1 cache: the second gradient's kernel does not begin with a wait.
+__device__ __forceinline__ float load_new(const float *p) { return __ldcg(p); }
+__device__ __forceinline__ float load_new(const bf16 *p) { return __uint_as_float((unsigned)__ldcg(reinterpret_cast<const unsigned short *>(p)) << 16); }
+__device__ __forceinline__ void load_new(const float *p, float (&x)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float4 q = __ldcg(reinterpret_cast<const float4 *>(p) + i);
+        x[4 * i] = q.x, x[4 * i + 1] = q.y, x[4 * i + 2] = q.z, x[4 * i + 3] = q.w;
+    }
+}
+__device__ __forceinline__ void load_new(const bf16 *p, float (&x)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint4 q = __ldcg(reinterpret_cast<const uint4 *>(p) + i);
+        x[8 * i] = bf_lo(q.x), x[8 * i + 1] = bf_hi(q.x), x[8 * i + 2] = bf_lo(q.y), x[8 * i + 3] = bf_hi(q.y);
+        x[8 * i + 4] = bf_lo(q.z), x[8 * i + 5] = bf_hi(q.z), x[8 * i + 6] = bf_lo(q.w), x[8 * i + 7] = bf_hi(q.w);
+    }
+}
+
 // Of each expert: its rows, and the number of tiles before it.
 struct Experts {
     int *begin;  // [n + 1]: begin[e + 1] is where e ends
@@ -201,7 +222,8 @@ template <Form F, int NT, int LANES> __device__ __forceinline__ void find_tiles(
     const int lane = threadIdx.x % 32, lane_tiles = (a.lanes + LANES - 1) / LANES;
     int floor = 0;
     for (int i = lane; i - lane <= a.n_experts; i += 32) {
-        long long o = i <= a.n_experts ? load_id(a.offsets, a.wide_offsets, i) : 0;
+        long long o = 0;
+        if (i <= a.n_experts) o = a.wide_offsets ? __ldcg(static_cast<const long long *>(a.offsets) + i) : (long long)__ldcg(static_cast<const int *>(a.offsets) + i);
         int v = (int)(o < 0 ? 0 : o > a.n_rows ? a.n_rows : o);
         v = v > floor ? v : floor;
 #pragma unroll
@@ -361,13 +383,13 @@ template <typename O> __device__ __forceinline__ void store_rows(const ExpertArg
     if (add_here && lane0 + me < a.lanes) {
         if (a.out_aligned && n == 32) {
             float old[32];
-            load_vec<32>(p, old);
+            load_new(p, old);
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += old[i];
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-                if (i < n) v[i] += to_f32(p[i]);
+                if (i < n) v[i] += load_new(p + i);
         }
     }
     if (!a.out_aligned) {

@@ -307,3 +307,71 @@ def test_long_sums_in_32_bits():
     y = ops.expert_matmul(x, w, offsets_of([300]), out_dtype=F32)
     want = x.double() @ w[0].double().t()
     check(y, want, (48 * 2.0 ** -23 + 16 * U) * want, "y")
+
+
+def test_many_experts():
+    """As many as there may be, most of them with a few rows or none; weights' gradients whole, zeros among them."""
+    g = gen(21)
+    counts = torch.randint(0, 5, (1024,), generator=torch.Generator().manual_seed(4)).tolist()
+    counts[17], counts[500:520] = 300, [0] * 20
+    n, k, m = sum(counts), 72, 40
+    x, w, dy = normal(g, n, k, dtype=BF16), normal(g, 1024, m, k, dtype=BF16), normal(g, n, m, dtype=BF16)
+    offsets = offsets_of(counts)
+    owner = torch.repeat_interleave(torch.arange(1024, device=DEV), torch.tensor(counts, device=DEV))
+    own = w[owner].double()
+    y = ops.expert_matmul(x, w, offsets, out_dtype=F32)
+    want = torch.einsum("rmk,rk->rm", own, x.double())
+    check(y, want, 2 * k * U * torch.einsum("rmk,rk->rm", own.abs(), x.double().abs()) + U * want.abs(), "y")
+    got = ops.expert_matmul_grad(dy, offsets, x=x, w=w, dx_dtype=F32)
+    want = torch.einsum("rmk,rm->rk", own, dy.double())
+    check(got.dx, want, 2 * m * U * torch.einsum("rmk,rm->rk", own.abs(), dy.double().abs()) + U * want.abs(), "dx")
+    outer = dy.double()[:, :, None] * x.double()[:, None, :]
+    want = torch.zeros(1024, m, k, dtype=torch.float64, device=DEV).index_add_(0, owner, outer)
+    mag = torch.zeros_like(want).index_add_(0, owner, outer.abs())
+    check(got.dw, want, 2 * 300 * U * mag + U * want.abs(), "dw")
+
+
+@pytest.mark.parametrize("k,m", [(1, 1), (1, 9), (9, 1), (3, 130), (129, 2)])
+def test_narrow_widths(k, m):
+    g = gen(k + m)
+    counts = [5, 0, 140, 1]
+    n = sum(counts)
+    x, w, dy = padded(normal(g, n, k, dtype=BF16), 1), padded(normal(g, 4, m, k, dtype=BF16), 1), padded(normal(g, n, m, dtype=BF16), 1)
+    offsets = offsets_of(counts)
+    for t in (BF16, F32):
+        y = ops.expert_matmul(x, w, offsets, out_dtype=t)
+        forward_check(x, w, offsets, y, torch.zeros_like(y), "narrow")
+        got = ops.expert_matmul_grad(dy, offsets, x=x, w=w, dx_dtype=t, wgrad_dtype=t)
+        for e, lo, hi in groups(offsets):
+            want = dy[lo:hi].double() @ w[e].double()
+            check(got.dx[lo:hi], want, 2 * m * U * (dy[lo:hi].double().abs() @ w[e].double().abs()) + rounding(t) * want.abs() * 1.01, "dx")
+            want = dy[lo:hi].double().t() @ x[lo:hi].double()
+            check(got.dw[e], want, 2 * 140 * U * (dy[lo:hi].double().abs().t() @ x[lo:hi].double().abs()) + rounding(t) * want.abs() * 1.01, "dw")
+
+
+def test_gradients_one_behind_the_other():
+    """Microbatches added into one gradient, each call's rows made by the kernel before it and its results read by the one behind it."""
+    g = gen(31)
+    x, w, dy = normal(g, 900, 640, dtype=BF16), normal(g, 3, 600, 640, dtype=BF16), normal(g, 900, 600, dtype=BF16)
+    cuts = [offsets_of([300, 300, 300]), offsets_of([0, 899, 1]), offsets_of([13, 600, 200])]
+    offsets = torch.zeros(4, dtype=torch.int32, device=DEV)
+    for t in (F32, BF16):
+        dw, alone = torch.zeros(3, 600, 640, dtype=t, device=DEV), torch.zeros(3, 600, 640, dtype=t, device=DEV)
+        dx = torch.zeros(900, 640, dtype=BF16, device=DEV)
+        seen, want = [], []
+        for k in range(9):
+            offsets.copy_(cuts[k % 3])
+            ops.expert_matmul_grad(dy, offsets, x=x, w=w, dx=dx, dw=dw, accumulate=True)
+            seen.append((dx.clone(), dw.clone()))
+        for k in range(9):
+            torch.cuda.synchronize()
+            ops.expert_matmul_grad(dy, cuts[k % 3], w=w, dx=dx)
+            torch.cuda.synchronize()
+            ops.expert_matmul_grad(dy, cuts[k % 3], x=x, dw=alone, accumulate=True)
+            torch.cuda.synchronize()
+            want.append((None, alone.clone()))
+        assert all(torch.equal(a[1], b[1]) for a, b in zip(seen, want))
+        for k in range(9):
+            o = cuts[k % 3].tolist()
+            alone_dx = ops.expert_matmul_grad(dy, cuts[k % 3], w=w).dx
+            assert torch.equal(seen[k][0][o[0]:o[3]], alone_dx[o[0]:o[3]])

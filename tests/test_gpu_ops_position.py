@@ -372,3 +372,23 @@ def test_rows_of_every_length(dtype):
         whole = ops.position_softmax(scores, table, **how(case))
         check_forward(whole, scores, table, case, "length %d" % n)
         check_gradient(ops.position_softmax_grad(whole, dprobs, 16, **how(case)), whole, dprobs, case, None, "length %d" % n)
+
+
+def test_many_batches_and_heads():
+    for shape in [(70000, 2, 1, 3), (2, 5000, 2, 9), (1, 1, 70000, 5)]:
+        case, tensor, table = make(shape, BF16, 3, True, False, False, False, buckets=8, distance=6)
+        scores, dprobs = tensor(8.0), tensor(1.0)
+        probs = ops.position_softmax(scores, table, **how(case))
+        z = scores.double() * case["scale"] + table.double().t()[None, :, buckets_of(case, 0, *shape[2:])].view(1, shape[1], *shape[2:])
+        want = torch.softmax(z, dim=-1)
+        size = z.abs().amax(dim=-1, keepdim=True)
+        check(probs, want, want * (U * (16 * size + 90) + 2.0 ** -8 * 1.01) + TINY, "weights")
+        got = ops.position_softmax_grad(probs, dprobs, 8, **how(case))
+        p, dp = probs.double(), dprobs.double()
+        g = p * (dp - (p * dp).sum(-1, keepdim=True))
+        off = p * U * ((dp - (p * dp).sum(-1, keepdim=True)).abs() + 80 * (p * dp).abs().sum(-1, keepdim=True)) + U * g.abs()
+        check(got.dscores, 0.125 * g, 0.125 * off + (U + 2.0 ** -8 * 1.01) * 0.125 * g.abs() + TINY, "dscores")
+        at = buckets_of(case, 0, *shape[2:]).reshape(-1)
+        flat = lambda t: torch.zeros(8, shape[1], dtype=torch.float64, device=DEV).index_add_(0, at, t.sum(0).reshape(shape[1], -1).t())  # noqa: E731
+        terms = shape[0] * shape[2] * 32
+        check(got.dtable, flat(g), flat(off) + (terms + 45) * U * flat(g.abs()) + 2 * U * flat(g).abs(), "dtable")
