@@ -4,7 +4,9 @@
 //
 // Two kernels: k_squares leaves one 64-bit sum a block, k_scale adds those up - every block all of them, in the same order, so
 // that no block waits for another - and writes c g.  Bound by memory: the gradients are read twice, because c is not known
-// before the last one was read; what the L2 cache still holds of them (126 MB) comes from there, since k_scale walks backwards.
+// before the last one was read; what the L2 cache still holds of them comes from there, since k_scale walks backwards (lists of 32 MB: all
+// at twice the copy rate; of 96 MB and more hardly any).  Measured on a B200: 61M float32 elements, norm 40.7 us (6.0 TB/s), clipped into a
+// bf16 row 98 us, 354M bf16 elements 353 us: 6.2 and 6.0 TB/s of three passes.
 // The tensors' addresses travel as a kernel argument (29 bytes each, 1024 a launch), so that nothing is copied to
 // the device or kept there and a captured call holds its own list.
 #include "ops_common.cuh"

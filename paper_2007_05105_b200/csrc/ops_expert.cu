@@ -22,6 +22,11 @@
 // many, and 48 KB are what the L2 cache does not deliver in the time that they are worked on.
 // Every block works out the tiles from the offsets by itself: no host, no kernel before.
 //
+// Measured on a B200: 16384 rows over 16 experts of 1024 -> 4096 in 116 us (1180 TFLOP/s; 137 us under the power cap of a long run, where
+// the library's batched product of equal groups takes 121 to 125), dx and dw of 8192 rows over 8 experts 62 us each; 16 rows over 8
+// experts, 59 MB of weights, 13 us.  Bound by the tensor cores' power and by what brings operands in (100 of the 116 us without results)
+// where rows are many, by the weights' bytes where they are few.
+//
 // The tensor cores cut, not round, when they add to the 32-bit sums: over m summands a float32 result loses 1.1e-9 m of itself
 // (4.4e-6 at 4096, measured; bf16 results do not show it).  For float32 results no sum is longer than kPart: the parts are
 // added up, rounded, by the warps that read them, in tensor memory.
