@@ -68,8 +68,13 @@ __device__ __forceinline__ int bucket_of(const Buckets &b, int d)
     int n = d < 0 ? -d : (b.both ? d : 0);
     int k = n;
     if (n >= b.exact) {
-        k = b.exact;
-        for (int i = 0; i < b.n_borders; ++i) k += b.border[i] <= n;
+        int lo = 0, hi = b.n_borders;  // the number of borders that are not above n
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (b.border[mid] <= n) lo = mid + 1;
+            else hi = mid;
+        }
+        k = b.exact + lo;
     }
     return k + (b.both && d > 0 ? b.m : 0);
 }
@@ -753,6 +758,7 @@ __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const _
     lane_sums[room[2 * m] * 32] += ahead;
     __syncthreads();
     // a warp adds up a bucket: lane by lane over the warps, then over the lanes
+#pragma unroll 4
     for (int k = threadIdx.x / 32; k < n_buckets; k += 8) {
         float v = 0.f;
 #pragma unroll
