@@ -23,7 +23,8 @@
 //
 // While a row is worked on, the group's next one is on its way into shared memory, each thread's part to a place of its own.
 //
-// Rows may start anywhere (then without that): accesses are cut at 16-byte boundaries of memory, the ragged ends of a row go element by element.
+// Rows may start anywhere (then without that): accesses are cut at 16-byte boundaries of memory; what one brings of the next row is not used,
+// and the ragged ends of a row are stored in pieces.  Short ones have kernels of their own.
 #include "ops_common.cuh"
 
 #include <algorithm>
@@ -55,6 +56,7 @@ struct PositionArgs {
     float *partials;
     const void *lengths, *starts;
     Strides s_at, dp_at, out_at;
+    long long s_span, dp_span;  // elements from the first one to behind the last
     long long rows;      // batch * n_queries
     long long ld_table;
     int n_queries, n_keys, chunks;
@@ -154,12 +156,23 @@ template <typename T, bool LONG, bool EVEN> constexpr bool kRowsAhead = sizeof(T
 // Elements by which an address lies behind a 16-byte boundary.
 template <typename T> __device__ __forceinline__ int off16(const T *p) { return (int)((uintptr_t)p % 16 / sizeof(T)); }
 
-// 16 bytes: elements c .. c + V - 1 of a row of n; those outside are 0.  EVEN: rows begin on and end at 16-byte boundaries, and all
-// matrices have the same strides.
-template <bool EVEN, typename T> __device__ __forceinline__ uint4 load_raw(const T *row, int c, int n, bool aligned)
+// How 16 bytes of a row are read that reach over its ends: whole where they are on a boundary and, `inside`, the matrix goes on around the
+// row (what they bring of it is not used; one by one, the ends' elements are a wait for memory of their own: bf16 rows of 500, gradient, 135 us, 105);
+// element by element where it does not.
+struct Reach {
+    bool aligned, inside;
+};
+template <typename T> __device__ __forceinline__ Reach reach_of(const T *row, int off, long long at, int n, long long span)
 {
     constexpr int V = 16 / sizeof(T);
-    if (EVEN || (aligned && c >= 0 && c + V <= n)) return *reinterpret_cast<const uint4 *>(row + c);
+    return {off16(row) == off, at >= V && at + n + V <= span};
+}
+// 16 bytes: elements c .. c + V - 1 of a row of n, of which one at least is the row's; what lies outside is 0 or anything.  EVEN: rows begin
+// on and end at 16-byte boundaries, and all matrices have the same strides.
+template <bool EVEN, typename T> __device__ __forceinline__ uint4 load_raw(const T *row, int c, int n, Reach reach)
+{
+    constexpr int V = 16 / sizeof(T);
+    if (EVEN || (reach.aligned && (reach.inside || (c >= 0 && c + V <= n)))) return *reinterpret_cast<const uint4 *>(row + c);
     union {
         uint4 raw;
         T x[V];
@@ -217,12 +230,42 @@ template <bool EVEN, int P> __device__ __forceinline__ void keep_live(f2 (&x)[P]
         x[i] = pack2(lo, hi);
     }
 }
+// Elements lo .. hi - 1 of 16 bytes on a boundary, where lo is 0 or hi is V.
+__device__ __forceinline__ void store_end(float *p, int lo, int hi, const float (&x)[4])
+{
+    if (lo == 0) {
+        if (hi & 2) *reinterpret_cast<float2 *>(p) = make_float2(x[0], x[1]);
+        if (hi & 1) p[hi - 1] = hi & 2 ? x[2] : x[0];
+    } else {
+        const int k = 4 - lo;
+        if (k & 2) *reinterpret_cast<float2 *>(p + 2) = make_float2(x[2], x[3]);
+        if (k & 1) p[lo] = k & 2 ? x[1] : x[3];
+    }
+}
+__device__ __forceinline__ void store_end(bf16 *p, int lo, int hi, const float (&x)[8])
+{
+    unsigned *q = reinterpret_cast<unsigned *>(p);
+    const unsigned a = bf_pack(x[0], x[1]), b = bf_pack(x[2], x[3]), c = bf_pack(x[4], x[5]), d = bf_pack(x[6], x[7]);
+    unsigned short *h = reinterpret_cast<unsigned short *>(p);
+    if (lo == 0) {
+        if (hi & 4) *reinterpret_cast<uint2 *>(q) = make_uint2(a, b);
+        if (hi & 2) q[hi & 4 ? 2 : 0] = hi & 4 ? c : a;
+        if (hi & 1) h[hi - 1] = (unsigned short)(hi & 4 ? (hi & 2 ? d : c) : (hi & 2 ? b : a));
+    } else {
+        const int k = 8 - lo;
+        if (k & 4) *reinterpret_cast<uint2 *>(q + 2) = make_uint2(c, d);
+        if (k & 2) q[k & 4 ? 1 : 3] = k & 4 ? b : d;
+        if (k & 1) h[lo] = (unsigned short)((k & 4 ? (k & 2 ? a : b) : (k & 2 ? c : d)) >> 16);
+    }
+}
 template <bool EVEN, typename T, int P> __device__ __forceinline__ void store_cols(T *row, int c, int n, bool aligned, const f2 (&x)[P])
 {
     float y[2 * P];
     flat(x, y);
     if (EVEN || (aligned && c >= 0 && c + 2 * P <= n)) {
         store_vec_streaming<2 * P>(row + c, y);
+    } else if (aligned && (c >= 0 || c + 2 * P <= n)) {  // one end: elements from `lo` on or up to `hi`, in pieces of powers of two
+        store_end(row + c, c < 0 ? -c : 0, c < 0 ? 2 * P : n - c, y);
     } else {
 #pragma unroll
         for (int e = 0; e < 2 * P; ++e)
@@ -389,7 +432,8 @@ template <int P> __device__ __forceinline__ float max_of(const f2 (&x)[P], float
 }
 
 // Logits of V adjacent keys; -inf where not live.
-template <bool EVEN, typename T, int P>
+// INNER: all of them are.
+template <bool EVEN, bool INNER, typename T, int P>
 __device__ __forceinline__ void logits(const Bias &t, const Row &w, const uint4 &raw, int c, float scale, f2 (&x)[P])
 {
     f2 bias[P];
@@ -397,15 +441,21 @@ __device__ __forceinline__ void logits(const Bias &t, const Row &w, const uint4 
     bias_of(t, c - w.pos, bias);
 #pragma unroll
     for (int i = 0; i < P; ++i) x[i] = fma2(pack2(scale, scale), x[i], bias[i]);
-    keep_live<EVEN>(x, c, w.live, -INFINITY);
+    if constexpr (!INNER) keep_live<EVEN>(x, c, w.live, -INFINITY);
 }
 
 // Blocks of an SM: registers for E elements a thread, without spilling, decide.
-template <int GS, int E> constexpr int kSoftmaxBlocks = GS > 256 ? 1 : E > 16 ? 3 : 4;
+template <typename T, int GS, int E, bool EVEN>
+constexpr int kSoftmaxBlocks = GS > 256                   ? 1
+                               : E <= 8                   ? 4
+                               : E <= 16                  ? (EVEN || sizeof(T) == 2 ? 4 : 3)
+                               : E <= 24                  ? (EVEN || sizeof(T) == 2 ? 3 : 2)
+                               : EVEN && sizeof(T) == 2   ? 3
+                                                          : 2;
 
 // GS threads a row, E elements a thread; LONG: rows of any length, read twice.
 template <typename T, int GS, int E, bool LONG, bool EVEN>
-__global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<GS, E>) k_softmax(const __grid_constant__ PositionArgs a)
+__global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<T, GS, E, EVEN>) k_softmax(const __grid_constant__ PositionArgs a)
 {
     constexpr int V = 16 / sizeof(T), P = V / 2, NV = E / V, kThreads = GS > 256 ? GS : 256, kGroups = kThreads / GS;
     extern __shared__ __align__(16) unsigned char room[];
@@ -438,6 +488,7 @@ __global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<GS, E>) k_
         T *p = static_cast<T *>(a.out) + (EVEN ? w.at : offset_of(a.out_at, w, head));
         const int off = EVEN ? 0 : off16(s);
         const bool aligned = off16(p) == off;
+        const Reach reach = reach_of(s, off, w.at, n, a.s_span);
         if constexpr (!LONG) {
             f2 x[NV][P];
             uint4 raw[NV];
@@ -445,7 +496,7 @@ __global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<GS, E>) k_
             if constexpr (kAhead) copy_wait<0>();
 #pragma unroll
             for (int v = 0; v < NV; ++v)
-                if (at(v) - off < w.live) raw[v] = kAhead ? mine[v * kThreads] : load_raw<EVEN>(s, at(v) - off, n, true);
+                if (at(v) - off < w.live) raw[v] = kAhead ? mine[v * kThreads] : load_raw<EVEN>(s, at(v) - off, n, reach);
             // the group's accesses that end before `plain` are live and far behind: most of them, with nothing to look up
             const int plain = EVEN ? min(w.live, w.pos - t.max_distance + 1) : 0;
 #pragma unroll
@@ -457,8 +508,11 @@ __global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<GS, E>) k_
 #pragma unroll
                     for (int i = 0; i < P; ++i) x[v][i] = fma2(factor, x[v][i], bias);
                     top = max_of(x[v], top);
+                } else if (EVEN && (v + 1) * GS * V <= w.live) {
+                    logits<EVEN, true, T, P>(t, w, raw[v], c, a.scale, x[v]);
+                    top = max_of(x[v], top);
                 } else if (c < w.live) {
-                    logits<EVEN, T, P>(t, w, raw[v], c, a.scale, x[v]);
+                    logits<EVEN, false, T, P>(t, w, raw[v], c, a.scale, x[v]);
                     top = max_of(x[v], top);
                 } else if (v * GS * V - off < w.live) {
 #pragma unroll
@@ -494,7 +548,7 @@ __global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<GS, E>) k_
             float top = -INFINITY, sum = 0.f;
             for (int c = lane * V - off; c < w.live; c += GS * V) {
                 f2 x[P];
-                logits<EVEN, T, P>(t, w, load_raw<EVEN>(s, c, n, true), c, a.scale, x);
+                logits<EVEN, false, T, P>(t, w, load_raw<EVEN>(s, c, n, reach), c, a.scale, x);
                 const float best = max_of(x, top), base = best == -INFINITY ? 0.f : best;
                 exp_of(x, base);
                 sum = sum * exp_of(top == -INFINITY ? base : top, base) + sum_of(x);
@@ -507,7 +561,7 @@ __global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<GS, E>) k_
             for (int c = lane * V - off; c < n; c += GS * V) {
                 f2 x[P] = {};
                 if (c < w.live) {
-                    logits<EVEN, T, P>(t, w, load_raw<EVEN>(s, c, n, true), c, a.scale, x);
+                    logits<EVEN, false, T, P>(t, w, load_raw<EVEN>(s, c, n, reach), c, a.scale, x);
                     exp_of(x, all);
 #pragma unroll
                     for (int i = 0; i < P; ++i) x[i] = mul2(x[i], pack2(inv, inv));
@@ -525,9 +579,9 @@ __global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<GS, E>) k_
 // keys from 128 before the query to 136 behind it, in whole accesses, into shared memory, and lane l takes the distances
 // l - 136, l - 104, ... from there.  (One by one into the sums by bucket: 9 instructions a key, for 8 keys wherever one lane's keys are
 // in different buckets.)
-constexpr int kNear = 128, kNearKeys = 2 * kNear + 16, kNearTakes = 9;
+constexpr int kNear = 128, kNearKeys = 2 * kNear + 16, kNearTakes = 9, kNearRoom = 32 * kNearTakes;
 struct Near {
-    float *room;  // [kNearKeys] of this warp
+    float *room;  // [kNearRoom] of this warp
     float sum[kNearTakes];
     __device__ __forceinline__ static int distance(int k) { return (int)threadIdx.x % 32 - kNear - 8 + 32 * k; }
     // The first key: as many elements behind a boundary of 8 as the rows begin before one.
@@ -537,7 +591,7 @@ struct Near {
 // Shared memory before the rows that are on their way: the buckets by distance, the sums.
 __host__ __device__ inline size_t grad_bytes(int max_distance, int n_buckets)
 {
-    return bucket_bytes(max_distance) + (n_buckets ? 8 * (128 * (size_t)n_buckets + 4 * kNearKeys) : 0);
+    return bucket_bytes(max_distance) + (n_buckets ? 8 * (128 * (size_t)n_buckets + 4 * kNearRoom) : 0);
 }
 
 // Adds V adjacent values, the first at distance d, to the lane's sums by bucket.
@@ -569,6 +623,68 @@ __device__ __forceinline__ void add_buckets(const unsigned char *bucket, int m, 
 // three, 127 with three and 80 bytes spilled).
 template <typename T, int E> constexpr int kGradBlocks = sizeof(T) == 2 ? (E <= 8 ? 4 : E <= 24 ? 3 : 2) : (E <= 8 ? 4 : E <= 16 ? 3 : 2);
 
+// The sums by bucket of a block, in shared memory behind the buckets of all distances, and of a thread.
+struct Sums {
+    float *lane_sums, *all;  // of this lane, one every 32; [warp][bucket][lane]
+    float behind, ahead;
+    Near near;
+    __device__ __forceinline__ Sums(const PositionArgs &a, unsigned char *room)
+    {
+        const int m = a.buckets.max_distance, n = a.buckets.n;
+        all = reinterpret_cast<float *>(room + bucket_bytes(m));
+        if (a.partials) {
+            for (int i = threadIdx.x; i <= 2 * m; i += 256) room[i] = (unsigned char)bucket_of(a.buckets, i - m);
+            for (int i = threadIdx.x; i < 8 * n * 8; i += 256) reinterpret_cast<float4 *>(all)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        __syncthreads();
+        lane_sums = all + (threadIdx.x / 32) * n * 32 + threadIdx.x % 32;
+        behind = ahead = 0.f;
+        near.room = all + 8 * n * 32 + threadIdx.x / 32 * kNearRoom;
+#pragma unroll
+        for (int k = 0; k < kNearTakes; ++k) near.sum[k] = 0.f;
+    }
+    // What the warp has put into its room from key `first` on; the group's threads have V adjacent keys each,
+    // `off` elements in front of the row the first.
+    template <int GS, int V> __device__ __forceinline__ void take(const PositionArgs &a, const Row &w, int first, int off)
+    {
+        constexpr unsigned kWarps = GS < 32 ? 1 : GS / 32;
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < kNearTakes; ++k) {
+            if (a.causal && k > 4) break;  // distances from 24 on
+            const int j = w.pos + Near::distance(k);
+            // live, and one of this warp's
+            if (j >= 0 && j < w.live && (kWarps == 1 || (unsigned)(j + off) / (32 * V) % kWarps == threadIdx.x % GS / 32) &&
+                (V == 1 || (unsigned)(j - first) < (unsigned)kNearKeys))
+                near.sum[k] += near.room[j - first];
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ void leave(const PositionArgs &a, const unsigned char *room, int head, int chunk)
+    {
+        const int m = a.buckets.max_distance, n = a.buckets.n;
+        if (!a.partials) return;
+#pragma unroll
+        for (int k = 0; k < kNearTakes; ++k) {
+            int d = Near::distance(k);
+            d = d < -m ? -m : d > m ? m : d;
+            lane_sums[room[d + m] * 32] += near.sum[k];
+        }
+        lane_sums[room[0] * 32] += behind;
+        lane_sums[room[2 * m] * 32] += ahead;
+        __syncthreads();
+        // a warp adds up a bucket: lane by lane over the warps, then over the lanes
+#pragma unroll 4
+        for (int k = threadIdx.x / 32; k < n; k += 8) {
+            float v = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += all[(i * n + k) * 32 + threadIdx.x % 32];
+            v = warp_sum(v);
+            if (threadIdx.x % 32 == 0) a.partials[((long long)head * n + k) * a.chunks + chunk] = v;
+        }
+    }
+};
+
 template <typename T, int GS, int E, bool LONG, bool EVEN>
 __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const __grid_constant__ PositionArgs a)
 {
@@ -579,28 +695,15 @@ __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const _
     griddep_wait();
     if (a.partials) griddep_launch();  // the successor is another kernel of this call
     const int head = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, m = a.buckets.max_distance;
-    float *sums = reinterpret_cast<float *>(room + bucket_bytes(m));  // [warp][bucket][lane]
-    const int n_buckets = a.buckets.n;
-    if (a.partials) {
-        for (int i = threadIdx.x; i <= 2 * m; i += 256) room[i] = (unsigned char)bucket_of(a.buckets, i - m);
-        for (int i = threadIdx.x; i < 8 * n_buckets * 8; i += 256) reinterpret_cast<float4 *>(sums)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    __syncthreads();
-    float *lane_sums = sums + (threadIdx.x / 32) * n_buckets * 32 + threadIdx.x % 32;
-    float behind = 0.f, ahead = 0.f;
+    Sums sums(a, room);
     f2 behind2 = 0ull;
     const int far_from = m > kNear + 8 ? m : kNear + 8;  // keys so far behind are in the last bucket and none of those by distance
     constexpr bool kByDistance = GS >= 32;
-    constexpr unsigned kWarps = GS < 32 ? 1 : GS / 32;
-    Near near;
-    near.room = sums + 8 * n_buckets * 32 + threadIdx.x / 32 * kNearKeys;
-#pragma unroll
-    for (int k = 0; k < kNearTakes; ++k) near.sum[k] = 0.f;
     const int lane = threadIdx.x % GS;
     const f2 scale = pack2(a.scale, a.scale);
     const auto at = [&](int v) { return (v * GS + lane) * V; };
     constexpr bool kAhead = kRowsAhead<T, LONG, EVEN>;
-    uint4 *mine = reinterpret_cast<uint4 *>(room + grad_bytes(m, a.partials ? n_buckets : 0)) + threadIdx.x;
+    uint4 *mine = reinterpret_cast<uint4 *>(room + grad_bytes(m, a.partials ? a.buckets.n : 0)) + threadIdx.x;
     const auto request = [&](const Row &w) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -619,10 +722,12 @@ __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const _
         walk.next(a);
         next = walk.here(a);
         const int n = w.n;
-        const T *p = static_cast<const T *>(a.s) + w.at, *dp = static_cast<const T *>(a.dp) + (EVEN ? w.at : offset_of(a.dp_at, w, head));
+        const long long dp_from = EVEN ? w.at : offset_of(a.dp_at, w, head);
+        const T *p = static_cast<const T *>(a.s) + w.at, *dp = static_cast<const T *>(a.dp) + dp_from;
         T *ds = static_cast<T *>(a.out) + (EVEN ? w.at : offset_of(a.out_at, w, head));
         const int off = EVEN ? 0 : off16(p);
-        const bool aligned = off16(dp) == off, out_aligned = off16(ds) == off;
+        const bool out_aligned = off16(ds) == off;
+        const Reach reach = reach_of(p, off, w.at, n, a.s_span), dp_reach = reach_of(dp, off, dp_from, n, a.dp_span);
         const int near_first = Near::first(w, off);
         // of V adjacent keys, with zeros where nothing is live: g, its sums, ds
         const auto finish = [&](const uint4 &p_raw, const uint4 &dp_raw, int c, float dot) {
@@ -638,9 +743,9 @@ __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const _
                     if (kByDistance && (unsigned)(c - near_first) < (unsigned)kNearKeys) {
                         float x[V];
                         flat(g, x);
-                        store_vec<V>(near.room + (c - near_first), x);
+                        store_vec<V>(sums.near.room + (c - near_first), x);
                     } else {
-                        add_buckets<P>(room, m, lane_sums, c - w.pos, g, behind, ahead);
+                        add_buckets<P>(room, m, sums.lane_sums, c - w.pos, g, sums.behind, sums.ahead);
                     }
                 }
 #pragma unroll
@@ -661,8 +766,8 @@ __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const _
         };
         // zeros where nothing is live
         const auto fetch = [&](int c, uint4 &p_raw, uint4 &dp_raw) {
-            p_raw = load_raw<EVEN>(p, c, n, true);
-            dp_raw = load_raw<EVEN>(dp, c, n, aligned);
+            p_raw = load_raw<EVEN>(p, c, n, reach);
+            dp_raw = load_raw<EVEN>(dp, c, n, dp_reach);
             keep_live<EVEN, T>(p_raw, c, w.live);
             keep_live<EVEN, T>(dp_raw, c, w.live);
         };
@@ -675,8 +780,8 @@ __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const _
             for (int v = 0; v < NV; ++v) {
                 const int c = at(v) - off;
                 if (c < w.live) {
-                    x[v] = kAhead ? mine[2 * v * 256] : load_raw<EVEN>(p, c, n, true);
-                    y[v] = kAhead ? mine[(2 * v + 1) * 256] : load_raw<EVEN>(dp, c, n, aligned);
+                    x[v] = kAhead ? mine[2 * v * 256] : load_raw<EVEN>(p, c, n, reach);
+                    y[v] = kAhead ? mine[(2 * v + 1) * 256] : load_raw<EVEN>(dp, c, n, dp_reach);
                 }
             }
 #pragma unroll
@@ -729,43 +834,136 @@ __global__ void __launch_bounds__(256, kGradBlocks<T, E>) k_softmax_grad(const _
                 finish(x, y, c, dot);
             }
         }
-        if (kByDistance && a.partials) {
-            __syncwarp();
-#pragma unroll
-            for (int k = 0; k < kNearTakes; ++k) {
-                if (a.causal && k > 4) break;  // distances from 24 on
-                const int j = w.pos + Near::distance(k);
-                // live, and one of this warp's
-                if (j >= 0 && j < w.live && (GS == 32 || (unsigned)(j + off) / (32 * V) % kWarps == threadIdx.x % GS / 32) &&
-                    (unsigned)(j - near_first) < (unsigned)kNearKeys)
-                    near.sum[k] += near.room[j - near_first];
-            }
-            __syncwarp();
-        }
-    }
-    if (!a.partials) return;
-    if constexpr (kByDistance) {
-#pragma unroll
-        for (int k = 0; k < kNearTakes; ++k) {
-            int d = Near::distance(k);
-            d = d < -m ? -m : d > m ? m : d;
-            lane_sums[room[d + m] * 32] += near.sum[k];
-        }
+        if (kByDistance && a.partials) sums.template take<GS, V>(a, w, near_first, off);
     }
     float lo, hi;
     unpack2(behind2, lo, hi);
-    lane_sums[room[0] * 32] += behind + (lo + hi);
-    lane_sums[room[2 * m] * 32] += ahead;
+    sums.behind += lo + hi;
+    sums.leave(a, room, head, chunk);
+}
+
+// ---- short rows anywhere --------------------------------------------------------------------
+// Rows of up to kAnyMax elements that do not begin on and end at 16-byte boundaries, or whose matrices have different strides: the threads of
+// a group take adjacent elements, one each.  16-byte accesses spend more on the ragged ends (120 MB of bf16 rows of 130: 232 us, 195; of 250
+// 144 and 129; gradient 336 and 220, 195 and 167), longer rows do not (float32 of 250: 63 and 67, gradient 81 and 92).
+template <typename T> constexpr int kAnyMax = sizeof(T) == 4 ? 192 : 256;
+
+__device__ __forceinline__ float bias_at(const Bias &t, int d)
+{
+    const int m = t.max_distance;
+    d = d < -m ? -m : d > m ? m : d;
+    return t.bucket ? t.by_distance[t.bucket[d + m]] : t.by_distance[d + t.reach];
+}
+
+template <typename T, int GS, int E>
+__global__ void __launch_bounds__(GS > 256 ? GS : 256, kSoftmaxBlocks<T, GS, E, false>) k_softmax_any(const __grid_constant__ PositionArgs a)
+{
+    constexpr int kThreads = GS > 256 ? GS : 256, kGroups = kThreads / GS;
+    extern __shared__ __align__(16) unsigned char room[];
+    __shared__ float scratch[2][32];
+    griddep_wait();
+    griddep_launch();
+    const int head = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+    const Bias t = make_bias(a, head, room);
     __syncthreads();
-    // a warp adds up a bucket: lane by lane over the warps, then over the lanes
-#pragma unroll 4
-    for (int k = threadIdx.x / 32; k < n_buckets; k += 8) {
-        float v = 0.f;
+    const int lane = threadIdx.x % GS;
+    Walk<kGroups> walk(a, head, chunk, threadIdx.x / GS);
+    // the groups of a block take as many rounds
+    for (unsigned r = chunk * kGroups; r < (unsigned)a.rows; r += walk.step, walk.next(a)) {
+        const Row w = walk.here(a);
+        const T *s = static_cast<const T *>(a.s) + w.at;
+        T *p = static_cast<T *>(a.out) + offset_of(a.out_at, w, head);
+        const int far = w.pos - t.max_distance + 1;  // keys before it are far behind
+        float x[E], top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v += sums[(i * n_buckets + k) * 32 + threadIdx.x % 32];
-        v = warp_sum(v);
-        if (threadIdx.x % 32 == 0) a.partials[((long long)head * n_buckets + k) * a.chunks + chunk] = v;
+        for (int k = 0; k < E; ++k)
+            if (k * GS + lane < w.live) x[k] = to_f32(s[k * GS + lane]);
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            const int c = k * GS + lane;
+            if (k * GS >= w.live) break;
+            if ((k + 1) * GS <= min(far, w.live)) x[k] = fmaf(a.scale, x[k], t.behind);
+            else x[k] = c < w.live ? fmaf(a.scale, x[k], bias_at(t, c - w.pos)) : -INFINITY;
+            top = fmaxf(top, x[k]);
+        }
+        top = group_join<GS, true>(top, scratch);
+        if (top == -INFINITY) top = 0.f;  // nothing is live, all is -inf, or the rest is NaN
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            if (k * GS >= w.live) break;
+            sum += x[k] = exp_of(x[k], top);
+        }
+        sum = group_join<GS, false>(sum, scratch + 1);
+        const float inv = sum == 0.f ? 0.f : reciprocal(sum);
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            const int c = k * GS + lane;
+            if (c < w.n) put(p + c, c < w.live ? x[k] * inv : 0.f);
+        }
     }
+}
+
+template <typename T, int E> constexpr int kGradAnyBlocks = E <= 8 ? 4 : E <= 16 ? 3 : 2;
+
+template <typename T, int GS, int E>
+__global__ void __launch_bounds__(256, kGradAnyBlocks<T, E>) k_softmax_grad_any(const __grid_constant__ PositionArgs a)
+{
+    constexpr int kGroups = 256 / GS;
+    extern __shared__ __align__(16) unsigned char room[];
+    __shared__ float scratch[2][32];
+    int turn = 0;
+    griddep_wait();
+    if (a.partials) griddep_launch();  // the successor is another kernel of this call
+    const int head = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, m = a.buckets.max_distance;
+    Sums sums(a, room);
+    constexpr bool kByDistance = GS >= 32;
+    const int far_from = m > kNear + 8 ? m : kNear + 8;  // keys so far behind are in the last bucket and none of those by distance
+    const int lane = threadIdx.x % GS;
+    Walk<kGroups> walk(a, head, chunk, threadIdx.x / GS);
+    for (unsigned r = chunk * kGroups; r < (unsigned)a.rows; r += walk.step, walk.next(a)) {
+        const Row w = walk.here(a);
+        const T *p = static_cast<const T *>(a.s) + w.at, *dp = static_cast<const T *>(a.dp) + offset_of(a.dp_at, w, head);
+        T *ds = static_cast<T *>(a.out) + offset_of(a.out_at, w, head);
+        const int near_first = w.pos - kNear - 8;
+        // g of a live key
+        const auto add = [&](float g, int c) {
+            if (kByDistance && (unsigned)(c - near_first) < (unsigned)kNearRoom) {
+                sums.near.room[c - near_first] = g;
+            } else {
+                const int d = c - w.pos;
+                if (d <= -m) sums.behind += g;
+                else if (d >= m) sums.ahead += g;
+                else sums.lane_sums[room[d + m] * 32] += g;
+            }
+        };
+        float dot = 0.f;
+        float x[E], y[E];
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            if (k * GS + lane < w.live) {
+                x[k] = to_f32(p[k * GS + lane]);
+                y[k] = to_f32(dp[k * GS + lane]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+            if (k * GS + lane < w.live) dot = fmaf(x[k], y[k], dot);
+        dot = group_join<GS, false>(dot, scratch + (turn ^= 1));
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            const int c = k * GS + lane;
+            if (k * GS >= w.n) break;
+            float g = 0.f;
+            if (c < w.live) {
+                g = x[k] * (y[k] - dot);
+                if ((k + 1) * GS <= w.pos - far_from) sums.behind += g;
+                else if (a.partials) add(g, c);
+            }
+            if (a.out && c < w.n) put(ds + c, a.scale * g);
+        }
+        if (kByDistance && a.partials) sums.template take<GS, 1>(a, w, near_first, 0);
+    }
+    sums.leave(a, room, head, chunk);
 }
 
 struct JoinArgs {
@@ -882,15 +1080,21 @@ int chunks_of(long long rows, long long heads, int groups, int sms, int blocks, 
     return (int)std::max<long long>(1, std::min(std::min(want, most), ceil_div(rows, groups)));
 }
 
-template <typename T, int GS, int E, bool LONG, bool EVEN> cudaError_t run_softmax(PositionArgs &a, int heads, int sms, cudaStream_t s)
+// How rows are read: 16 bytes a thread, on boundaries or with ragged ends, or one element a thread.
+enum Rows { kEven, kRagged, kAny };
+
+template <typename T, int GS, int E, bool LONG, Rows R> cudaError_t run_softmax(PositionArgs &a, int heads, int sms, cudaStream_t s)
 {
     static OncePerDevice known;
     constexpr int kThreads = GS > 256 ? GS : 256;
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_softmax<T, GS, E, LONG, EVEN>), known);
+    void (*kernel)(PositionArgs);
+    if constexpr (R == kAny) kernel = k_softmax_any<T, GS, E>;
+    else kernel = k_softmax<T, GS, E, LONG, R == kEven>;
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(kernel), known);
     if (e != cudaSuccess) return e;
-    const size_t smem = bias_bytes(a.buckets.max_distance, a.buckets.n) + (kRowsAhead<T, LONG, EVEN> ? kThreads * E * sizeof(T) : 0);
-    a.chunks = chunks_of(a.rows, heads, kThreads / GS, sms, kSoftmaxBlocks<GS, E>, smem);
-    return launch(k_softmax<T, GS, E, LONG, EVEN>, (long long)heads * a.chunks, kThreads, smem, s, a);
+    const size_t smem = bias_bytes(a.buckets.max_distance, a.buckets.n) + (R != kAny && kRowsAhead<T, LONG, R == kEven> ? kThreads * E * sizeof(T) : 0);
+    a.chunks = chunks_of(a.rows, heads, kThreads / GS, sms, kSoftmaxBlocks<T, GS, E, R == kEven>, smem);
+    return launch(kernel, (long long)heads * a.chunks, kThreads, smem, s, a);
 }
 // Whether all rows of a matrix begin on 16-byte boundaries.
 template <typename T> bool on16(const void *p, const Strides &at)
@@ -909,45 +1113,77 @@ template <typename T> bool all_even(const PositionArgs &a)
     return a.n_keys % (16 / (int)sizeof(T)) == 0 && on16<T>(a.s, a.s_at) && same(a.dp, a.dp_at) && same(a.out, a.out_at);
 }
 // The narrowest group whose registers hold a row.
-template <typename T, bool EVEN> cudaError_t pick_softmax(PositionArgs &a, int heads, int sms, cudaStream_t s)
+template <typename T, Rows R> cudaError_t pick_softmax(PositionArgs &a, int heads, int sms, cudaStream_t s)
 {
-    const long long n = held<T>(a);
-    if (n <= 8 * 8) return run_softmax<T, 8, 8, false, EVEN>(a, heads, sms, s);
-    if (n <= 8 * 16) return run_softmax<T, 8, 16, false, EVEN>(a, heads, sms, s);
-    if (n <= 32 * 8) return run_softmax<T, 32, 8, false, EVEN>(a, heads, sms, s);
-    if (n <= 32 * 16) return run_softmax<T, 32, 16, false, EVEN>(a, heads, sms, s);
-    if (n <= 32 * 32) return run_softmax<T, 32, 32, false, EVEN>(a, heads, sms, s);
-    if (n <= 64 * 32) return run_softmax<T, 64, 32, false, EVEN>(a, heads, sms, s);
-    if (n <= 128 * 32) return run_softmax<T, 128, 32, false, EVEN>(a, heads, sms, s);
-    if (n <= 256 * 32) return run_softmax<T, 256, 32, false, EVEN>(a, heads, sms, s);
-    if (n <= 1024 * 16) return run_softmax<T, 1024, 16, false, EVEN>(a, heads, sms, s);
-    return run_softmax<T, 1024, 8, true, EVEN>(a, heads, sms, s);
+    const long long n = R == kRagged ? held<T>(a) : a.n_keys;
+    if constexpr (R != kRagged) {
+        if (n <= 8 * 8) return run_softmax<T, 8, 8, false, R>(a, heads, sms, s);
+        if (n <= 8 * 16) return run_softmax<T, 8, 16, false, R>(a, heads, sms, s);
+    }
+    if (R == kAny || n <= 32 * 8) return run_softmax<T, 32, 8, false, R>(a, heads, sms, s);
+    if constexpr (R != kAny) {
+        if (n <= 32 * 16) return run_softmax<T, 32, 16, false, R>(a, heads, sms, s);
+        if (n <= 32 * 24) return run_softmax<T, 32, 24, false, R>(a, heads, sms, s);
+        if (n <= 32 * 32) return run_softmax<T, 32, 32, false, R>(a, heads, sms, s);
+        if (n <= 64 * 32) return run_softmax<T, 64, 32, false, R>(a, heads, sms, s);
+        if (n <= 128 * 32) return run_softmax<T, 128, 32, false, R>(a, heads, sms, s);
+        if (n <= 256 * 32) return run_softmax<T, 256, 32, false, R>(a, heads, sms, s);
+        if (n <= 1024 * 16) return run_softmax<T, 1024, 16, false, R>(a, heads, sms, s);
+        return run_softmax<T, 1024, 8, true, R>(a, heads, sms, s);
+    }
+}
+template <typename T> cudaError_t pick_softmax(PositionArgs &a, int heads, int sms, cudaStream_t s)
+{
+    if (all_even<T>(a)) return pick_softmax<T, kEven>(a, heads, sms, s);
+    return a.n_keys <= kAnyMax<T> ? pick_softmax<T, kAny>(a, heads, sms, s) : pick_softmax<T, kRagged>(a, heads, sms, s);
 }
 
-template <typename T, int GS, int E, bool LONG, bool EVEN> cudaError_t run_grad(PositionArgs &a, int heads, int sms, cudaStream_t s)
+template <typename T, int GS, int E, bool LONG, Rows R> cudaError_t run_grad(PositionArgs &a, int heads, int sms, cudaStream_t s)
 {
     static OncePerDevice known;
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(&k_softmax_grad<T, GS, E, LONG, EVEN>), known);
+    void (*kernel)(PositionArgs);
+    if constexpr (R == kAny) kernel = k_softmax_grad_any<T, GS, E>;
+    else kernel = k_softmax_grad<T, GS, E, LONG, R == kEven>;
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(kernel), known);
     if (e != cudaSuccess) return e;
-    const size_t smem = grad_bytes(a.buckets.max_distance, a.partials ? a.buckets.n : 0) + (kRowsAhead<T, LONG, EVEN> ? 256 * 2 * E * sizeof(T) : 0);
-    a.chunks = chunks_of(a.rows, heads, 256 / GS, sms, kGradBlocks<T, E>, smem);
-    return launch(k_softmax_grad<T, GS, E, LONG, EVEN>, (long long)heads * a.chunks, 256, smem, s, a);
+    const size_t smem = grad_bytes(a.buckets.max_distance, a.partials ? a.buckets.n : 0) +
+                        (R != kAny && kRowsAhead<T, LONG, R == kEven> ? 256 * 2 * E * sizeof(T) : 0);
+    a.chunks = chunks_of(a.rows, heads, 256 / GS, sms, R == kAny ? kGradAnyBlocks<T, E> : kGradBlocks<T, E>, smem);
+    return launch(kernel, (long long)heads * a.chunks, 256, smem, s, a);
 }
-template <typename T, bool EVEN> cudaError_t pick_grad(PositionArgs &a, int heads, int sms, cudaStream_t s)
+template <typename T, Rows R> cudaError_t pick_grad(PositionArgs &a, int heads, int sms, cudaStream_t s)
 {
-    const long long n = held<T>(a);
-    if (n <= 8 * 8) return run_grad<T, 8, 8, false, EVEN>(a, heads, sms, s);
-    if (n <= 8 * 16) return run_grad<T, 8, 16, false, EVEN>(a, heads, sms, s);
-    if (n <= 32 * 8) return run_grad<T, 32, 8, false, EVEN>(a, heads, sms, s);
-    if (n <= 32 * 16) return run_grad<T, 32, 16, false, EVEN>(a, heads, sms, s);
-    if (n <= 32 * 24) return run_grad<T, 32, 24, false, EVEN>(a, heads, sms, s);
-    if (n <= 32 * 32) return run_grad<T, 32, 32, false, EVEN>(a, heads, sms, s);
-    if (n <= 64 * 32) return run_grad<T, 64, 32, false, EVEN>(a, heads, sms, s);
-    if (n <= 128 * 32) return run_grad<T, 128, 32, false, EVEN>(a, heads, sms, s);
-    if (n <= 256 * 32) return run_grad<T, 256, 32, false, EVEN>(a, heads, sms, s);
-    return run_grad<T, 256, 8, true, EVEN>(a, heads, sms, s);
+    const long long n = R == kRagged ? held<T>(a) : a.n_keys;
+    if constexpr (R != kRagged) {
+        if (n <= 8 * 8) return run_grad<T, 8, 8, false, R>(a, heads, sms, s);
+        if (n <= 8 * 16) return run_grad<T, 8, 16, false, R>(a, heads, sms, s);
+    }
+    if (R == kAny || n <= 32 * 8) return run_grad<T, 32, 8, false, R>(a, heads, sms, s);
+    if constexpr (R != kAny) {
+        if (n <= 32 * 16) return run_grad<T, 32, 16, false, R>(a, heads, sms, s);
+        if (n <= 32 * 24) return run_grad<T, 32, 24, false, R>(a, heads, sms, s);
+        if (n <= 32 * 32) return run_grad<T, 32, 32, false, R>(a, heads, sms, s);
+        if (n <= 64 * 32) return run_grad<T, 64, 32, false, R>(a, heads, sms, s);
+        if (n <= 128 * 32) return run_grad<T, 128, 32, false, R>(a, heads, sms, s);
+        if (n <= 256 * 32) return run_grad<T, 256, 32, false, R>(a, heads, sms, s);
+        return run_grad<T, 256, 8, true, R>(a, heads, sms, s);
+    }
+}
+template <typename T> cudaError_t pick_grad(PositionArgs &a, int heads, int sms, cudaStream_t s)
+{
+    if (all_even<T>(a)) return pick_grad<T, kEven>(a, heads, sms, s);
+    return a.n_keys <= kAnyMax<T> ? pick_grad<T, kAny>(a, heads, sms, s) : pick_grad<T, kRagged>(a, heads, sms, s);
 }
 
+// Strides, 0 where there is only one; and how many elements a matrix reaches over.
+template <typename A> Strides used(const A &a, long long b, long long h, long long q)
+{
+    return {a.batch > 1 ? b : 0, a.heads > 1 ? h : 0, a.n_queries > 1 ? q : 0};
+}
+template <typename A> long long span_of(const A &a, const Strides &at)
+{
+    return (a.batch - 1) * at.b + (a.heads - 1) * at.h + (a.n_queries - 1) * at.q + a.n_keys;
+}
 template <typename A> void fill_common(PositionArgs &p, const A &a)
 {
     p.lengths = a.lengths;
@@ -989,11 +1225,12 @@ extern "C" adascale_status adascale_position_softmax(const adascale_position_sof
     p.out = a.probs;
     p.table = a.table;
     p.ld_table = a.ld_table;
-    p.s_at = {a.scores_stride_b, a.scores_stride_h, a.scores_stride_q};
-    p.out_at = {a.probs_stride_b, a.probs_stride_h, a.probs_stride_q};
+    p.s_at = used(a, a.scores_stride_b, a.scores_stride_h, a.scores_stride_q);
+    p.out_at = used(a, a.probs_stride_b, a.probs_stride_h, a.probs_stride_q);
+    p.s_span = span_of(a, p.s_at);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    if (a.dtype == ADASCALE_BF16) OPS_CU(all_even<bf16>(p) ? pick_softmax<bf16, true>(p, (int)a.heads, sms, s) : pick_softmax<bf16, false>(p, (int)a.heads, sms, s));
-    else OPS_CU(all_even<float>(p) ? pick_softmax<float, true>(p, (int)a.heads, sms, s) : pick_softmax<float, false>(p, (int)a.heads, sms, s));
+    if (a.dtype == ADASCALE_BF16) OPS_CU(pick_softmax<bf16>(p, (int)a.heads, sms, s));
+    else OPS_CU(pick_softmax<float>(p, (int)a.heads, sms, s));
     return ADASCALE_OK;
 }
 
@@ -1036,13 +1273,15 @@ extern "C" adascale_status adascale_position_softmax_grad(const adascale_positio
     p.dp = a.dprobs;
     p.out = a.dscores;
     p.partials = a.dtable ? static_cast<float *>(a.workspace) : nullptr;
-    p.s_at = {a.probs_stride_b, a.probs_stride_h, a.probs_stride_q};
-    p.dp_at = {a.dprobs_stride_b, a.dprobs_stride_h, a.dprobs_stride_q};
-    p.out_at = {a.dscores_stride_b, a.dscores_stride_h, a.dscores_stride_q};
+    p.s_at = used(a, a.probs_stride_b, a.probs_stride_h, a.probs_stride_q);
+    p.dp_at = used(a, a.dprobs_stride_b, a.dprobs_stride_h, a.dprobs_stride_q);
+    p.out_at = used(a, a.dscores_stride_b, a.dscores_stride_h, a.dscores_stride_q);
+    p.s_span = span_of(a, p.s_at);
+    p.dp_span = span_of(a, p.dp_at);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     if (!nothing) {
-        if (a.dtype == ADASCALE_BF16) OPS_CU(all_even<bf16>(p) ? pick_grad<bf16, true>(p, (int)a.heads, sms, s) : pick_grad<bf16, false>(p, (int)a.heads, sms, s));
-        else OPS_CU(all_even<float>(p) ? pick_grad<float, true>(p, (int)a.heads, sms, s) : pick_grad<float, false>(p, (int)a.heads, sms, s));
+        if (a.dtype == ADASCALE_BF16) OPS_CU(pick_grad<bf16>(p, (int)a.heads, sms, s));
+        else OPS_CU(pick_grad<float>(p, (int)a.heads, sms, s));
     }
     if (!a.dtable) return ADASCALE_OK;
     JoinArgs j = {p.partials, a.dtable, a.ld_dtable, (int)a.heads, a.n_buckets, nothing ? 0 : p.chunks, a.accumulate != 0};
