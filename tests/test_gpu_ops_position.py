@@ -392,3 +392,32 @@ def test_many_batches_and_heads():
         flat = lambda t: torch.zeros(8, shape[1], dtype=torch.float64, device=DEV).index_add_(0, at, t.sum(0).reshape(shape[1], -1).t())  # noqa: E731
         terms = shape[0] * shape[2] * 32
         check(got.dtable, flat(g), flat(off) + (terms + 45) * U * flat(g.abs()) + 2 * U * flat(g).abs(), "dtable")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(2, 3, 200, 13), (2, 3, 150, 201), (2, 4, 120, 301), (1, 8, 300, 999), (1, 2, 40, 2051)])
+def test_in_place_where_rows_share_accesses(shape, dtype):
+    """Rows whose ends lie in 16 bytes with their neighbours', which other threads write at the same time: the same bits as elsewhere,
+    in place and between poison on either side."""
+    case, tensor, table = make(shape, dtype, 7, True, False, True, False)
+    scores, dprobs = tensor(8.0), tensor(1.0)
+    probs = ops.position_softmax(scores, table, **how(case))
+    got = ops.position_softmax_grad(probs, dprobs, 32, **how(case))
+    for _ in range(3):
+        place = scores.clone()
+        assert torch.equal(ops.position_softmax(place, table, **how(case), out=place), probs)
+        for alias in (0, 1):
+            args = [probs.clone(), dprobs.clone()]
+            ops.position_softmax_grad(*args, 32, **how(case), dscores=args[alias])
+            assert torch.equal(args[alias], got.dscores)
+    for before in (1, 3, 8):  # whatever lies around the tensors is not used and stays
+        whole = [torch.full((before + scores.numel() + 9,), float("nan"), dtype=dtype, device=DEV) for _ in range(4)]
+        s, d, p, o = (w[before:before + scores.numel()].view(shape) for w in whole)
+        s.copy_(scores)
+        d.copy_(dprobs)
+        ops.position_softmax(s, table, **how(case), out=p)
+        again = ops.position_softmax_grad(p, d, 32, **how(case), dscores=o)
+        check_forward(p, scores, table, case, "between poison")
+        check_gradient(again, p, dprobs, case, None, "between poison")
+        for w in whole:
+            assert bool(torch.isnan(w[:before]).all()) and bool(torch.isnan(w[before + scores.numel():]).all())
