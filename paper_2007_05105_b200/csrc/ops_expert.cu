@@ -287,13 +287,21 @@ template <Form F, int NT, int LANES> __device__ __forceinline__ void find_tile(c
     }
 }
 
-// Waits of this kernel have a limit (kWaitNs) like all others, and one that runs out sets a flag that ends every other: the
-// block then runs to its end without copies, and what it would have stored is NaN.
-template <bool CLUSTER> __device__ __noinline__ void wait_long(u64 *bar, unsigned parity, volatile int *gave_up)
+// Waits of this kernel have a limit like all others (kWaitNs, or kPolls), and one that runs out sets a flag that ends the block's others.
+// Who gave up does nothing further that others go by: no instruction is issued and no barrier arrived at for what has not come, so
+// that in a pair the other block's waits run out too, rather than that it stores half a sum.  What a block has not computed is NaN.
+// The thread that issues copies does not look at the flag: in a pair both then stop at the same stage, and their copies are seen
+// through (see the end of its branch), as are the matrix instructions, before shared and tensor memory are given up.
+#ifndef ADASCALE_EXPERT_POLLS  // a test makes the waits run out at once
+#define ADASCALE_EXPERT_POLLS (1u << 22)
+#endif
+constexpr unsigned kPolls = ADASCALE_EXPERT_POLLS;
+template <bool CLUSTER> __device__ __noinline__ bool wait_long(u64 *bar, unsigned parity, volatile int *gave_up)
 {
     u64 t0 = 0;
-    for (unsigned spin = 0; spin < 1u << 22; ++spin) {
-        if (mbar_poll<CLUSTER>(smem_u32(bar), parity) || *gave_up) return;
+    for (unsigned spin = 0; spin < kPolls; ++spin) {
+        if (mbar_poll<CLUSTER>(smem_u32(bar), parity)) return true;
+        if (*gave_up) return false;
         if ((spin & 63u) == 63u) {
             u64 now;
             asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
@@ -302,10 +310,12 @@ template <bool CLUSTER> __device__ __noinline__ void wait_long(u64 *bar, unsigne
         }
     }
     *gave_up = 1;
+    return false;
 }
-template <bool CLUSTER = false> __device__ __forceinline__ void wait_for(u64 *bar, unsigned parity, volatile int *gave_up)
+// False if it gave up.
+template <bool CLUSTER = false> __device__ __forceinline__ bool wait_for(u64 *bar, unsigned parity, volatile int *gave_up)
 {
-    if (!mbar_poll<CLUSTER>(smem_u32(bar), parity)) wait_long<CLUSTER>(bar, parity, gave_up);
+    return mbar_poll<CLUSTER>(smem_u32(bar), parity) || wait_long<CLUSTER>(bar, parity, gave_up);
 }
 
 // ---- results -------------------------------------------------------------------------------
@@ -480,15 +490,19 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
         if (elected()) {
             Tile t = {};
             int stage = 0, issued = 0;
+            bool in_time = true;
             unsigned phase = 1;  // the first pass over the ring waits for nobody
-            for (int tile = first_tile; tile < n_tiles; tile += step) {
+            for (int tile = first_tile; in_time && tile < n_tiles; tile += step) {
                 find_tile<F, NT, LANES>(a, x, tile, rank, t);
                 // this block's columns: all of them, or its half
                 const int half = PAIR ? (t.width + 31) / 32 * 16 : t.width, column = t.column + rank * half;
                 const int boxes = F == DW ? (half + 63) / 64 : (half + kBox - 1) / kBox;
                 for (int k = 0; k < t.summands; k += kK) {
-                    wait_for(&empty[stage], phase, &gave_up);
-                    if (gave_up) break;
+                    in_time = mbar_wait(&empty[stage], phase);
+                    if (!in_time) {
+                        gave_up = 1;
+                        break;
+                    }
                     unsigned char *as = ring + stage * kStageBytes<NT, PAIR>, *bs = as + kA;
                     const int bytes = kA + boxes * (F == DW ? 64 : kBox) * kK * 2;
                     // in a pair the first block's barrier takes both blocks' bytes; the ends of groups go to each one's own
@@ -510,38 +524,43 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                     if (++stage == S) stage = 0, phase ^= 1;
                 }
             }
-            // copies in flight end before the block does: their stages have been worked on
-            for (int i = 0; i < min(issued, S); ++i) {
+            // Copies in flight end before the block does.  The first block's barriers know of both blocks' (which leave together); the second
+            // one sees its last stage worked on, or has waited for it as long as a wait can last.
+            for (int i = 0; i < min(issued, S) && rank == 0; ++i) {
                 const int n = issued - 1 - i;
-                wait_for(&empty[n % S], (n / S) & 1, &gave_up);
+                if (!mbar_wait(&full[n % S], (n / S) & 1)) break;
             }
+            if (rank == 1 && issued > 0) (void)mbar_wait(&empty[(issued - 1) % S], ((issued - 1) / S) & 1);
         }
     } else if (warp == 1 && rank == 0) {
         if (elected()) {
             Tile t = {};
             int stage = 0, turn = 0;
+            bool in_time = true;
             unsigned phase = 0, free_phase = 1, end_phase = 0, there_phase = 0;
-            for (int tile = first_tile; tile < n_tiles; tile += step) {
+            for (int tile = first_tile; in_time && tile < n_tiles; tile += step) {
                 find_tile<F, NT, LANES>(a, x, tile, rank, t);
                 const unsigned n = PAIR ? (t.width + 31) / 32 * 32 : (t.width + 15) / 16 * 16;
                 const unsigned what =
                     1u << 4 | 1u << 7 | 1u << 10 | (kAcrossA ? 1u << 15 : 0u) | (kAcrossB ? 1u << 16 : 0u) | n / 8 << 17 | (unsigned)(LANES / 16) << 24;
                 for (int begin = 0; begin < t.summands; begin += part) {
-                    wait_for<PAIR>(&taken[turn], free_phase, &gave_up);
+                    in_time = wait_for<PAIR>(&taken[turn], free_phase, &gave_up);
+                    if (!in_time) break;
                     tmem_fence_after();
                     const unsigned d = tmem + turn * NT;
                     const int end = min(t.summands, begin + part);
                     for (int k = begin; k < end; k += kK) {
-                        wait_for(&full[stage], phase, &gave_up);
-                        if (F == DW && t.summands - k < kK) {  // it is there: warp 2 may end it
+                        in_time = wait_for(&full[stage], phase, &gave_up);
+                        if (F == DW && in_time && t.summands - k < kK) {  // it is there: warp 2 may end it
                             mbar_arrive(&arrived);
-                            wait_for(&ended, end_phase, &gave_up);
+                            in_time = wait_for(&ended, end_phase, &gave_up);
                             end_phase ^= 1;
                             if constexpr (PAIR) {
-                                wait_for<true>(&there[stage], there_phase >> stage & 1, &gave_up);
+                                in_time = in_time && wait_for<true>(&there[stage], there_phase >> stage & 1, &gave_up);
                                 there_phase ^= 1u << stage;
                             }
                         }
+                        if (!in_time) break;
                         tmem_fence_after();
                         const unsigned as = smem_u32(ring + stage * kStageBytes<NT, PAIR>);
                         const u64 da = operand(as, kAcrossA ? 8192 : 16), db = operand(as + kA, kAcrossB ? 8192 : 16);
@@ -551,6 +570,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                         mma_commit<PAIR>(&empty[stage]);
                         if (++stage == S) stage = 0, phase ^= 1;
                     }
+                    if (!in_time) break;
                     mma_commit<PAIR>(&done[turn]);
                     if (a.in_parts) {
                         free_phase ^= 1;
@@ -560,6 +580,9 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                     }
                 }
             }
+            // those in flight end before the block does: the last one's stage
+            if (stage == 0) phase ^= 1;
+            (void)mbar_wait(&empty[stage == 0 ? S - 1 : stage - 1], phase);
         }
     } else if (F == DW && warp == 2) {  // rows of the next expert, or of nobody, behind the last of e's: zeros
         Tile t = {};
@@ -571,14 +594,15 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
             const int left = t.summands % kK;
             if (left == 0) continue;
             const int stage = (blocks - 1) % S;
+            bool in_time;
             if (rank == 0) {
-                wait_for(&arrived, phase, &gave_up);
+                in_time = wait_for(&arrived, phase, &gave_up);
                 phase ^= 1;
             } else {
-                wait_for(&full[stage], phase >> stage & 1, &gave_up);
+                in_time = wait_for(&full[stage], phase >> stage & 1, &gave_up);
                 phase ^= 1u << stage;
             }
-            __syncwarp();
+            if (!__all_sync(0xffffffffu, in_time)) break;
             unsigned char *as = ring + stage * kStageBytes<NT, PAIR>;
             const int half = PAIR ? (t.width + 31) / 32 * 16 : t.width, boxes = 2 + (half + 63) / 64;
             for (int box = 0; box < boxes; ++box)
@@ -600,16 +624,15 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
         Tile t = {};
         int turn = 0;
         unsigned phase = 0;
+        bool lost = false;  // a wait ran out, in this tile or one before: NaN from here on
         for (int tile = first_tile; tile < n_tiles; tile += step) {
             find_tile<F, NT, LANES>(a, x, tile, rank, t);
             for (int begin = 0; begin < t.summands || begin == 0; begin += part) {
                 const bool any = t.summands > 0, last = begin + part >= t.summands;
-                if (any) {
-                    wait_for(&done[turn], phase, &gave_up);
-                    __syncwarp();
+                if (any && !lost) {
+                    lost = !__all_sync(0xffffffffu, wait_for(&done[turn], phase, &gave_up));
                     tmem_fence_after();
                 }
-                const bool lost = __any_sync(0xffffffffu, gave_up);
                 const unsigned from = tmem + turn * NT + mine, sums = tmem + NT + mine;
                 const auto taken_now = [&] {
                     tmem_fence_before();
@@ -619,7 +642,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                         else mbar_arrive(&taken[turn]);
                     }
                 };
-                if (a.in_parts && any) {  // to the running sum at once, so that the next part may begin before results are stored
+                if (a.in_parts && any && !lost) {  // to the running sum at once, so that the next part may begin before results are stored
                     for (int c = first; c < t.width; c += kEvery) {
                         unsigned now[32], before[32];
                         tmem_load(from + c, now);
@@ -659,7 +682,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                         else store_tokens<O>(a, v, room, t.lane + quarter * 32, t.column + c, n);
                     }
                 }
-                if (!any) continue;
+                if (!any || lost) continue;
                 if (!a.in_parts) taken_now();
                 if (a.in_parts) {
                     phase ^= 1;
