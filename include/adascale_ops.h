@@ -28,7 +28,7 @@
  *     adascale_step may follow directly, with ADASCALE_FLAG_GRADS_READY too.
  *   - Results are the same bits from run to run: no sum depends on the order in which blocks run.
  *   - Inputs and outputs must not overlap unless a field says so.
- *   - Waits inside a kernel (for its own copies and instructions) are bounded, by seconds: results that were not computed because one ran
+ *   - Waits inside a kernel (for its own copies and instructions) are bounded, by seconds in which it gets no further: results that were not computed because one ran
  *     out are NaN, and the kernel ends when its copies in flight have come.  The call has returned by then: no status tells of it.
  *   - Errors: INVALID_ARG (null pointer, negative size, unknown enum, stride below the row's length,
  *     non-finite constant, workspace too small), ALIGNMENT (a pointer not aligned to its element size),

@@ -287,7 +287,7 @@ template <Form F, int NT, int LANES> __device__ __forceinline__ void find_tile(c
     }
 }
 
-// Waits of this kernel have a limit like all others (kWaitNs, or kPolls), and one that runs out sets a flag that ends the block's others.
+// Waits of this kernel have a limit like all others (kWaitNs, or kPolls, in which the block gets no further), and one that runs out sets a flag that ends the block's others.
 // Who gave up does nothing further that others go by: no instruction is issued and no barrier arrived at for what has not come, so
 // that in a pair the other block's waits run out too, rather than that it stores half a sum.  What a block has not computed is NaN.
 // The thread that issues copies does not look at the flag: in a pair both then stop at the same stage, and their copies are seen
@@ -296,26 +296,38 @@ template <Form F, int NT, int LANES> __device__ __forceinline__ void find_tile(c
 #define ADASCALE_EXPERT_POLLS (1u << 22)
 #endif
 constexpr unsigned kPolls = ADASCALE_EXPERT_POLLS;
-template <bool CLUSTER> __device__ __noinline__ bool wait_long(u64 *bar, unsigned parity, volatile int *gave_up)
+// What a block's waits go by.
+struct Waits {
+    volatile int gave_up;
+    volatile unsigned issued;  // stages, by the thread that issues copies
+};
+template <bool CLUSTER> __device__ __noinline__ bool wait_long(u64 *bar, unsigned parity, Waits &waits)
 {
-    u64 t0 = 0;
-    for (unsigned spin = 0; spin < kPolls; ++spin) {
-        if (mbar_poll<CLUSTER>(smem_u32(bar), parity)) return true;
-        if (*gave_up) return false;
-        if ((spin & 63u) == 63u) {
-            u64 now;
-            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
-            if (t0 == 0) t0 = now;
-            else if (now - t0 > kWaitNs) break;
+    // A sum may last (2^31 rows of 8 columns, one block's, 13 s), and who waits for its end or for the end of a group behind it is not late: the
+    // limit holds for a time in which nothing was issued either.
+    for (unsigned seen = waits.issued;;) {
+        u64 t0 = 0;
+        for (unsigned spin = 0; spin < kPolls; ++spin) {
+            if (mbar_poll<CLUSTER>(smem_u32(bar), parity)) return true;
+            if (waits.gave_up) return false;
+            if ((spin & 63u) == 63u) {
+                u64 ns;
+                asm volatile("mov.u64 %0, %globaltimer;" : "=l"(ns));
+                if (t0 == 0) t0 = ns;
+                else if (ns - t0 > kWaitNs) break;
+            }
         }
+        const unsigned now = waits.issued;
+        if (now == seen) break;
+        seen = now;
     }
-    *gave_up = 1;
+    waits.gave_up = 1;
     return false;
 }
 // False if it gave up.
-template <bool CLUSTER = false> __device__ __forceinline__ bool wait_for(u64 *bar, unsigned parity, volatile int *gave_up)
+template <bool CLUSTER = false> __device__ __forceinline__ bool wait_for(u64 *bar, unsigned parity, Waits &waits)
 {
-    return mbar_poll<CLUSTER>(smem_u32(bar), parity) || wait_long<CLUSTER>(bar, parity, gave_up);
+    return mbar_poll<CLUSTER>(smem_u32(bar), parity) || wait_long<CLUSTER>(bar, parity, waits);
 }
 
 // ---- results -------------------------------------------------------------------------------
@@ -444,7 +456,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
     extern __shared__ unsigned char raw[];
     __shared__ u64 full[S], there[S], empty[S], done[2], taken[2], arrived, ended;
     __shared__ unsigned tmem_base;
-    __shared__ volatile int gave_up;
+    __shared__ Waits waits;
     __shared__ int begins[kMaxExperts + 1], tile_sums[kMaxExperts + 1];
     unsigned char *staging = raw + (1024 - smem_u32(raw) % 1024) % 1024, *ring = staging + kStaging<O>;
     const Experts x = {begins, tile_sums};
@@ -458,7 +470,8 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
             mbar_init(&there[i], 1);
             mbar_init(&empty[i], 1);
         }
-        gave_up = 0;
+        waits.gave_up = 0;
+        waits.issued = 0;
         mbar_init(&arrived, 1);
         mbar_init(&ended, 1);
         for (int i = 0; i < 2; ++i) {
@@ -500,7 +513,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                 for (int k = 0; k < t.summands; k += kK) {
                     in_time = mbar_wait(&empty[stage], phase);
                     if (!in_time) {
-                        gave_up = 1;
+                        waits.gave_up = 1;
                         break;
                     }
                     unsigned char *as = ring + stage * kStageBytes<NT, PAIR>, *bs = as + kA;
@@ -520,7 +533,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                         }
                         for (int i = 0; i < boxes; ++i) tensor_load<PAIR>(bs + i * kBox * kK * 2, &a.b, k, column + i * kBox, 0, bar);
                     }
-                    ++issued;
+                    waits.issued = ++issued;
                     if (++stage == S) stage = 0, phase ^= 1;
                 }
             }
@@ -544,19 +557,19 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                 const unsigned what =
                     1u << 4 | 1u << 7 | 1u << 10 | (kAcrossA ? 1u << 15 : 0u) | (kAcrossB ? 1u << 16 : 0u) | n / 8 << 17 | (unsigned)(LANES / 16) << 24;
                 for (int begin = 0; begin < t.summands; begin += part) {
-                    in_time = wait_for<PAIR>(&taken[turn], free_phase, &gave_up);
+                    in_time = wait_for<PAIR>(&taken[turn], free_phase, waits);
                     if (!in_time) break;
                     tmem_fence_after();
                     const unsigned d = tmem + turn * NT;
                     const int end = min(t.summands, begin + part);
                     for (int k = begin; k < end; k += kK) {
-                        in_time = wait_for(&full[stage], phase, &gave_up);
+                        in_time = wait_for(&full[stage], phase, waits);
                         if (F == DW && in_time && t.summands - k < kK) {  // it is there: warp 2 may end it
                             mbar_arrive(&arrived);
-                            in_time = wait_for(&ended, end_phase, &gave_up);
+                            in_time = wait_for(&ended, end_phase, waits);
                             end_phase ^= 1;
                             if constexpr (PAIR) {
-                                in_time = in_time && wait_for<true>(&there[stage], there_phase >> stage & 1, &gave_up);
+                                in_time = in_time && wait_for<true>(&there[stage], there_phase >> stage & 1, waits);
                                 there_phase ^= 1u << stage;
                             }
                         }
@@ -596,10 +609,10 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
             const int stage = (blocks - 1) % S;
             bool in_time;
             if (rank == 0) {
-                in_time = wait_for(&arrived, phase, &gave_up);
+                in_time = wait_for(&arrived, phase, waits);
                 phase ^= 1;
             } else {
-                in_time = wait_for(&full[stage], phase >> stage & 1, &gave_up);
+                in_time = wait_for(&full[stage], phase >> stage & 1, waits);
                 phase ^= 1u << stage;
             }
             if (!__all_sync(0xffffffffu, in_time)) break;
@@ -630,7 +643,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
             for (int begin = 0; begin < t.summands || begin == 0; begin += part) {
                 const bool any = t.summands > 0, last = begin + part >= t.summands;
                 if (any && !lost) {
-                    lost = !__all_sync(0xffffffffu, wait_for(&done[turn], phase, &gave_up));
+                    lost = !__all_sync(0xffffffffu, wait_for(&done[turn], phase, waits));
                     tmem_fence_after();
                 }
                 const unsigned from = tmem + turn * NT + mine, sums = tmem + NT + mine;

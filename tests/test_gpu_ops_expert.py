@@ -375,3 +375,23 @@ def test_gradients_one_behind_the_other():
             o = cuts[k % 3].tolist()
             alone_dx = ops.expert_matmul_grad(dy, cuts[k % 3], w=w).dx
             assert torch.equal(seen[k][0][o[0]:o[3]], alone_dx[o[0]:o[3]])
+
+
+@pytest.mark.parametrize("n,first", [((1 << 31) - 513, (1 << 31) - 1025), ((1 << 29) + 33, 1 << 29)])
+def test_sums_that_last(n, first):
+    """Up to as many rows as there may be, in one sum that takes seconds (3 and 13) on its block, which has a tile of another expert behind it; the end of the
+    sum, or only of the one behind it, is no multiple of 64 rows.  Sums of ones and twos: all but the last are multiples of 768 below 2^32,
+    which 32 bits hold, so that nothing is rounded but the result."""
+    if torch.cuda.mem_get_info()[0] < n * 40:
+        pytest.skip("wants %d GB" % (n * 40 >> 30))
+    experts = torch.cuda.get_device_properties(0).multi_processor_count + 1
+    x, dy = (torch.ones(n, 8, dtype=BF16, device=DEV) for _ in range(2))
+    x[:, 5] = 2.0
+    offsets = torch.full((experts + 1,), first, device=DEV)
+    offsets[0], offsets[-1] = 0, n
+    got = ops.expert_matmul_grad(dy, offsets, x=x)
+    ones = torch.zeros(experts, dtype=torch.float64, device=DEV)
+    ones[0], ones[-1] = first, n - first
+    want = ones[:, None, None].expand(experts, 8, 8).clone()
+    want[:, :, 5] *= 2.0
+    check(got.dw, want, U * want, "dw")
