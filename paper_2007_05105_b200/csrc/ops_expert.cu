@@ -305,21 +305,18 @@ template <bool CLUSTER> __device__ __noinline__ bool wait_long(u64 *bar, unsigne
 {
     // A sum may last (2^31 rows of 8 columns, one block's, 13 s), and who waits for its end or for the end of a group behind it is not late: the
     // limit holds for a time in which nothing was issued either.
-    for (unsigned seen = waits.issued;;) {
-        u64 t0 = 0;
-        for (unsigned spin = 0; spin < kPolls; ++spin) {
-            if (mbar_poll<CLUSTER>(smem_u32(bar), parity)) return true;
-            if (waits.gave_up) return false;
-            if ((spin & 63u) == 63u) {
-                u64 ns;
-                asm volatile("mov.u64 %0, %globaltimer;" : "=l"(ns));
-                if (t0 == 0) t0 = ns;
-                else if (ns - t0 > kWaitNs) break;
-            }
+    u64 t0 = 0;
+    unsigned seen = 0;
+    for (unsigned spin = 0; spin < kPolls; ++spin) {
+        if (mbar_poll<CLUSTER>(smem_u32(bar), parity)) return true;
+        if (waits.gave_up) return false;
+        if ((spin & 63u) == 63u) {
+            const unsigned issued = waits.issued;
+            u64 now;
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+            if (t0 == 0 || issued != seen) t0 = now, seen = issued, spin = 63;
+            else if (now - t0 > kWaitNs) break;
         }
-        const unsigned now = waits.issued;
-        if (now == seen) break;
-        seen = now;
     }
     waits.gave_up = 1;
     return false;
