@@ -57,7 +57,7 @@ struct ExpertArgs {
     int n_experts, wide_offsets;
     int lanes, columns, summed;    // extents; the one that is e's rows is 0
     int accumulate, out_aligned;
-    int in_parts;                  // sums are cut at kPart
+    int part;                      // summands at which sums are cut
     // Two kernels of one call that do not need each other: the first (leads) lets the second (follows) start as soon as all of its blocks
     // have passed their wait for what was before it - which is then done for the second too - so that the second's blocks take the SMs
     // that the first one's leave.  The second waits for the first before it ends, so that who waits for it has waited for both.
@@ -219,6 +219,7 @@ __device__ __forceinline__ void load_new(const bf16 *p, float (&x)[32])
 struct Experts {
     int *begin;  // [n + 1]: begin[e + 1] is where e ends
     int *tiles;  // [n + 1]
+    int *most;   // rows of the largest
 };
 
 // By one warp: offsets, ascending and within the rows, and running sums of the tiles.
@@ -240,11 +241,12 @@ template <Form F, int NT, int LANES> __device__ __forceinline__ void find_tiles(
         floor = __shfl_sync(0xffffffffu, v, 31);
     }
     __syncwarp();
-    int sum = 0;
+    int sum = 0, most = 0;
     for (int i = lane; i - lane < a.n_experts; i += 32) {
         int v = 0;
         if (i < a.n_experts) {
             const int rows = x.begin[i + 1] - x.begin[i];
+            most = max(most, rows);
             v = rows || (F == DW && !a.accumulate) ? lane_tiles * (((F == DW ? a.columns : rows) + NT - 1) / NT) : 0;
         }
 #pragma unroll
@@ -256,7 +258,11 @@ template <Form F, int NT, int LANES> __device__ __forceinline__ void find_tiles(
         if (i < a.n_experts) x.tiles[i + 1] = v;
         sum = __shfl_sync(0xffffffffu, v, 31);
     }
-    if (lane == 0) x.tiles[0] = 0;
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) {
+        x.tiles[0] = 0;
+        *x.most = most;
+    }
 }
 
 struct Tile {
@@ -454,9 +460,9 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
     __shared__ u64 full[S], there[S], empty[S], done[2], taken[2], arrived, ended;
     __shared__ unsigned tmem_base;
     __shared__ Waits waits;
-    __shared__ int begins[kMaxExperts + 1], tile_sums[kMaxExperts + 1];
+    __shared__ int begins[kMaxExperts + 1], tile_sums[kMaxExperts + 1], most_rows;
     unsigned char *staging = raw + (1024 - smem_u32(raw) % 1024) % 1024, *ring = staging + kStaging<O>;
-    const Experts x = {begins, tile_sums};
+    const Experts x = {begins, tile_sums, &most_rows};
     const int warp = threadIdx.x / 32, rank = PAIR ? (int)pair_rank() : 0;
 
     if (threadIdx.x == 0) {
@@ -492,7 +498,10 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
     tmem_fence_after();
     const unsigned tmem = tmem_base;
     const int n_tiles = x.tiles[a.n_experts], first_tile = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
-    const int part = a.in_parts ? kPart : 0x7fffffc0;  // more than there are rows
+    // Sums in parts have one buffer of tensor memory, the other holds what has been added up: only where a sum is that long.  (By the rows of
+    // all experts instead, us: 1024 x 4096, f32 dw of 8192 rows over 11 experts 96, 88 so; over 16 97 and 92; 1024 x 1024 over 64 61.1 and 62.5.)
+    const bool in_parts = (F == DW ? most_rows : a.summed) > a.part;
+    const int part = in_parts ? a.part : 0x7fffffc0;  // more than there are rows
     // operands whose summands lie across the rows in memory
     constexpr bool kAcrossA = F != Y, kAcrossB = F == DW;
 
@@ -582,7 +591,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                     }
                     if (!in_time) break;
                     mma_commit<PAIR>(&done[turn]);
-                    if (a.in_parts) {
+                    if (in_parts) {
                         free_phase ^= 1;
                     } else {
                         free_phase ^= turn;
@@ -652,7 +661,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                         else mbar_arrive(&taken[turn]);
                     }
                 };
-                if (a.in_parts && any && !lost) {  // to the running sum at once, so that the next part may begin before results are stored
+                if (in_parts && any && !lost) {  // to the running sum at once, so that the next part may begin before results are stored
                     for (int c = first; c < t.width; c += kEvery) {
                         unsigned now[32], before[32];
                         tmem_load(from + c, now);
@@ -679,7 +688,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                         unsigned now[32];
                         float v[32];
                         if (any && !lost) {
-                            tmem_load(a.in_parts ? sums + c : from + c, now);
+                            tmem_load(in_parts ? sums + c : from + c, now);
                             tmem_loaded(now);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(now[i]);
@@ -693,8 +702,8 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                     }
                 }
                 if (!any || lost) continue;
-                if (!a.in_parts) taken_now();
-                if (a.in_parts) {
+                if (!in_parts) taken_now();
+                if (in_parts) {
                     phase ^= 1;
                 } else {
                     phase ^= turn;
@@ -775,8 +784,7 @@ template <Form F, int NT, bool PAIR, typename O> cudaError_t run_tiles(const Exp
 template <Form F, int NT, bool PAIR = false> cudaError_t run_type(ExpertArgs &a, int dtype, cudaStream_t s)
 {
     const long long lane_tiles = ceil_div(a.lanes, PAIR ? 2 * kLanes : kLanes);
-    const long long summands = F == DW ? a.n_rows : a.summed;
-    a.in_parts = dtype == ADASCALE_F32 && summands > kPart;
+    a.part = dtype == ADASCALE_F32 ? kPart : 0x7fffffc0;
     // at most this many tiles: each expert may have one that is not full
     const long long tiles = F == DW ? a.n_experts * lane_tiles * ceil_div(a.columns, NT)
                                     : lane_tiles * (a.n_rows / NT + std::min<long long>(a.n_experts, a.n_rows));

@@ -395,3 +395,20 @@ def test_sums_that_last(n, first):
     want = ones[:, None, None].expand(experts, 8, 8).clone()
     want[:, :, 5] *= 2.0
     check(got.dw, want, U * want, "dw")
+
+
+@pytest.mark.parametrize("counts", [[768, 700], [5, 769, 768], [100] * 20 + [1537], [768, 0, 764]], ids=str)
+def test_sums_around_a_part(counts):
+    """Groups up to and beyond 768 rows, the length at which a float32 sum is cut, beside others; tolerances of short and of long sums."""
+    g = gen(sum(counts))
+    x, dy = normal(g, sum(counts), 320, dtype=BF16).abs(), normal(g, sum(counts), 264, dtype=BF16).abs()
+    offsets = offsets_of(counts)
+    dw0 = normal(g, len(counts), 264, 320)
+    got, more = ops.expert_matmul_grad(dy, offsets, x=x).dw, dw0.clone()
+    ops.expert_matmul_grad(dy, offsets, x=x, dw=more, accumulate=True)
+    for e, lo, hi in groups(offsets):
+        want = dy[lo:hi].double().t() @ x[lo:hi].double()
+        off = (48 * 2.0 ** -23 + 2 * U) * want
+        check(got[e], want, off, "dw")
+        whole = dw0[e].double() + want
+        check(more[e], whole, off + U * whole.abs(), "dw added")
