@@ -286,7 +286,8 @@ int64_t adascale_position_softmax_grad_workspace(int64_t heads, int64_t n_bucket
  *
  *   y[r, :] = w[e] x[r, :]
  *
- * x and w are bf16; sums are 32-bit (tensor cores), y is rounded once.  offsets has n_experts + 1 ascending numbers on the device;
+ * x and w are bf16; sums are 32-bit, y is rounded once.  The tensor cores cut where they add: a sum of terms of one sign comes out too small
+ * by up to 2e-6 of itself before it is stored as float32, 1e-4 (a twentieth of the rounding) as bf16, whatever its length.  offsets has n_experts + 1 ascending numbers on the device;
  * rows before the first or behind the last, up to n_rows, are neither used nor written.  Offsets outside 0 .. n_rows are
  * clamped, and one below an earlier one counts as that.  An expert may have no rows.
  * The rows of x and w start on 16-byte boundaries (ALIGNMENT otherwise): strides are multiples of 8 elements.  Widths may be odd.

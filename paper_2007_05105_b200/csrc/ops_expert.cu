@@ -27,9 +27,11 @@
 // experts, 59 MB of weights, 13 us.  Bound by the tensor cores' power and by what brings operands in (100 of the 116 us without results)
 // where rows are many, by the weights' bytes where they are few.
 //
-// The tensor cores cut, not round, when they add to the 32-bit sums: over m summands a float32 result loses 1.1e-9 m of itself
-// (4.4e-6 at 4096, measured; bf16 results do not show it).  For float32 results no sum is longer than kPart: the parts are
-// added up, rounded, by the warps that read them, in tensor memory.
+// The tensor cores cut, not round, when they add to the 32-bit sums: of sums of one sign 6e-7 to 1.3e-6 is lost over 768 summands, 8e-6 to
+// 1.4e-5 over 4096, 6.5e-5 to 8.2e-5 over 16384, 6e-9 m over m beyond (two units in the last place an instruction; measured).  So
+// no sum is longer than kPart for float32 results, kLongPart for bf16 ones, whose own rounding is 2e-3 to 4e-3: the parts are added up,
+// rounded, by the warps that read them, in tensor memory.  (bf16 dw of 131072 rows of one expert, 1024 x 1024: 578 us without parts,
+// 583 with parts of 32768, 590 of 16384, 603 of 8192.)
 #include "ops_common.cuh"
 
 #include <cuda.h>
@@ -41,7 +43,8 @@ namespace {
 constexpr int kMaxExperts = ADASCALE_EXPERT_MAX_EXPERTS;
 constexpr int kLanes = 128;      // of a block
 constexpr int kK = 64;           // summands of a stage: 128 bytes, the swizzle's width
-constexpr int kPart = 12 * kK;   // summands of one sum in tensor memory, for float32 results
+constexpr int kPart = 12 * kK;       // summands of one sum in tensor memory, for float32 results
+constexpr int kLongPart = 256 * kK;  // and for bf16 results
 constexpr int kResultWarps = 8;
 constexpr int kThreads = 128 + 32 * kResultWarps;  // warps: copies, matrix instructions, ends of groups, one idle; results
 constexpr int kDynamicMax = 216 * 1024;
@@ -562,15 +565,15 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                 const unsigned n = PAIR ? (t.width + 31) / 32 * 32 : (t.width + 15) / 16 * 16;
                 const unsigned what =
                     1u << 4 | 1u << 7 | 1u << 10 | (kAcrossA ? 1u << 15 : 0u) | (kAcrossB ? 1u << 16 : 0u) | n / 8 << 17 | (unsigned)(LANES / 16) << 24;
-                for (int begin = 0; begin < t.summands; begin += part) {
+                for (int left = t.summands; left > 0; left -= part) {
                     in_time = wait_for<PAIR>(&taken[turn], free_phase, waits);
                     if (!in_time) break;
                     tmem_fence_after();
                     const unsigned d = tmem + turn * NT;
-                    const int end = min(t.summands, begin + part);
-                    for (int k = begin; k < end; k += kK) {
+                    const int now = min(left, part);
+                    for (int k = 0; k < now; k += kK) {
                         in_time = wait_for(&full[stage], phase, waits);
-                        if (F == DW && in_time && t.summands - k < kK) {  // it is there: warp 2 may end it
+                        if (F == DW && in_time && left - k < kK) {  // it is there: warp 2 may end it
                             mbar_arrive(&arrived);
                             in_time = wait_for(&ended, end_phase, waits);
                             end_phase ^= 1;
@@ -585,7 +588,7 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                         const u64 da = operand(as, kAcrossA ? 8192 : 16), db = operand(as + kA, kAcrossB ? 8192 : 16);
 #pragma unroll
                         for (int i = 0; i < kK / 16; ++i)  // summands behind the last are zeros
-                            mma<PAIR>(d, da + (u64)(i * (kAcrossA ? 2048 : 32) >> 4), db + (u64)(i * (kAcrossB ? 2048 : 32) >> 4), what, k + i > begin);
+                            mma<PAIR>(d, da + (u64)(i * (kAcrossA ? 2048 : 32) >> 4), db + (u64)(i * (kAcrossB ? 2048 : 32) >> 4), what, k + i > 0);
                         mma_commit<PAIR>(&empty[stage]);
                         if (++stage == S) stage = 0, phase ^= 1;
                     }
@@ -646,8 +649,8 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
         bool lost = false;  // a wait ran out, in this tile or one before: NaN from here on
         for (int tile = first_tile; tile < n_tiles; tile += step) {
             find_tile<F, NT, LANES>(a, x, tile, rank, t);
-            for (int begin = 0; begin < t.summands || begin == 0; begin += part) {
-                const bool any = t.summands > 0, last = begin + part >= t.summands;
+            for (int left = t.summands; left > 0 || left == t.summands; left -= part) {
+                const bool any = t.summands > 0, first_part = left == t.summands, last = left <= part;
                 if (any && !lost) {
                     lost = !__all_sync(0xffffffffu, wait_for(&done[turn], phase, waits));
                     tmem_fence_after();
@@ -665,9 +668,9 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
                     for (int c = first; c < t.width; c += kEvery) {
                         unsigned now[32], before[32];
                         tmem_load(from + c, now);
-                        if (begin > 0) tmem_load(sums + c, before);
+                        if (!first_part) tmem_load(sums + c, before);
                         tmem_loaded(now);
-                        if (begin > 0) {
+                        if (!first_part) {
                             tmem_loaded(before);
 #pragma unroll
                             for (int i = 0; i < 32; i += 2) {
@@ -784,7 +787,7 @@ template <Form F, int NT, bool PAIR, typename O> cudaError_t run_tiles(const Exp
 template <Form F, int NT, bool PAIR = false> cudaError_t run_type(ExpertArgs &a, int dtype, cudaStream_t s)
 {
     const long long lane_tiles = ceil_div(a.lanes, PAIR ? 2 * kLanes : kLanes);
-    a.part = dtype == ADASCALE_F32 ? kPart : 0x7fffffc0;
+    a.part = dtype == ADASCALE_F32 ? kPart : kLongPart;
     // at most this many tiles: each expert may have one that is not full
     const long long tiles = F == DW ? a.n_experts * lane_tiles * ceil_div(a.columns, NT)
                                     : lane_tiles * (a.n_rows / NT + std::min<long long>(a.n_experts, a.n_rows));

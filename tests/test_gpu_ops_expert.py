@@ -412,3 +412,62 @@ def test_sums_around_a_part(counts):
         check(got[e], want, off, "dw")
         whole = dw0[e].double() + want
         check(more[e], whole, off + U * whole.abs(), "dw added")
+
+
+def check_rounded_once(got, want, off):
+    """bf16 results: half a step of the value, and `off` of it."""
+    half = torch.exp2(torch.floor(torch.log2(want.abs())) - 8)
+    check(got, want, half * (1 + 2.0 ** -20) + off * want.abs(), "rounded once")
+
+
+# A part of 16384 terms of one sign is cut 1024 times (16 terms an instruction), each time by two units in the last place of what it holds, which is
+# half of its end on average and whose unit is 2^-23 of it at most; each part's addition is rounded by 2^-24.
+LONG = 1024 * 2.0 ** -23
+
+
+@pytest.mark.parametrize("m", [64, 200])
+def test_long_sums_in_bf16(m):
+    """Sums so long that instructions that cut would lose more of them than the results' rounding: 2^23 rows of one expert (1e-2 of itself), beside
+    another's, and 2^20 summands of a product (1e-3, half of a step's half), on blocks alone and in pairs."""
+    g = gen(m)
+    counts = [(1 << 23) + 40, 77, 65536]
+    x, dy = (torch.empty(sum(counts), c, dtype=BF16, device=DEV).uniform_(0.5, 1.5, generator=g) for c in (32, m))
+    offsets = offsets_of(counts, ids=torch.int64)
+    got = ops.expert_matmul_grad(dy, offsets, x=x, wgrad_dtype=BF16).dw
+    for e, lo, hi in groups(offsets):
+        want = sum(dy[k:min(k + (1 << 20), hi)].double().t() @ x[k:min(k + (1 << 20), hi)].double() for k in range(lo, hi, 1 << 20))
+        check_rounded_once(got[e], want, LONG + 520 * U)
+    del x, dy
+    k = 1 << 20
+    x, w = (torch.empty(s, k, dtype=BF16, device=DEV).uniform_(0.5, 1.5, generator=g) for s in (70, m))
+    want = sum(x[:, c:c + (1 << 16)].double() @ w[:, c:c + (1 << 16)].double().t() for c in range(0, k, 1 << 16))
+    check_rounded_once(ops.expert_matmul(x, w.view(1, m, k), offsets_of([70])), want, LONG + 70 * U)
+    wide = torch.empty(1, k, m, dtype=BF16, device=DEV).uniform_(0.5, 1.5, generator=g)
+    want = sum(x[:, c:c + (1 << 16)].double() @ wide[0, c:c + (1 << 16)].double() for c in range(0, k, 1 << 16))
+    check_rounded_once(ops.expert_matmul_grad(x, offsets_of([70]), w=wide).dx, want, LONG + 70 * U)
+
+
+@pytest.mark.parametrize("counts", [[16384, 16000], [5, 16385, 16384], [32768, 32000], [5, 32769, 32768], [65537]], ids=str)
+def test_bf16_sums_around_a_part(counts):
+    """Whole numbers, so that every sum is exact but for the result's rounding."""
+    g = gen(sum(counts))
+    x, dy = (torch.randint(-2, 3, (sum(counts), c), device=DEV, generator=g).to(BF16) for c in (72, 136))
+    dw0 = torch.randint(-9, 9, (len(counts), 136, 72), device=DEV, generator=g).to(BF16)
+    offsets, more = offsets_of(counts), dw0.clone()
+    got = ops.expert_matmul_grad(dy, offsets, x=x, wgrad_dtype=BF16).dw
+    ops.expert_matmul_grad(dy, offsets, x=x, dw=more, accumulate=True)
+    for e, lo, hi in groups(offsets):
+        want = dy[lo:hi].double().t() @ x[lo:hi].double()
+        assert torch.equal(got[e], want.to(BF16)) and torch.equal(more[e], (want + dw0[e].double()).to(BF16))
+
+
+def test_as_many_rows_as_there_may_be_in_bf16():
+    n = (1 << 31) - 513
+    if torch.cuda.mem_get_info()[0] < n * 40:
+        pytest.skip("wants %d GB" % (n * 40 >> 30))
+    x, dy = (torch.ones(n, 8, dtype=BF16, device=DEV) for _ in range(2))
+    x[:, 5] = 2.0
+    got = ops.expert_matmul_grad(dy, torch.tensor([0, n], device=DEV), x=x, wgrad_dtype=BF16).dw
+    want = torch.full((1, 8, 8), float(n), dtype=torch.float64, device=DEV)
+    want[:, :, 5] *= 2.0
+    check_rounded_once(got, want, 2 * U)
