@@ -312,7 +312,8 @@ adascale_status adascale_expert_matmul(const adascale_expert_matmul_args *args, 
  *
  * Without `accumulate` all of dw is written, zeros for experts without rows; with it the sums are added to what dw holds and
  * experts without rows are not touched.  Adding to a float32 dw may be one addition per element by the L2 cache, which takes subnormal
- * numbers for zeros.  w = NULL leaves dx out, x = NULL dw.  Rows of dy, x and w start on 16-byte boundaries.
+ * numbers for zeros.  w = NULL leaves dx out, x = NULL dw.  Rows of dy, x and w start on 16-byte boundaries.  With n_rows = 0 none of dy, x
+ * and dx is looked at, and dw, where it is not NULL, is all zeros without `accumulate`, whether x is NULL or not.
  */
 typedef struct {
     const void *dy;      /* [n_rows, out_dim] of bf16 */

@@ -669,6 +669,8 @@ PyObject *expert_matmul_grad(PyObject *const *o)
 {
     const at::Tensor &dy = wanted(o[0], "dy"), &offsets = wanted(o[1], "offsets");
     const at::Tensor *x = tensor(o[2], "x"), *w = tensor(o[3], "w"), *given_x = tensor(o[7], "dx"), *given_w = tensor(o[8], "dw");
+    if (given_x && !w) refuse("dx: w is needed for it");
+    if (given_w && !x) refuse("dw: x is needed for it");
     if (!dy.is_cuda() || dy.dim() != 2) refuse("dy: a [rows, out] matrix on a CUDA device is expected");
     if (!x && !w) refuse("x (for dw) or w (for dx) is needed");
     if (offsets.numel() < 2) refuse("offsets: one more than the experts are expected");

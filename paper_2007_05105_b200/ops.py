@@ -308,7 +308,8 @@ def expert_matmul_grad(dy, offsets, x=None, w=None, dx_dtype=None, wgrad_dtype=N
 
     ``dx[r] = w[e]^T dy[r]`` where ``w`` is given (bfloat16 unless ``dx_dtype`` or ``dx`` say otherwise), ``dw[e] = sum of dy[r] x[r]^T`` where
     ``x`` is (float32 unless ``wgrad_dtype`` or ``dw``, a slot of a gradient row say, do); None otherwise.  With ``accumulate``
-    the sums are added to what ``dw`` holds and experts without rows are not touched, without it theirs are zeros.
+    the sums are added to what ``dw`` holds and experts without rows are not touched, without it theirs are zeros.  A ``dx`` without ``w``
+    and a ``dw`` without ``x`` are refused.
     """
     if stream is not None:
         with _on(stream, dy):

@@ -471,3 +471,15 @@ def test_as_many_rows_as_there_may_be_in_bf16():
     want = torch.full((1, 8, 8), float(n), dtype=torch.float64, device=DEV)
     want[:, :, 5] *= 2.0
     check_rounded_once(got, want, 2 * U)
+
+
+def test_gradients_that_would_not_be_written_are_refused():
+    """A slot of a gradient row that is given without what its gradient is made of would stay as it was."""
+    x, w, dy = (torch.zeros(*s, dtype=BF16, device=DEV) for s in ((10, 16), (2, 24, 16), (10, 24)))
+    offsets, dx, dw = offsets_of([5, 5]), torch.zeros(10, 16, device=DEV), torch.zeros(2, 24, 16, device=DEV)
+    for bad in [lambda: ops.expert_matmul_grad(dy, offsets, w=w, dw=dw), lambda: ops.expert_matmul_grad(dy, offsets, x=x, dx=dx),
+                lambda: ops.expert_matmul_grad(dy, offsets, w=w, dx=dx, dw=dw, accumulate=True), lambda: ops.expert_matmul_grad(dy, offsets, x=x, dx=dx, dw=dw)]:
+        with pytest.raises(ValueError):
+            bad()
+    got = ops.expert_matmul_grad(dy, offsets, w=w, accumulate=True)  # which is about dw alone
+    assert got.dw is None and got.dx.shape == (10, 16)

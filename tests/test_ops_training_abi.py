@@ -146,3 +146,12 @@ def test_tensors_on_the_host_are_refused(ops):  # noqa: F811
                 lambda: ops.expert_matmul_grad(t, ids, x=t), lambda: ops.grad_norm([t]), lambda: ops.clip_grads([t], 1.0)]:
         with pytest.raises(ValueError):
             bad()
+
+
+def test_slots_without_what_they_are_made_of_are_refused(ops):  # noqa: F811
+    """Before the tensors' device is looked at."""
+    import torch
+    x, w, dy, ids = torch.zeros(10, 16), torch.zeros(2, 24, 16), torch.zeros(10, 24), torch.zeros(3, dtype=torch.int64)
+    for given in (dict(w=w, dw=torch.zeros(2, 24, 16)), dict(x=x, dx=torch.zeros(10, 16))):
+        with pytest.raises(ValueError, match="needed for it"):
+            ops.expert_matmul_grad(dy, ids, **given)
