@@ -322,9 +322,23 @@ def expert_matmul_grad(dy, offsets, x=None, w=None, dx_dtype=None, wgrad_dtype=N
 # --------------------------------------------------------------------------
 
 
+def _listed(grads):
+    """As a list that has a first tensor, whose device the stream is to be on."""
+    try:
+        grads = list(grads)
+    except TypeError:
+        raise TypeError("grads is not a list of tensors") from None
+    if not grads:
+        raise ValueError("grads: the list is empty")
+    if not isinstance(grads[0], torch.Tensor):
+        raise TypeError("grads is not a tensor")
+    return grads
+
+
 def grad_norm(grads, workspace=None, stream=None):
-    """2-norm over all elements of a list of float32 and bfloat16 tensors, as a float32 scalar on the device."""
+    """2-norm over all elements of a list (or another iterable) of float32 and bfloat16 tensors, as a float32 scalar on the device."""
     if stream is not None:
+        grads = _listed(grads)
         with _on(stream, grads[0]):
             return grad_norm(grads, workspace)
     return _c.clip_grads(grads, None, None, 0.0, workspace)
@@ -338,6 +352,7 @@ def clip_grads(grads, max_norm, out=None, eps=1e-6, workspace=None, stream=None)
     ``workspace``: a uint8 tensor of at least ``clip_grads_workspace(len(grads))`` bytes, made here when not given.
     """
     if stream is not None:
+        grads = _listed(grads)
         with _on(stream, grads[0]):
             return clip_grads(grads, max_norm, out, eps, workspace)
     if max_norm is None:

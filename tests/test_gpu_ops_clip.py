@@ -201,3 +201,16 @@ def test_refusals():
                 lambda: ops.grad_norm([t], workspace=torch.zeros(16, dtype=torch.uint8, device=DEV))]:
         with pytest.raises(B.AdaScaleError):
             bad()
+
+
+def test_any_iterable_of_gradients():
+    grads = [normal(gen(k), 700 + k) for k in range(5)]
+    want, stream = ops.grad_norm(grads), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for how in (None, stream):
+        assert torch.equal(ops.grad_norm(tuple(grads), stream=how), want) and torch.equal(ops.grad_norm((t for t in grads), stream=how), want)
+        by_name = {str(k): t.clone() for k, t in enumerate(grads)}
+        out = {k: torch.empty_like(t) for k, t in by_name.items()}
+        assert torch.equal(ops.clip_grads(by_name.values(), 3.0, out=out.values(), stream=how), want)
+        torch.cuda.synchronize()
+        check_all(grads, list(out.values()), want, 3.0)

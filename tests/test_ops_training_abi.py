@@ -155,3 +155,15 @@ def test_slots_without_what_they_are_made_of_are_refused(ops):  # noqa: F811
     for given in (dict(w=w, dw=torch.zeros(2, 24, 16)), dict(x=x, dx=torch.zeros(10, 16))):
         with pytest.raises(ValueError, match="needed for it"):
             ops.expert_matmul_grad(dy, ids, **given)
+
+
+@pytest.mark.parametrize("stream", [None, 0])
+def test_what_is_no_list_of_gradients(ops, stream):  # noqa: F811
+    """Refused in the same way with a stream and without."""
+    for call in (lambda g: ops.grad_norm(g, stream=stream), lambda g: ops.clip_grads(g, 1.0, stream=stream)):
+        for empty in ([], (), iter(())):
+            with pytest.raises(ValueError, match="empty"):
+                call(empty)
+        for bad in (5, [None], (3,), None):
+            with pytest.raises(TypeError):
+                call(bad)
