@@ -421,3 +421,75 @@ def test_in_place_where_rows_share_accesses(shape, dtype):
         check_gradient(again, p, dprobs, case, None, "between poison")
         for w in whole:
             assert bool(torch.isnan(w[:before]).all()) and bool(torch.isnan(w[before + scores.numel():]).all())
+
+
+def check_table_exactly(shape, dtype, case, shift, seed, what):
+    """The table's gradient of weights 1/4 and whole numbers: products, rows' sums, differences and sums by bucket are multiples of 1/16
+    which 32 bits hold, so that nothing is rounded, in whatever order it is added up."""
+    g = gen(seed)
+    B, H, lq, lk = shape
+    live = torch.stack([live_of(case, b, lq, lk) for b in range(B)])[:, None]
+    whole = torch.randint(-3, 4, shape, device=DEV, generator=g).double()
+    # in whole rows of even length: as many of either sign, so that g is a small number
+    pairs = whole[..., :lk // 2]
+    whole = torch.cat([pairs, -pairs, whole[..., 2 * (lk // 2):]], dim=-1).gather(-1, torch.rand(shape, device=DEV, generator=g).argsort(dim=-1))
+
+    def tensor(values):
+        t = torch.empty(B, H, lq, lk + shift, dtype=dtype, device=DEV)[..., shift:] if shift else torch.empty(shape, dtype=dtype, device=DEV)
+        return t.copy_(values).masked_fill_(~live, float("nan"))
+    probs, dprobs = tensor(torch.full(shape, 0.25, device=DEV)), tensor(whole)
+    kept = torch.where(live, whole, 0.0)
+    terms = torch.where(live, 0.25 * (kept - 0.25 * kept.sum(-1, keepdim=True)), 0.0)
+    want, size = (torch.zeros(case["buckets"], H, dtype=torch.float64, device=DEV) for _ in range(2))
+    for b in range(B):
+        at = buckets_of(case, b, lq, lk).reshape(-1)
+        want.index_add_(0, at, terms[b].reshape(H, -1).t())
+        size.index_add_(0, at, terms[b].abs().reshape(H, -1).t())
+    assert float(size.max()) * 16 < 2 ** 24 and bool(want.any() or lk == 1)
+    got = ops.position_softmax_grad(probs, dprobs, case["buckets"], **how(case))
+    assert torch.equal(got.dtable.double(), want), what
+    assert torch.equal(ops.position_softmax_grad(probs, dprobs, case["buckets"], **how(case), want_dscores=False).dtable, got.dtable)
+
+
+BUCKETS = [(2, 2, False), (4, 2, True), (8, 3, True), (7, 20, False), (16, 16384, True), (32, 128, True), (64, 65, False), (128, 33, True),
+           (128, 65, False), (128, 1000, True), (32, 16384, False), (30, 90, True), (64, 150, False)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("buckets,distance,both", BUCKETS)
+def test_every_bucket_of_the_gradient(buckets, distance, both, dtype):
+    """Keys on either side of queries before, among and behind them: near ones, which are summed by distance, and far ones; rows on
+    16-byte boundaries and off them, of every kind of group."""
+    for lk in (1, 50, 110, 160, 301, 700, 1500, 2 * distance + 41):
+        for shift in (0, 3):
+            starts = torch.tensor([0, lk // 2, lk + distance // 2, -(distance // 3), lk - 1], device=DEV)
+            case = dict(buckets=buckets, distance=distance, both=both, causal=False, scale=0.125, lengths=None, starts=starts)
+            check_table_exactly((5, 2, 3 if lk < 5000 else 1, lk), dtype, case, shift, lk, "%d keys, shift %d" % (lk, shift))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("buckets,distance", [(7, 20), (32, 128), (64, 65), (64, 150), (128, 1000)])
+def test_every_bucket_of_the_gradient_with_masks(buckets, distance, dtype):
+    for lk in (7, 66, 128, 250, 301, 700, 1500):
+        for shift in (0, 1):
+            lengths = torch.tensor([lk, 0, lk // 2 + 1, lk - 1], device=DEV)
+            for causal, starts in ((True, torch.tensor([0, 3, lk // 3, lk - 4], device=DEV)), (False, None)):
+                case = dict(buckets=buckets, distance=distance, both=False, causal=causal, scale=0.125, lengths=lengths, starts=starts)
+                check_table_exactly((4, 3, 40, lk), dtype, case, shift, lk, "%d keys, shift %d" % (lk, shift))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(70000, 2, 1, 3), (2, 5000, 2, 9), (1, 1, 70000, 5), (9, 1, 3000, 20), (300, 4, 64, 64)])
+def test_table_gradient_of_many_rows(shape, dtype):
+    case = dict(buckets=8, distance=6, both=True, causal=False, scale=0.125, lengths=None, starts=None)
+    if shape[0] > 1000:  # the formula a batch at a time would take minutes: all of them are alike
+        g = gen(1)
+        dprobs = torch.randint(-3, 4, shape, device=DEV, generator=g).double()
+        terms = 0.25 * (dprobs - 0.25 * dprobs.sum(-1, keepdim=True))
+        at = buckets_of(case, 0, *shape[2:]).reshape(-1)
+        want, size = (torch.zeros(8, shape[1], dtype=torch.float64, device=DEV).index_add_(0, at, t.sum(0).reshape(shape[1], -1).t()) for t in (terms, terms.abs()))
+        assert float(size.max()) * 16 < 2 ** 24 and bool(want.any())
+        got = ops.position_softmax_grad(torch.full(shape, 0.25, dtype=dtype, device=DEV), dprobs.to(dtype), 8, **how(case))
+        assert torch.equal(got.dtable.double(), want)
+    else:
+        check_table_exactly(shape, dtype, case, 0, 2, "many rows")
