@@ -488,9 +488,11 @@ template <Form F, int NT, bool PAIR, typename O> __global__ void __launch_bounds
     }
     if (warp == 1) tmem_alloc<PAIR>(&tmem_base, kColumns);
     if (warp == 3 && elected()) {
-        prefetch_map(&a.a);
-        prefetch_map(&a.b);
-        prefetch_map(&a.c);
+        if (a.n_rows > 0) {  // without rows there are no operands' maps
+            prefetch_map(&a.a);
+            prefetch_map(&a.b);
+        }
+        if (a.out_aligned) prefetch_map(&a.c);
     }
     if (!a.follows) griddep_wait();
     if (a.leads) griddep_launch();
