@@ -250,8 +250,8 @@ bool overlapping(const adascale_clip_grads_args &a)
 
 adascale_status check_clip(const adascale_clip_grads_args &a)
 {
+    if (a.n_tensors > ADASCALE_CLIP_MAX_TENSORS) return ADASCALE_ERR_TOO_LARGE;  // for which there is no workspace either
     if (a.n_tensors < 0 || !a.norm || !a.workspace) return ADASCALE_ERR_INVALID_ARG;
-    if (a.n_tensors > ADASCALE_CLIP_MAX_TENSORS) return ADASCALE_ERR_TOO_LARGE;
     if (a.n_tensors && (!a.grads || !a.numels || !a.grad_dtypes || (a.out && !a.out_dtypes))) return ADASCALE_ERR_INVALID_ARG;
     if (a.out && !(std::isfinite(a.max_norm) && a.max_norm >= 0.f && std::isfinite(a.eps) && a.eps >= 0.f)) return ADASCALE_ERR_INVALID_ARG;
     if (a.workspace_bytes < adascale_clip_grads_workspace(a.n_tensors)) return ADASCALE_ERR_INVALID_ARG;

@@ -214,3 +214,11 @@ def test_any_iterable_of_gradients():
         assert torch.equal(ops.clip_grads(by_name.values(), 3.0, out=out.values(), stream=how), want)
         torch.cuda.synchronize()
         check_all(grads, list(out.values()), want, 3.0)
+
+
+def test_as_many_tensors_as_there_may_be():
+    t = torch.full((3,), 2.0, device=DEV)
+    want = math.sqrt(12 * 65536)
+    assert abs(float(ops.grad_norm([t] * 65536)) - want) <= NORM * want
+    with pytest.raises(B.AdaScaleError, match="maximum"):
+        ops.grad_norm([t] * 65537)

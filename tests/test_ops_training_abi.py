@@ -167,3 +167,8 @@ def test_what_is_no_list_of_gradients(ops, stream):  # noqa: F811
         for bad in (5, [None], (3,), None):
             with pytest.raises(TypeError):
                 call(bad)
+
+
+def test_a_list_too_long_is_too_large(ops):  # noqa: F811
+    """Also with the workspace that its size asks for, which is none."""
+    assert clip(ops, n=65537, workspace=None, workspace_bytes=ops.clip_grads_workspace(65537)) == 5
