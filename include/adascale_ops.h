@@ -28,8 +28,9 @@
  *     adascale_step may follow directly, with ADASCALE_FLAG_GRADS_READY too.
  *   - Results are the same bits from run to run: no sum depends on the order in which blocks run.
  *   - Inputs and outputs must not overlap unless a field says so.
- *   - Waits inside a kernel (for its own copies and instructions) are bounded, by seconds in which it gets no further: results that were not computed because one ran
- *     out are NaN, and the kernel ends when its copies in flight have come.  The call has returned by then: no status tells of it.
+ *   - Waits inside a kernel (for its own copies and instructions) are bounded, by seconds in which it gets no further: results that
+ *     were not computed because one ran out are NaN, and the kernel ends when its copies in flight have come.  The call has
+ *     returned by then: no status tells of it.
  *   - Errors: INVALID_ARG (null pointer, negative size, unknown enum, stride below the row's length,
  *     non-finite constant, workspace too small), ALIGNMENT (a pointer not aligned to its element size),
  *     TOO_LARGE (beyond a maximum below), CUDA (a launch failed).  Nothing is enqueued after an error of the first three kinds.
@@ -342,6 +343,7 @@ adascale_status adascale_expert_matmul_grad(const adascale_expert_matmul_grad_ar
  * then); otherwise it overlaps neither another output nor a gradient.  No output may be given twice.
  * Sums are 64-bit joins of 32-bit sums of a few terms; where squares leave the 32-bit range they are 64-bit throughout.  A NaN
  * anywhere makes norm and all of out NaN; with an infinity and no NaN norm is inf, c 0, and out 0, NaN in the infinity's place.
+ * A call per gradient row clips each row by its own norm: what adascale_step then sees, and its gain is of, are clipped gradients.
  * workspace: at least adascale_clip_grads_workspace(n_tensors) bytes, 16-byte aligned, contents neither expected nor kept.
  */
 typedef struct {

@@ -22,10 +22,10 @@
 // many, and 48 KB are what the L2 cache does not deliver in the time that they are worked on.
 // Every block works out the tiles from the offsets by itself: no host, no kernel before.
 //
-// Measured on a B200: 16384 rows over 16 experts of 1024 -> 4096 in 116 us (1180 TFLOP/s; 137 us under the power cap of a long run, where
-// the library's batched product of equal groups takes 121 to 125), dx and dw of 8192 rows over 8 experts 62 us each; 16 rows over 8
-// experts, 59 MB of weights, 13 us.  Bound by the tensor cores' power and by what brings operands in (100 of the 116 us without results)
-// where rows are many, by the weights' bytes where they are few.
+// Measured on a B200: 16384 rows over 16 experts of 1024 -> 4096 in 113 us (1220 TFLOP/s; 133 to 136 us under the power cap of a long run,
+// where equal groups take 129 and the library's batched product of them 127), dx of 8192 rows over 8 experts 59 us, dw 62; 16 rows over 8
+// experts, 59 MB of weights, 13 to 16 us.  Bound by the tensor cores' power, by what brings operands in, and by results (16 us of
+// the first, whose stores do not all hide) where rows are many, by the weights' bytes where they are few.
 //
 // The tensor cores cut, not round, when they add to the 32-bit sums: of sums of one sign 6e-7 to 1.3e-6 is lost over 768 summands, 8e-6 to
 // 1.4e-5 over 4096, 6.5e-5 to 8.2e-5 over 16384, 6e-9 m over m beyond (two units in the last place an instruction; measured).  So
@@ -804,7 +804,9 @@ template <Form F> cudaError_t run_wide(ExpertArgs &a, int dtype, cudaStream_t s)
     const long long summands = F == DW ? a.n_rows / a.n_experts : a.summed;
     return a.lanes > kLanes && summands > 512 ? run_type<F, 256, true>(a, dtype, s) : run_type<F, 256>(a, dtype, s);
 }
-// Tiles of tokens are as wide as the rows of an expert on average, as far as the host knows.
+// Tiles of tokens are as wide as the rows of an expert on average, as far as the host knows: rows before the first offset and behind the last
+// count.  With room for 16384 more behind 16 to 2048 rows of 8 or 16 experts a product takes 0.8 to 1.4 us longer (11.3 and 12.1, 8.7 and 10.1),
+// a weights' gradient, which then takes pairs, 3 to 5 (14.3 and 17.4, 22.2 and 27.3): a caller who knows the rows gives a slice.
 template <Form F> cudaError_t run_tokens(ExpertArgs &a, int dtype, cudaStream_t s, int n)
 {
     if (n == 32) return run_type<F, 32>(a, dtype, s);

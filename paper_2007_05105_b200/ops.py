@@ -296,6 +296,7 @@ def expert_matmul(x, w, offsets, out=None, out_dtype=None, stream=None):
     x: [rows, in], w: [experts, out, in], bfloat16, their rows on 16-byte boundaries.  offsets: int32 or int64 [experts + 1], ascending, on
     the device: nothing is copied to the host.  Sums are 32-bit; ``out`` is bfloat16 or float32 (``out_dtype``, bfloat16
     when not given).  Rows before the first offset and behind the last are neither used nor written: in a new ``out`` they hold anything.
+    (Many of them cost a little: widths of tiles go by all rows.  Where the host knows better, give a slice.)
     """
     if stream is not None:
         with _on(stream, x):
@@ -348,7 +349,8 @@ def clip_grads(grads, max_norm, out=None, eps=1e-6, workspace=None, stream=None)
     """``out[k] = min(1, max_norm / (norm + eps)) * grads[k]`` with the norm over all of ``grads``; returns the norm.
 
     ``out``: a tensor for each gradient, of its shape and order in memory - the slots of a gradient row, in that row's type - or
-    None: in place.  Nothing waits for the device.  Elements of a tensor are adjacent; no two outputs overlap.
+    None: in place.  Nothing waits for the device.  Elements of a tensor are adjacent; no two outputs overlap.  Rows that are clipped one by one
+    have norms of their own: the step's gain is that of the clipped gradients.
     ``workspace``: a uint8 tensor of at least ``clip_grads_workspace(len(grads))`` bytes, made here when not given.
     """
     if stream is not None:
