@@ -338,7 +338,8 @@ template <bool CLUSTER = false> __device__ __forceinline__ bool wait_for(u64 *ba
 
 // ---- results -------------------------------------------------------------------------------
 // Two warps share 32 lanes and take every other 32 columns of them, each by way of its room of 32 x 32 results in shared memory and a
-// copy by tensor map, which leaves out what lies outside the matrix.
+// copy by tensor map, which leaves out what lies outside the matrix - in units of 16 bytes: of a row that ends inside 16 it would write
+// zeros behind the end.  So the map ends before, and the rows' last elements are stored by the warp.
 
 // Until the last copy out of the warp's room has read it; lane 0 has the copies.
 __device__ __forceinline__ void room_wait()
@@ -386,7 +387,12 @@ template <typename O> __device__ __forceinline__ void store_tokens(const ExpertA
 #pragma unroll
     for (int i = 0; i < 32; ++i) put(room + i * 32 + me, v[i]);
     if (n == 32) {
-        copy_out([&] { tensor_store(&a.c, lane0, token, 0, room); });
+        const int all = a.lanes - lane0, copied = all / V * V;  // of this token's row; lane0 is a multiple of V
+        copy_out([&] {
+            if (copied > 0) tensor_store(&a.c, lane0, token, 0, room);
+        });
+        if (all < 32)
+            for (int e = copied; e < all; ++e) out[me * a.ld_out + e] = room[me * 32 + e];
         return;
     }
     __syncwarp();  // the last tokens of a group: what follows them is not ours
@@ -410,11 +416,27 @@ template <typename O> __device__ __forceinline__ void store_rows(const ExpertArg
     constexpr int V = 16 / sizeof(O), kPieces = 32 / V;
     const int me = threadIdx.x % 32;
     if (lane0 >= a.lanes) return;
-    // a float32 gradient that is copied is added to on the way; others are read, added to in 32 bits and rounded once
-    const bool add_here = a.accumulate && (sizeof(O) == 2 || !a.out_aligned);
     O *p = static_cast<O *>(a.out) + expert * a.stride_out + (lane0 + me) * a.ld_out + column;
-    if (add_here && lane0 + me < a.lanes) {
-        if (a.out_aligned && n == 32) {
+    if (!a.out_aligned || (column + 32 > a.columns && a.columns % V != 0)) {  // nothing of these 32 x 32 is copied
+        if (lane0 + me < a.lanes)
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                float x[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) x[e] = v[j * V + e] + (a.accumulate && j * V + e < n ? load_new(p + j * V + e) : 0.f);
+                if (a.out_aligned && (j + 1) * V <= n) {
+                    store_vec<V>(p + j * V, x);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (j * V + e < n) put(p + j * V + e, x[e]);
+                }
+            }
+        return;
+    }
+    // a float32 gradient is added to on the way; others are read, added to in 32 bits and rounded once
+    if (sizeof(O) == 2 && a.accumulate && lane0 + me < a.lanes) {
+        if (n == 32) {
             float old[32];
             load_new(p, old);
 #pragma unroll
@@ -424,13 +446,6 @@ template <typename O> __device__ __forceinline__ void store_rows(const ExpertArg
             for (int i = 0; i < 32; ++i)
                 if (i < n) v[i] += load_new(p + i);
         }
-    }
-    if (!a.out_aligned) {
-        if (lane0 + me < a.lanes)
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < n) put(p + i, v[i]);
-        return;
     }
     room_wait();
 #pragma unroll
@@ -768,11 +783,12 @@ bool operand_map(CUtensorMap *map, const void *p, const Extents &x, int box)
 {
     return make_map(map, p, x, ADASCALE_BF16, 64, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-// Results, 32 x 32 a copy, where their rows allow it.
-bool result_map(ExpertArgs &e, const Extents &x, int dtype, CUtensorMapSwizzle swizzle)
+// Results, 32 x 32 a copy, where their rows allow it: as far as they go in whole 16 bytes.
+bool result_map(ExpertArgs &e, Extents x, int dtype, CUtensorMapSwizzle swizzle)
 {
     const int b = elem_bytes(dtype);
-    e.out_aligned = on(e.out, 16) && (x.rows <= 1 || x.ld * b % 16 == 0) && (x.n <= 1 || x.stride * b % 16 == 0);
+    x.cols = x.cols * b / 16 * 16 / b;
+    e.out_aligned = x.cols > 0 && on(e.out, 16) && (x.rows <= 1 || x.ld * b % 16 == 0) && (x.n <= 1 || x.stride * b % 16 == 0);
     return !e.out_aligned || make_map(&e.c, e.out, x, dtype, 32, 32, swizzle);
 }
 

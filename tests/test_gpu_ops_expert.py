@@ -483,3 +483,59 @@ def test_gradients_that_would_not_be_written_are_refused():
             bad()
     got = ops.expert_matmul_grad(dy, offsets, w=w, accumulate=True)  # which is about dw alone
     assert got.dw is None and got.dx.shape == (10, 16)
+
+
+def inside(shape, dtype, rows_around=3):
+    """A matrix (or one of each expert) inside a wide buffer, its rows on 16-byte boundaries, with NaN on all sides; and whether those are left."""
+    *e, n, d = shape
+    whole = torch.full((*e, n + 2 * rows_around, 512), float("nan"), dtype=dtype, device=DEV)
+    view = whole[..., rows_around:n + rows_around, 64:64 + d]
+
+    def intact():
+        around = torch.isnan(whole)
+        around[..., rows_around:n + rows_around, 64:64 + d] = True
+        assert bool(around.all()), "written beside the matrix"
+    return view, intact
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [1, 7, 9, 12, 20, 33, 36, 39, 100, 130, 257])
+def test_rows_that_end_inside_16_bytes(width, dtype):
+    """Slices of wider matrices, on 16-byte boundaries: what is beside them, in the same 16 bytes, is someone else's."""
+    g = gen(width)
+    for counts in ([20], [32, 3], [70, 0, 64], [300, 520]):
+        n, E = sum(counts), len(counts)
+        offsets = offsets_of(counts)
+        x, narrow, dy = normal(g, n, 40, dtype=BF16), padded(normal(g, n, width, dtype=BF16), 1), normal(g, n, 40, dtype=BF16)
+        to, back = padded(normal(g, E, width, 40, dtype=BF16), 1), padded(normal(g, E, 40, width, dtype=BF16), 1)
+        y, y_intact = inside((n, width), dtype)
+        ops.expert_matmul(x, to, offsets, out=y)
+        forward_check(x, to, offsets, y, torch.zeros_like(y), "y")
+        y_intact()
+        for accumulate in (False, True):
+            dx, dx_intact = inside((n, width), dtype)
+            dw, dw_intact = inside((E, 40, width), dtype)
+            before = normal(g, E, 40, width, dtype=dtype)
+            dw.copy_(before)
+            ops.expert_matmul_grad(dy, offsets, x=narrow, w=back, dx=dx, dw=dw, accumulate=accumulate)
+            for e, lo, hi in groups(offsets):
+                want, mag = dy[lo:hi].double() @ back[e].double(), dy[lo:hi].double().abs() @ back[e].double().abs()
+                check(dx[lo:hi], want, 80 * U * mag + rounding(dtype) * want.abs() * 1.01, "dx")
+                part, mag = dy[lo:hi].double().t() @ narrow[lo:hi].double(), dy[lo:hi].double().abs().t() @ narrow[lo:hi].double().abs()
+                whole = part + before[e].double() if accumulate else part
+                check(dw[e], whole, 2 * max(hi - lo, 1) * U * mag + U * whole.abs() + rounding(dtype) * whole.abs() * 1.01, "dw")
+            dx_intact()
+            dw_intact()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_one_row_of_weights_between_other_slots(dtype):
+    """A single output: its gradient's row is a slot of any width, with others' right behind it."""
+    g = gen(6)
+    for width in (3, 13, 37, 250):
+        x, dy, offsets = padded(normal(g, 90, width, dtype=BF16), 1), padded(normal(g, 90, 1, dtype=BF16), 1), offsets_of([90])
+        row = torch.full((width + 40,), float("nan"), dtype=dtype, device=DEV)
+        ops.expert_matmul_grad(dy, offsets, x=x, dw=row[16:16 + width].view(1, 1, width))
+        want = dy.double().t() @ x.double()
+        check(row[16:16 + width].view(1, width), want, 180 * U * (dy.double().abs().t() @ x.double().abs()) + rounding(dtype) * want.abs() * 1.01, "dw")
+        assert bool(torch.isnan(row[:16]).all()) and bool(torch.isnan(row[16 + width:]).all())
