@@ -4,6 +4,7 @@ Nothing in it can fault or hang: the waits only end earlier, and those for copie
 """
 import ctypes as C
 import os
+import shutil
 import subprocess
 
 import pytest
@@ -22,6 +23,8 @@ from test_gpu_ops_expert import offsets_of  # noqa: E402
 @pytest.fixture(scope="module")
 def hasty(tmp_path_factory):
     """The calls with waits of one poll, each of which may last 20 us: shorter than the sums below."""
+    if shutil.which(build._nvcc()) is None:
+        pytest.skip("needs nvcc")
     out = str(tmp_path_factory.mktemp("hasty") / "hasty.so")
     source = os.path.join(os.path.dirname(build.OPS_SOURCE), "ops_expert.cu")
     subprocess.check_call([build._nvcc()] + build.NVCC_FLAGS + ["-DADASCALE_EXPERT_POLLS=0u", "-o", out, source])
